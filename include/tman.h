@@ -246,6 +246,58 @@ tman_status tman_mpgemv_static(const void *packed, size_t packed_bytes, const vo
                                void *y_f16, int M, int K, int N, int bits, int group,
                                unsigned int *status_dev, tman_stream_t stream);
 
+/* ---- microscaled 4-bit floating point ------------------------------------------------------------
+ * (No counterpart in the paper.)  Matrices of e2m1 values (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; sign in bit 3 of the
+ * code) with a scale per block of `block` consecutive k of a row:
+ *   block = 32   scale e8m0, 2^(byte - 127), 255 is NaN; row scales are 1 and not stored
+ *   block = 16   scale e4m3, times an fp32 scale per row (a checkpoint's one scale per matrix: the same number in every row)
+ * A matrix has `rows` rows of K values; weights are [N][K], one row per output channel, quantized activations [M][K].  Both are held in
+ * the same packed buffer, which the products read by linear copies (layout: csrc/f4.cuh).
+ *   - rows >= 1, any number; K a multiple of block (else TMAN_ERR_SHAPE).  dtype: 0 = fp16, 1 = bf16 (else TMAN_ERR_UNSUPPORTED).
+ *   - ldx, ldy: values from a row of x or y to the next, at least the row's length.  x is 16-byte aligned and ldx a multiple of 8
+ *     (TMAN_ERR_SHAPE); y of the products needs the alignment of its type only.
+ *   - packed and workspace are 256-byte aligned.  The rules on the stream order of packed buffers below hold for these too;
+ *     tman_pack_f4 and tman_quantize_rows_f4 may be followed by any call. */
+
+/* Bytes of the packed buffer of `rows` rows. */
+tman_status tman_packed_bytes_f4(int rows, int K, int block, size_t *out_bytes /*host*/);
+
+/* Bytes of scratch, op as for tman_workspace_bytes: 0 = tman_mpgemv_f4, 1 = tman_mpgemm_f4, 2 = the other calls.  Prepared with
+ * tman_workspace_init like every workspace. */
+tman_status tman_workspace_bytes_f4(int op, int M, int K, int N, int block, size_t *out_bytes /*host*/);
+
+/* A checkpoint's matrix into the packed layout.  codes: uint8 [rows][K/2], the even k in the low half of a byte; scales: uint8
+ * [rows][K/block]; row_scale: fp32 [rows] or NULL (ones; not read for block = 32). */
+tman_status tman_pack_f4(const uint8_t *codes, const uint8_t *scales, const float *row_scale, int rows, int K, int block,
+                         void *packed, size_t packed_bytes, tman_stream_t stream);
+
+/* Inverse of tman_pack_f4; row_scale may be NULL. */
+tman_status tman_unpack_f4(const void *packed, size_t packed_bytes, int rows, int K, int block, uint8_t *codes, uint8_t *scales,
+                           float *row_scale, void *workspace, size_t ws_bytes, tman_stream_t stream);
+
+/* Quantization of rows (activations before tman_mpgemm_f4, or a weight matrix).  With top the largest magnitude of a block:
+ *   block = 32   scale 2^(floor(log2 top) - 2), 2^-127 at least
+ *   block = 16   row scale r = the least power of two with max|row| <= 2688 r (2^-126 at least; 1 for a row of zeros),
+ *                scale = e4m3(top / (6 r))
+ * and the codes of x / (scale r), all roundings to nearest, ties to even, saturating.  The codes are those of the exact quotients.  A
+ * block that holds an infinity or a NaN gets the scale NaN and stands for NaN; row scales are of the finite values.  The bytes of the
+ * buffer that belong to no row are not specified. */
+tman_status tman_quantize_rows_f4(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, size_t packed_bytes,
+                                  tman_stream_t stream);
+
+/* The values a packed matrix stands for, rounded once to fp16 or bf16.  x is the output, rows as for the input of
+ * tman_quantize_rows_f4. */
+tman_status tman_dequant_rows_f4(const void *packed, size_t packed_bytes, int rows, int K, int block, void *x, int ldx, int dtype,
+                                 void *workspace, size_t ws_bytes, tman_stream_t stream);
+
+/* Decode: y[m][n] = sum_k x[m][k] w[n][k] for 16-bit activations, M in [1, 8]; x and y have the type `dtype`. */
+tman_status tman_mpgemv_f4(const void *packed, size_t packed_bytes, const void *x, int ldx, void *y, int ldy, int dtype,
+                           int M, int K, int N, int block, void *workspace, size_t ws_bytes, tman_stream_t stream);
+
+/* Both operands in 4 bits: y[m][n] = sum_k a[m][k] w[n][k], M >= 1, `a` packed (tman_quantize_rows_f4) with the weights' block. */
+tman_status tman_mpgemm_f4(const void *packed, size_t packed_bytes, const void *a_packed, size_t a_bytes, void *y, int ldy, int dtype,
+                           int M, int K, int N, int block, void *workspace, size_t ws_bytes, tman_stream_t stream);
+
 /* ---- test-only extractors of the integer / table intermediates -------------------------- */
 
 /* idx uint8 [bits][K/4][N]: the 4-bit table index of every (plane, 4 activations, column)

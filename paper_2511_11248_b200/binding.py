@@ -20,12 +20,15 @@ STATUS_NAMES = {
     4: "TMAN_ERR_BUFFER_TOO_SMALL", 5: "TMAN_ERR_BAD_PACKED", 6: "TMAN_ERR_CUDA", 7: "TMAN_ERR_TIMEOUT",
 }
 OP_GEMV, OP_GEMM, OP_AUX, OP_TERNARY = 0, 1, 2, 3
+DTYPE_F16, DTYPE_BF16 = 0, 1            # of the 16-bit matrices beside 4-bit floating-point ones
 
 EXPORTS = [
     "tman_status_string", "tman_version", "tman_packed_bytes", "tman_workspace_bytes",
     "tman_workspace_init", "tman_read_status", "tman_pack_weights", "tman_unpack_weights",
     "tman_mpgemv", "tman_mpgemm", "tman_debug_indices", "tman_debug_luts", "tman_debug_gemm_plan", "tman_mpgemv_static", "tman_mpgemv_grouped",
     "tman_debug_microbench", "tman_debug_cluster_capacity", "tman_debug_gemm_plan_for", "tman_debug_gemv_plan", "tman_debug_wait_timeout", "tman_debug_mpgemm_variant", "tman_quantize_rows", "tman_mpgemv_ternary", "tman_dequant_ternary_int8", "tman_debug_role_stamps", "tman_quantize_rows_i8", "tman_mpgemm_ternary_i8",
+    "tman_packed_bytes_f4", "tman_workspace_bytes_f4", "tman_pack_f4", "tman_unpack_f4", "tman_quantize_rows_f4", "tman_dequant_rows_f4",
+    "tman_mpgemv_f4", "tman_mpgemm_f4",
 ]
 
 _lib = None
@@ -75,6 +78,14 @@ def lib() -> C.CDLL:
         L.tman_dequant_ternary_int8.argtypes = [vp, sz, i, i, i, vp, vp, sz, vp]
         L.tman_quantize_rows.argtypes = [vp, i, i, i, vp, vp, vp]
         L.tman_mpgemv_ternary.argtypes = [vp, sz, vp, vp, C.c_float, vp, vp, i, i, i, i, vp, sz, vp]
+        L.tman_packed_bytes_f4.argtypes = [i, i, i, C.POINTER(sz)]
+        L.tman_workspace_bytes_f4.argtypes = [i, i, i, i, i, C.POINTER(sz)]
+        L.tman_pack_f4.argtypes = [vp, vp, vp, i, i, i, vp, sz, vp]
+        L.tman_unpack_f4.argtypes = [vp, sz, i, i, i, vp, vp, vp, vp, sz, vp]
+        L.tman_quantize_rows_f4.argtypes = [vp, i, i, i, i, i, vp, sz, vp]
+        L.tman_dequant_rows_f4.argtypes = [vp, sz, i, i, i, vp, i, i, vp, sz, vp]
+        L.tman_mpgemv_f4.argtypes = [vp, sz, vp, i, vp, i, i, i, i, i, i, vp, sz, vp]
+        L.tman_mpgemm_f4.argtypes = [vp, sz, vp, sz, vp, i, i, i, i, i, i, vp, sz, vp]
         L.tman_debug_mpgemm_variant.argtypes = [i, vp, sz, vp, vp, i, i, i, i, i, vp, vp, sz, vp]
         for name in EXPORTS[2:]:
             getattr(L, name).restype = C.c_int
@@ -85,7 +96,8 @@ def lib() -> C.CDLL:
                               "`python -m paper_2511_11248_b200.build`; there is no fallback path") from e
         _marshal.bind(*[C.cast(getattr(L, name), vp).value for name in (
             "tman_mpgemv", "tman_mpgemv_grouped", "tman_mpgemm", "tman_quantize_rows", "tman_quantize_rows_i8",
-            "tman_mpgemv_ternary", "tman_mpgemm_ternary_i8", "tman_pack_weights")])
+            "tman_mpgemv_ternary", "tman_mpgemm_ternary_i8", "tman_pack_weights", "tman_quantize_rows_f4", "tman_dequant_rows_f4",
+            "tman_mpgemv_f4", "tman_mpgemm_f4")])
         _fast = _marshal
         _lib = L
     return _lib
@@ -248,6 +260,55 @@ def tman_mpgemv_ternary(packed, a, row_scale, w_scale, y, acc, M, K, N, group, w
     st = _hot().mpgemv_ternary(packed, a, row_scale, w_scale, y, acc, M, K, N, group, ws, _stream(stream))
     if st:
         raise TmanError(st, "tman_mpgemv_ternary")
+
+
+# ---- microscaled 4-bit floating point ----
+
+def tman_packed_bytes_f4(rows: int, K: int, block: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().tman_packed_bytes_f4(rows, K, block, C.byref(out)), "tman_packed_bytes_f4")
+    return int(out.value)
+
+
+def tman_workspace_bytes_f4(op: int, M: int, K: int, N: int, block: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().tman_workspace_bytes_f4(op, M, K, N, block, C.byref(out)), "tman_workspace_bytes_f4")
+    return int(out.value)
+
+
+def tman_pack_f4(codes, scales, row_scale, rows, K, block, packed, stream=None) -> None:
+    _check(lib().tman_pack_f4(_ptr(codes), _ptr(scales), _ptr(row_scale), rows, K, block, _ptr(packed),
+                              packed.numel() * packed.element_size(), _stream(stream)), "tman_pack_f4")
+
+
+def tman_unpack_f4(packed, rows, K, block, codes, scales, row_scale, workspace, stream=None) -> None:
+    _check(lib().tman_unpack_f4(_ptr(packed), packed.numel() * packed.element_size(), rows, K, block, _ptr(codes), _ptr(scales),
+                                _ptr(row_scale), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)),
+           "tman_unpack_f4")
+
+
+def tman_quantize_rows_f4(x, ldx, dtype, rows, K, block, packed, stream=None) -> None:
+    st = _hot().quantize_rows_f4(x, ldx, dtype, rows, K, block, packed, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_quantize_rows_f4")
+
+
+def tman_dequant_rows_f4(packed, rows, K, block, x, ldx, dtype, workspace, stream=None) -> None:
+    st = _hot().dequant_rows_f4(packed, rows, K, block, x, ldx, dtype, workspace, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_dequant_rows_f4")
+
+
+def tman_mpgemv_f4(packed, x, ldx, y, ldy, dtype, M, K, N, block, workspace, stream=None) -> None:
+    st = _hot().mpgemv_f4(packed, x, ldx, y, ldy, dtype, M, K, N, block, workspace, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_mpgemv_f4")
+
+
+def tman_mpgemm_f4(packed, a, y, ldy, dtype, M, K, N, block, workspace, stream=None) -> None:
+    st = _hot().mpgemm_f4(packed, a, y, ldy, dtype, M, K, N, block, workspace, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_mpgemm_f4")
 
 
 GEMM_VARIANTS = {"product": 0, "convert_dq": 1, "load_full": 2, "sequential": 3}

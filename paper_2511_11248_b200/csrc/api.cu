@@ -1,6 +1,7 @@
 // C ABI: argument validation and dispatch.  No allocation, no global state, no device sync
 // (except tman_read_status, whose job is to wait).
 #include "common.cuh"
+#include "f4.cuh"
 
 using namespace tman;
 
@@ -260,6 +261,117 @@ tman_status tman_debug_role_stamps(const void *workspace, size_t ws_bytes, int c
     if (!aligned_to(workspace, 256)) return TMAN_ERR_SHAPE;
     if (ws_bytes < mpgemm_workspace_bytes(1, 128, 8)) return TMAN_ERR_BUFFER_TOO_SMALL;
     return mpgemm_read_stamps(workspace, ctas, out_host, reinterpret_cast<cudaStream_t>(stream));
+}
+
+// ---- microscaled 4-bit floating point ----
+// A packed matrix and the workspace of a call that reads it.
+static tman_status check_f4(const void *packed, size_t packed_bytes, int rows, int K, int block)
+{
+    if (!packed) return TMAN_ERR_NULL;
+    const tman_status st = f4_check(rows, K, block);
+    if (st != TMAN_OK) return st;
+    if (packed_bytes < f4_layout(rows, K, block).total) return TMAN_ERR_BUFFER_TOO_SMALL;
+    return aligned_to(packed, 256) ? TMAN_OK : TMAN_ERR_SHAPE;
+}
+static tman_status check_f4_workspace(const void *workspace, size_t ws_bytes, size_t need)
+{
+    if (!workspace) return TMAN_ERR_NULL;
+    if (ws_bytes < need) return TMAN_ERR_BUFFER_TOO_SMALL;
+    return aligned_to(workspace, 256) ? TMAN_OK : TMAN_ERR_SHAPE;
+}
+static tman_status check_f4_rows(const void *x, int ldx, int dtype, int K)
+{
+    if (!x) return TMAN_ERR_NULL;
+    if (dtype != kF4Half && dtype != kF4Bf16) return TMAN_ERR_UNSUPPORTED;
+    if (ldx < K || ldx % 8 != 0 || !aligned_to(x, 16)) return TMAN_ERR_SHAPE;
+    return TMAN_OK;
+}
+static tman_status check_f4_output(const void *y, int ldy, int dtype, int N)
+{
+    if (!y) return TMAN_ERR_NULL;
+    if (dtype != kF4Half && dtype != kF4Bf16) return TMAN_ERR_UNSUPPORTED;
+    return ldy < N || !aligned_to(y, 2) ? TMAN_ERR_SHAPE : TMAN_OK;
+}
+#define TMAN_F4_CHECK(call)                        \
+    do {                                           \
+        const tman_status st_ = (call);            \
+        if (st_ != TMAN_OK) return st_;            \
+    } while (0)
+
+tman_status tman_packed_bytes_f4(int rows, int K, int block, size_t *out_bytes)
+{
+    if (!out_bytes) return TMAN_ERR_NULL;
+    TMAN_F4_CHECK(f4_check(rows, K, block));
+    *out_bytes = f4_layout(rows, K, block).total;
+    return TMAN_OK;
+}
+
+tman_status tman_workspace_bytes_f4(int op, int M, int K, int N, int block, size_t *out_bytes)
+{
+    if (!out_bytes) return TMAN_ERR_NULL;
+    TMAN_F4_CHECK(f4_check(N, K, block));
+    TMAN_F4_CHECK(f4_check(M, K, block));
+    if (op < 0 || op > 2) return TMAN_ERR_UNSUPPORTED;
+    if (op == 0 && M > 8) return TMAN_ERR_SHAPE;
+    *out_bytes = op == 2 ? kWsStatusBytes : f4_workspace_bytes(op, M, K, N, block);
+    return TMAN_OK;
+}
+
+tman_status tman_pack_f4(const uint8_t *codes, const uint8_t *scales, const float *row_scale, int rows, int K, int block, void *packed,
+                         size_t packed_bytes, tman_stream_t stream)
+{
+    if (!codes || !scales) return TMAN_ERR_NULL;
+    TMAN_F4_CHECK(check_f4(packed, packed_bytes, rows, K, block));
+    if (!aligned_to(row_scale, 4)) return TMAN_ERR_SHAPE;
+    return launch_f4_pack(codes, scales, row_scale, rows, K, block, packed, reinterpret_cast<cudaStream_t>(stream));
+}
+
+tman_status tman_unpack_f4(const void *packed, size_t packed_bytes, int rows, int K, int block, uint8_t *codes, uint8_t *scales, float *row_scale,
+                           void *workspace, size_t ws_bytes, tman_stream_t stream)
+{
+    if (!codes || !scales) return TMAN_ERR_NULL;
+    TMAN_F4_CHECK(check_f4(packed, packed_bytes, rows, K, block));
+    TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, kWsStatusBytes));
+    if (!aligned_to(row_scale, 4)) return TMAN_ERR_SHAPE;
+    return launch_f4_unpack(packed, rows, K, block, codes, scales, row_scale, static_cast<uint32_t *>(workspace), reinterpret_cast<cudaStream_t>(stream));
+}
+
+tman_status tman_quantize_rows_f4(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, size_t packed_bytes,
+                                  tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_f4(packed, packed_bytes, rows, K, block));
+    TMAN_F4_CHECK(check_f4_rows(x, ldx, dtype, K));
+    return launch_f4_quantize(x, ldx, dtype, rows, K, block, packed, reinterpret_cast<cudaStream_t>(stream));
+}
+
+tman_status tman_dequant_rows_f4(const void *packed, size_t packed_bytes, int rows, int K, int block, void *x, int ldx, int dtype, void *workspace,
+                                 size_t ws_bytes, tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_f4(packed, packed_bytes, rows, K, block));
+    TMAN_F4_CHECK(check_f4_rows(x, ldx, dtype, K));
+    TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, kWsStatusBytes));
+    return launch_f4_dequant(packed, rows, K, block, x, ldx, dtype, static_cast<uint32_t *>(workspace), reinterpret_cast<cudaStream_t>(stream));
+}
+
+tman_status tman_mpgemv_f4(const void *packed, size_t packed_bytes, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N,
+                           int block, void *workspace, size_t ws_bytes, tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_f4(packed, packed_bytes, N, K, block));
+    if (M < 1 || M > 8) return TMAN_ERR_SHAPE;
+    TMAN_F4_CHECK(check_f4_rows(x, ldx, dtype, K));
+    TMAN_F4_CHECK(check_f4_output(y, ldy, dtype, N));
+    TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, f4_workspace_bytes(0, M, K, N, block)));
+    return launch_f4_gemv(packed, x, ldx, y, ldy, dtype, M, K, N, block, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+tman_status tman_mpgemm_f4(const void *packed, size_t packed_bytes, const void *a_packed, size_t a_bytes, void *y, int ldy, int dtype, int M, int K,
+                           int N, int block, void *workspace, size_t ws_bytes, tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_f4(packed, packed_bytes, N, K, block));
+    TMAN_F4_CHECK(check_f4(a_packed, a_bytes, M, K, block));
+    TMAN_F4_CHECK(check_f4_output(y, ldy, dtype, N));
+    TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, f4_workspace_bytes(1, M, K, N, block)));
+    return launch_f4_gemm(packed, a_packed, y, ldy, dtype, M, K, N, block, workspace, reinterpret_cast<cudaStream_t>(stream));
 }
 
 tman_status tman_debug_indices(const void *packed, int K, int N, int bits, int group,

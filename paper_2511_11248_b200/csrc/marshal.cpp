@@ -15,7 +15,7 @@
 
 namespace {
 
-enum { F_GEMV, F_GROUPED, F_GEMM, F_QUANT, F_QUANT_I8, F_TERNARY, F_TERNARY_I8, F_PACK, F_COUNT };
+enum { F_GEMV, F_GROUPED, F_GEMM, F_QUANT, F_QUANT_I8, F_TERNARY, F_TERNARY_I8, F_PACK, F_QUANT_F4, F_DEQUANT_F4, F_GEMV_F4, F_GEMM_F4, F_COUNT };
 void *g_fn[F_COUNT];
 PyObject *g_data_ptr, *g_nbytes, *g_numel, *g_element_size;                // interned attribute names
 
@@ -230,6 +230,62 @@ PyObject *py_pack(PyObject *, PyObject *const *args, Py_ssize_t n)
     TMAN_ISSUE(tman_pack_weights, ((const uint8_t *)codes, scales, (const uint8_t *)zeros, K, N, bits, group, pk, pb, s));
 }
 
+PyObject *py_quant_f4(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_QUANT_F4;
+    if (!arity(n, 8)) return nullptr;
+    Reader r(args);
+    size_t pb = 0;
+    void *x = r.ptr();
+    const int ldx = r.num(), dtype = r.num(), rows = r.num(), K = r.num(), block = r.num();
+    void *pk = r.buf(&pb);
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_quantize_rows_f4, (x, ldx, dtype, rows, K, block, pk, pb, s));
+}
+
+PyObject *py_dequant_f4(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_DEQUANT_F4;
+    if (!arity(n, 9)) return nullptr;
+    Reader r(args);
+    size_t pb = 0, wb = 0;
+    void *pk = r.buf(&pb);
+    const int rows = r.num(), K = r.num(), block = r.num();
+    void *x = r.ptr();
+    const int ldx = r.num(), dtype = r.num();
+    void *ws = r.buf(&wb);
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_dequant_rows_f4, (pk, pb, rows, K, block, x, ldx, dtype, ws, wb, s));
+}
+
+PyObject *py_gemv_f4(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_GEMV_F4;
+    if (!arity(n, 12)) return nullptr;
+    Reader r(args);
+    size_t pb = 0, wb = 0;
+    void *pk = r.buf(&pb), *x = r.ptr();
+    const int ldx = r.num();
+    void *y = r.ptr();
+    const int ldy = r.num(), dtype = r.num(), M = r.num(), K = r.num(), N = r.num(), block = r.num();
+    void *ws = r.buf(&wb);
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_mpgemv_f4, (pk, pb, x, ldx, y, ldy, dtype, M, K, N, block, ws, wb, s));
+}
+
+PyObject *py_gemm_f4(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_GEMM_F4;
+    if (!arity(n, 11)) return nullptr;
+    Reader r(args);
+    size_t pb = 0, ab = 0, wb = 0;
+    void *pk = r.buf(&pb), *a = r.buf(&ab), *y = r.ptr();
+    const int ldy = r.num(), dtype = r.num(), M = r.num(), K = r.num(), N = r.num(), block = r.num();
+    void *ws = r.buf(&wb);
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_mpgemm_f4, (pk, pb, a, ab, y, ldy, dtype, M, K, N, block, ws, wb, s));
+}
+
 // bind(addresses): the loaded library's entry points, in the order of the enumeration above
 PyObject *py_bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -249,7 +305,8 @@ PyMethodDef methods[] = {
     TMAN_METHOD("bind", py_bind), TMAN_METHOD("mpgemv", py_gemv), TMAN_METHOD("mpgemv_grouped", py_grouped),
     TMAN_METHOD("mpgemm", py_gemm), TMAN_METHOD("quantize_rows", py_quant), TMAN_METHOD("quantize_rows_i8", py_quant_i8),
     TMAN_METHOD("mpgemv_ternary", py_ternary), TMAN_METHOD("mpgemm_ternary_i8", py_ternary_i8),
-    TMAN_METHOD("pack_weights", py_pack), {nullptr, nullptr, 0, nullptr}};
+    TMAN_METHOD("pack_weights", py_pack), TMAN_METHOD("quantize_rows_f4", py_quant_f4), TMAN_METHOD("dequant_rows_f4", py_dequant_f4),
+    TMAN_METHOD("mpgemv_f4", py_gemv_f4), TMAN_METHOD("mpgemm_f4", py_gemm_f4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -72,3 +72,22 @@ def pack_case(case, dev=None, device="cuda"):
 
 def to_f64(t: torch.Tensor) -> np.ndarray:
     return t.detach().cpu().to(torch.float64).numpy()
+
+
+# ---- microscaled 4-bit floating point ----
+
+def alloc_f4(rows, K, block, device="cuda"):
+    return guarded_bytes(B.tman_packed_bytes_f4(rows, K, block), "packed 4-bit matrix", device)
+
+
+def alloc_workspace_f4(op, M, K, N, block, device="cuda"):
+    ws = guarded_bytes(B.tman_workspace_bytes_f4(op, M, K, N, block), "workspace", device)
+    B.tman_workspace_init(ws)
+    return ws
+
+
+def alloc_matrix(rows, ld, dtype, fill=float("nan"), device="cuda"):
+    """[rows][ld] of a 16-bit type between guard bytes, pre-filled so that unwritten elements show."""
+    y = guarded_bytes(rows * ld * 2, f"matrix [{rows}][{ld}]", device).view(dtype).view(rows, ld)
+    y.fill_(fill)
+    return y
