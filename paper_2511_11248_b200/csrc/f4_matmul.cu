@@ -1,5 +1,5 @@
 // Products with microscaled 4-bit weights: y[m][n] = row_scale[n] sum_k x[m][k] w[n][k], x in 16 bits (decode) or 4 bits (any M).
-#include "f4.cuh"
+#include "f4_stream.cuh"
 
 namespace tman {
 
@@ -9,47 +9,6 @@ __device__ __forceinline__ float f4_value(const uint8_t *packed, const F4Layout 
     const uint32_t c = packed[L.codes_off + f4_code_at(r, k, L.height8, L.units)];
     const float2 p = __half22float2(f4_pair(c));
     return (k & 1 ? p.y : p.x) * f4_scale_value<BLOCK>(packed[L.scales_off + f4_scale_at(r, k / BLOCK, BLOCK, L.units)]);
-}
-
-// A warp has one output channel and up to eight rows of x, its lanes eight values of k each.
-template <int BLOCK, typename T>
-__global__ void __launch_bounds__(256) f4_gemv_kernel(const uint8_t *packed, F4Layout L, const T *x, int ldx, T *y, int ldy, int M, int K, int N, uint32_t *status)
-{
-    if (!f4_header_matches(packed, N, K, BLOCK)) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(status, 0u, (uint32_t)TMAN_ERR_BAD_PACKED);
-        return;
-    }
-    const int n = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (n >= N) return;
-    float acc[8] = {};
-    for (int k = lane * 8; k < K; k += 256) {
-        const uint32_t c = *reinterpret_cast<const uint32_t *>(packed + L.codes_off + f4_code_at(n, k, L.height8, L.units));
-        const float s = f4_scale_value<BLOCK>(packed[L.scales_off + f4_scale_at(n, k / BLOCK, BLOCK, L.units)]);
-        float w[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float2 p = __half22float2(f4_pair(c >> (8 * e)));
-            w[2 * e] = p.x * s;
-            w[2 * e + 1] = p.y * s;
-        }
-#pragma unroll
-        for (int m = 0; m < 8; ++m)
-            if (m < M) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(x + (size_t)m * ldx + k);
-                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 p = f4_to_float2<T>(u[e]);
-                    acc[m] = fmaf(p.x, w[2 * e], fmaf(p.y, w[2 * e + 1], acc[m]));
-                }
-            }
-    }
-    const float rs = BLOCK == 16 ? reinterpret_cast<const float *>(packed + L.rows_off)[n] : 1.f;
-#pragma unroll
-    for (int m = 0; m < 8; ++m) {
-        for (int o = 16; o; o >>= 1) acc[m] += __shfl_xor_sync(0xffffffffu, acc[m], o);
-        if (m < M && lane == 0) y[(size_t)m * ldy + n] = f4_from_float<T>(acc[m] * rs);
-    }
 }
 
 // 64 rows x 64 channels a CTA, 4 x 4 a thread, 32 values of k at a time through shared memory.
@@ -89,16 +48,26 @@ __global__ void __launch_bounds__(256) f4_gemm_kernel(const uint8_t *packed, F4L
 
 size_t f4_workspace_bytes(int, int, int, int, int) { return kWsStatusBytes; }
 
-template <int BLOCK, typename T>
-static tman_status gemv_as(const void *packed, const void *x, int ldx, void *y, int ldy, int M, int K, int N, void *ws, cudaStream_t s)
+static F4StreamParams stream_params(const void *packed, const void *a, const void *x, int ldx, void *y, int ldy, int M, int K, int N, int block, void *ws)
 {
-    f4_gemv_kernel<BLOCK, T><<<(unsigned)((N + 7) / 8), 256, 0, s>>>(static_cast<const uint8_t *>(packed), f4_layout(N, K, BLOCK), static_cast<const T *>(x), ldx,
-                                                                   static_cast<T *>(y), ldy, M, K, N, static_cast<uint32_t *>(ws));
-    return launch_status();
+    const F4Layout L = f4_layout(N, K, block), A = f4_layout(M, K, block);
+    F4StreamParams p = {};
+    p.w = static_cast<const uint8_t *>(packed);
+    p.a = static_cast<const uint8_t *>(a);
+    p.x = x;
+    p.y = y;
+    p.status = static_cast<uint32_t *>(ws);
+    p.w_codes = L.codes_off; p.w_scales = L.scales_off; p.w_rows = L.rows_off;
+    p.a_codes = A.codes_off; p.a_scales = A.scales_off; p.a_rows = A.rows_off;
+    p.M = M; p.K = K; p.N = N; p.ldx = ldx; p.ldy = ldy;
+    p.units = L.units;
+    p.height8 = L.height8;
+    return p;
 }
 template <int BLOCK, typename T>
 static tman_status gemm_as(const void *packed, const void *a, void *y, int ldy, int M, int K, int N, void *ws, cudaStream_t s)
 {
+    if (M <= kStreamMaxRows) return launch_stream<BLOCK, T, false>(stream_params(packed, a, nullptr, 0, y, ldy, M, K, N, BLOCK, ws), s);
     const long long grid = (long long)((N + 63) / 64) * ((M + 63) / 64);
     if (grid > 0x7FFFFFFFll) return TMAN_ERR_SHAPE;
     f4_gemm_kernel<BLOCK, T><<<(unsigned)grid, 256, 0, s>>>(static_cast<const uint8_t *>(packed), f4_layout(N, K, BLOCK), static_cast<const uint8_t *>(a),
@@ -108,8 +77,9 @@ static tman_status gemm_as(const void *packed, const void *a, void *y, int ldy, 
 
 tman_status launch_f4_gemv(const void *packed, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N, int block, void *ws, cudaStream_t s)
 {
-    if (dtype == kF4Half) return block == 32 ? gemv_as<32, __half>(packed, x, ldx, y, ldy, M, K, N, ws, s) : gemv_as<16, __half>(packed, x, ldx, y, ldy, M, K, N, ws, s);
-    return block == 32 ? gemv_as<32, __nv_bfloat16>(packed, x, ldx, y, ldy, M, K, N, ws, s) : gemv_as<16, __nv_bfloat16>(packed, x, ldx, y, ldy, M, K, N, ws, s);
+    const F4StreamParams p = stream_params(packed, nullptr, x, ldx, y, ldy, M, K, N, block, ws);
+    if (dtype == kF4Half) return block == 32 ? launch_stream<32, __half, true>(p, s) : launch_stream<16, __half, true>(p, s);
+    return block == 32 ? launch_stream<32, __nv_bfloat16, true>(p, s) : launch_stream<16, __nv_bfloat16, true>(p, s);
 }
 tman_status launch_f4_gemm(const void *packed, const void *a, void *y, int ldy, int dtype, int M, int K, int N, int block, void *ws, cudaStream_t s)
 {

@@ -1,0 +1,395 @@
+// Products of few rows with microscaled 4-bit weights, bound by the weights' bytes.
+//
+// y[m][n] = row_scale[n] sum_k x[m][k] w[n][k].  A CTA has 128 channels (the rows of the tensor-core tile, one per lane of tensor memory) and a
+// contiguous share of the units of k; the rows of x are the tile's columns.  Weights and their scales stream through a ring of shared memory
+// by linear bulk copies (the packed layout is the operands' layout), the scales go on to tensor memory by tcgen05.cp, one thread issues
+// the block-scaled MMAs: no instruction touches a weight.
+//
+// DIGITS: x in 16 bits.  The tensor cores multiply e2m1 with e2m1, so a row of x becomes eight columns of balanced octal digits.  In a block of 16
+// or 32 values with largest magnitude in [2^E, 2^(E+1)) every x is the fixed-point number 2^(E-20) X, X = round(x 2^(20-E)) < 2^21, off by
+// at most 2^(E-21); X = sum_j n_j 8^j with eight digits n_j in [-4, 4], and n_j / 2 is an e2m1 value.  Column 8 m + j holds the digits n_j of
+// row m, the block's scale (2^E as e8m0; as e4m3 relative to a power of two of the row) is the columns' block scale, and
+// x w = 4 sum_j 8^(j-7) (column j): products of digits and weights are exact, sums are in fp32.  Eight warps cut x up while the weights arrive.
+//
+// Otherwise: x is a packed 4-bit matrix, whose units are loaded as they are.
+//
+// The CTAs of a tile's shares of k form a cluster and add their sums through each other's shared memory, in the order of the shares.
+#pragma once
+
+#include "f4.cuh"
+#include "sm100_ptx.cuh"
+
+#include <type_traits>
+
+namespace tman {
+namespace {
+
+constexpr int kStreamThreads = 320;      // warp 0: loads, warp 1: MMAs, warps 2..9: digits, epilogue
+constexpr int kStreamMaxRows = 128;      // of a packed x
+constexpr int kStreamMaxSplit = 8;
+constexpr int kStreamMaxStages = 24;
+constexpr int kDigitLbo = 144, kDigitSbo = 4 * kDigitLbo;      // (a bank's width more than the core matrices: the digits' stores meet no conflict)
+
+struct F4StreamParams {
+    const uint8_t *w, *a;                // packed weights, packed x
+    const void *x;
+    void *y;
+    uint32_t *status;
+    size_t w_codes, w_scales, w_rows, a_codes, a_scales, a_rows;
+    int M, K, N, ldx, ldy, units, height8, split, stages, stage_bytes, cols;
+};
+
+template <int BLOCK, bool DIGITS>
+__host__ __device__ inline int stream_b_bytes(int M, int cols) { return DIGITS ? (M + 1) / 2 * 2 * kDigitSbo : cols * 64; }
+
+// Balanced octal digits of eight numbers, as e2m1 codes: word j of the result holds digit j of number i in bits 4 i.
+// y[i] = X + sum_{j<7} 4 8^j + 2 8^7, so that octal digit j of y is n_j + 4 (of the top one n_7 + 2).
+__device__ __forceinline__ void digit_codes(const uint32_t (&y)[8], uint32_t (&out)[8])
+{
+    uint32_t c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        // octal digits into nibbles
+        uint32_t v = y[i] + (y[i] & 0x00FFF000u) * 15u;
+        v += (v & 0x0FC00FC0u) * 3u;
+        v += (v & 0x38383838u) + 0x20000000u;
+        // f = n + 4 into sign and magnitude: f & 3 for n >= 0; 8 + (4 - f) = 9 + (f ^ 3) below
+        const uint32_t neg = ~(v >> 2) & 0x11111111u;
+        c[i] = ((v & 0x33333333u) ^ (neg * 3u)) + neg * 9u;
+    }
+    // transpose: nibbles of pairs, then bytes
+    uint32_t even[4], odd[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        even[i] = bsel(0x0F0F0F0Fu, c[2 * i], c[2 * i + 1] << 4);
+        odd[i] = bsel(0x0F0F0F0Fu, c[2 * i] >> 4, c[2 * i + 1]);
+    }
+    auto bytes = [](const uint32_t (&w)[4], uint32_t *o) {
+        const uint32_t a = __byte_perm(w[0], w[1], 0x5140), b = __byte_perm(w[2], w[3], 0x5140);
+        const uint32_t d = __byte_perm(w[0], w[1], 0x7362), e = __byte_perm(w[2], w[3], 0x7362);
+        o[0] = __byte_perm(a, b, 0x5410);
+        o[2] = __byte_perm(a, b, 0x7632);
+        o[4] = __byte_perm(d, e, 0x5410);
+        o[6] = __byte_perm(d, e, 0x7632);
+    };
+    bytes(even, out);
+    bytes(odd, out + 1);
+}
+
+template <int BLOCK, typename T, bool DIGITS>
+__global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_constant__ F4StreamParams p)
+{
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) uint64_t full_bar[kStreamMaxStages], empty_bar[kStreamMaxStages], acc_bar;
+    __shared__ uint32_t tmem_slot, row_top[8];
+    __shared__ float w_row[128], a_row[kStreamMaxRows];
+    constexpr int SB = BLOCK == 32 ? 512 : 1024, CHUNKS = SB / 512;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % p.split, tile = blockIdx.x / p.split;
+    const int u0 = (int)((long long)p.units * rank / p.split), nu = (int)((long long)p.units * (rank + 1) / p.split) - u0;
+    const int h = min(kF4Tile, p.height8 - tile * kF4Tile);
+    const int pairs = (p.M + 1) / 2, b_bytes = stream_b_bytes<BLOCK, DIGITS>(p.M, p.cols);
+    const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), accf = smem_u32(&acc_bar), ring = smem_u32(smem);
+    const uint32_t off_sfa = kF4Tile * 64, off_b = off_sfa + SB, off_sfb = off_b + (uint32_t)b_bytes;
+    const int tmem_cols = p.cols <= 32 ? 64 : p.cols <= 96 ? 128 : 256;
+    bool ok = true;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(full0 + 8 * s, DIGITS ? 1 + pairs : 1);
+            mbar_init(empty0 + 8 * s, 1);
+        }
+        mbar_init(accf, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x < 8) row_top[threadIdx.x] = 0u;
+    if (warp == 1) {
+        tcgen05_alloc(smem_u32(&tmem_slot), (uint32_t)tmem_cols);
+        tcgen05_relinquish();
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_slot;
+
+    if (warp == 0) {
+        if (elect_one()) {
+            const uint8_t *codes = p.w + p.w_codes + (size_t)tile * p.units * (kF4Tile * 64) + (size_t)u0 * (h * 64);
+            const uint8_t *scales = p.w + p.w_scales + ((size_t)tile * p.units + u0) * SB;
+            const int a_h8 = (p.M + 7) / 8 * 8;
+            const uint8_t *a_codes = p.a + p.a_codes + (size_t)u0 * (a_h8 * 64), *a_scales = p.a + p.a_scales + (size_t)u0 * SB;
+            const uint32_t tx = (uint32_t)(h * 64 + SB) + (DIGITS ? 0u : (uint32_t)(a_h8 * 64 + SB));
+            auto load_w = [&](int i, int s) {
+                const uint32_t st = ring + (uint32_t)(s * p.stage_bytes), bar = full0 + 8 * s;
+                mbar_expect_tx(bar, tx);
+                bulk_load(st, codes + (size_t)i * (h * 64), (uint32_t)(h * 64), bar);
+                bulk_load(st + off_sfa, scales + (size_t)i * SB, SB, bar);
+            };
+            auto load_a = [&](int i, int s) {
+                const uint32_t st = ring + (uint32_t)(s * p.stage_bytes), bar = full0 + 8 * s;
+                bulk_load(st + off_b, a_codes + (size_t)i * (a_h8 * 64), (uint32_t)(a_h8 * 64), bar);
+                bulk_load(st + off_sfb, a_scales + (size_t)i * SB, SB, bar);
+            };
+            // weights of the first stages before the wait for the kernel ahead: nothing that may still be running writes them
+            const int first = min(nu, p.stages);
+            for (int i = 0; i < first; ++i) load_w(i, i);
+            if constexpr (!DIGITS) {
+                grid_wait();
+                for (int i = 0; i < first; ++i) load_a(i, i);
+            }
+            int s = 0;
+            uint32_t ph = 0;
+            for (int i = first; i < nu; ++i) {
+                if (!mbar_wait(empty0 + 8 * s, ph)) { ok = false; break; }
+                load_w(i, s);
+                if constexpr (!DIGITS) load_a(i, s);
+                if (++s == p.stages) { s = 0; ph ^= 1u; }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (elect_one()) {
+            const uint32_t id0 = f4_idesc(BLOCK, 128, p.cols, 0), id1 = f4_idesc(BLOCK, 128, p.cols, BLOCK == 32 ? 2 : 0);
+            const uint32_t sf0 = tmem + (uint32_t)p.cols;
+            const uint32_t lbo = DIGITS ? kDigitLbo : 128, sbo = DIGITS ? kDigitSbo : 512;
+            int s = 0;
+            uint32_t ph = 0;
+            for (int i = 0; i < nu; ++i) {
+                if (!mbar_wait(full0 + 8 * s, ph)) { ok = false; break; }
+                tcgen05_fence_after();
+                const uint32_t st = ring + (uint32_t)(s * p.stage_bytes), sfa = sf0 + (uint32_t)(i & 1) * 16u, sfb = sfa + 8u;
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+                    tcgen05_cp_scales(sfa + 4 * c, make_kmajor_desc(st + off_sfa + 512 * c, 128, 128));
+                    tcgen05_cp_scales(sfb + 4 * c, make_kmajor_desc(st + off_sfb + 512 * c, 128, 128));
+                }
+                tcgen05_mma_f4<BLOCK>(tmem, make_kmajor_desc(st, 128, 512), make_kmajor_desc(st + off_b, lbo, sbo), id0, sfa, sfb, i > 0);
+                tcgen05_mma_f4<BLOCK>(tmem, make_kmajor_desc(st + 256, 128, 512), make_kmajor_desc(st + off_b + 2 * lbo, lbo, sbo), id1,
+                                      sfa + (BLOCK == 32 ? 0 : 4), sfb + (BLOCK == 32 ? 0 : 4), 1);
+                tcgen05_commit(empty0 + 8 * s);
+                if (++s == p.stages) { s = 0; ph ^= 1u; }
+            }
+            tcgen05_commit(accf);
+        }
+        __syncwarp();
+    } else {
+        const int pt = threadIdx.x - 64;
+        if (BLOCK == 16 && pt < 128) w_row[pt] = tile * 128 + pt < p.N ? reinterpret_cast<const float *>(p.w + p.w_rows)[tile * 128 + pt] : 0.f;
+        grid_wait();
+        grid_launch_next();
+        if constexpr (!DIGITS) {
+            if (BLOCK == 16 && pt < p.M) a_row[pt] = ld_dependent(reinterpret_cast<const float *>(p.a + p.a_rows) + pt);
+        } else {
+            const T *x = static_cast<const T *>(p.x);
+            const int l16 = lane & 15;
+            if constexpr (BLOCK == 16) {
+                // the largest magnitude of each row of this share of k (of a row that holds an infinity or a NaN: whatever comes out)
+                const int k1 = min(p.K, (u0 + nu) * kF4Unit);
+                uint32_t mx[8] = {};
+                for (int k = u0 * kF4Unit + pt * 8; k < k1; k += 256 * 8) {
+                    uint4 v[8];
+#pragma unroll
+                    for (int m = 0; m < 8; ++m)
+                        if (m < p.M) v[m] = ld_dependent(reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx + k));
+#pragma unroll
+                    for (int m = 0; m < 8; ++m)
+                        if (m < p.M)
+                            mx[m] = __vmaxu2(mx[m], __vmaxu2(__vmaxu2(v[m].x & 0x7FFF7FFFu, v[m].y & 0x7FFF7FFFu), __vmaxu2(v[m].z & 0x7FFF7FFFu, v[m].w & 0x7FFF7FFFu)));
+                }
+#pragma unroll
+                for (int m = 0; m < 8; ++m)
+                    if (m < p.M) {
+                        const uint32_t top = __reduce_max_sync(0xffffffffu, max(mx[m] & 0xFFFFu, mx[m] >> 16));
+                        if (lane == 0) atomicMax(&row_top[m], top);
+                    }
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+            }
+            const int jobs = nu * pairs;
+            auto fetch = [&](int j) {
+                const int m = 2 * (j % pairs) + (lane >> 4), k = (u0 + j / pairs) * kF4Unit + l16 * 8;
+                return m < p.M && k < p.K ? ld_dependent(reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx + k)) : make_uint4(0u, 0u, 0u, 0u);
+            };
+            uint4 next = make_uint4(0u, 0u, 0u, 0u);
+            if (warp - 2 < jobs) next = fetch(warp - 2);
+            for (int j = warp - 2; j < jobs; j += 8) {
+                const uint4 cur = next;
+                if (j + 8 < jobs) next = fetch(j + 8);
+                const int i = j / pairs, m = 2 * (j % pairs) + (lane >> 4), s = i % p.stages;
+                const uint32_t w[4] = {cur.x, cur.y, cur.z, cur.w};
+                float f[8];
+                float top = 0.f;
+                bool fine = true;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 v = f4_to_float2<T>(w[e]);
+                    f[2 * e] = v.x;
+                    f[2 * e + 1] = v.y;
+                    fine = fine && fabsf(v.x) < __int_as_float(0x7F800000) && fabsf(v.y) < __int_as_float(0x7F800000);
+                    top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+                }
+                // largest magnitude of the block: exponents order like integers, and those of what is not finite above all others
+                uint32_t eb = fine ? __float_as_uint(top) >> 23 : 255u;
+#pragma unroll
+                for (int o = BLOCK / 16; o; o >>= 1) eb = max(eb, __shfl_xor_sync(0xffffffffu, eb, o));
+                uint32_t byte;                                   // the block's scale
+                int e2;                                          // E + 127
+                if constexpr (BLOCK == 32) {
+                    e2 = max((int)eb, std::is_same<T, __half>::value ? 103 : 1);
+                    byte = eb == 255u ? 255u : (uint32_t)e2;
+                } else {
+                    const uint32_t rt = row_top[m < p.M ? m : 0];
+                    const int r2 = max((int)(__float_as_uint(f4_to_float2<T>(rt).x) >> 23) - 8, 16);     // the row's power of two, + 127
+                    e2 = min(max((int)eb, r2 - 9), r2 + 8);
+                    const int d = e2 - r2;                       // -9 .. 8
+                    byte = eb == 255u ? 0x7Fu : d >= -6 ? (uint32_t)(d + 7) << 3 : 1u << (d + 9);
+                }
+                // X + bias in the low 23 bits of 2^23 + X + bias
+                constexpr float kMagic = 8388608.f + 4.f * 299593.f + 2.f * 2097152.f;      // 299593 = (8^7 - 1) / 7
+                uint32_t yb[8];
+                if constexpr (std::is_same<T, __half>::value) {
+                    const float mul = __uint_as_float((uint32_t)(127 + 20 + 127 - e2) << 23);           // 2^(20 - E), E >= -24
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) yb[e] = __float_as_uint(fmaf(f[e], mul, kMagic)) - 0x4B000000u;
+                } else {
+                    const int q = 147 - e2, qa = q >> 1;                                              // E down to -126: in two factors
+                    const float ma = __uint_as_float((uint32_t)(127 + qa) << 23), mb = __uint_as_float((uint32_t)(127 + q - qa) << 23);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) yb[e] = __float_as_uint(fmaf(f[e] * ma, mb, kMagic)) - 0x4B000000u;
+                }
+                uint32_t d[8];
+                digit_codes(yb, d);
+                uint32_t word = 0;                               // four blocks' scales
+                const int src = BLOCK == 32 ? (lane & 16) : (lane & 24);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) word |= __shfl_sync(0xffffffffu, byte, src + b * (BLOCK / 8)) << (8 * b);
+                if (i >= p.stages) {
+                    ok = warp_all(mbar_wait(empty0 + 8 * s, (uint32_t)(i / p.stages - 1) & 1u));
+                    if (!ok) break;
+                }
+                uint8_t *st = smem + (size_t)s * p.stage_bytes;
+                uint8_t *b = st + off_b + m * kDigitSbo + (l16 >> 2) * kDigitLbo + (l16 & 3) * 4;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) *reinterpret_cast<uint32_t *>(b + e * 16) = d[e];
+                if (BLOCK == 16 || l16 < 8) {
+                    const int t = 8 * m + (l16 & 7);
+                    *reinterpret_cast<uint32_t *>(st + off_sfb + (l16 >> 3) * 512 + (t & 31) * 16 + (t >> 5) * 4) = word;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full0 + 8 * s);
+            }
+        }
+    }
+
+    // ---- epilogue: warps 2..5, a channel a lane -------------------------------------------------
+    __syncthreads();                     // row scales and row_top are there; roles are done
+    const bool hdr_ok = f4_header_matches(p.w, p.N, p.K, BLOCK) && (DIGITS || f4_header_matches(p.a, p.M, p.K, BLOCK));
+    if (!hdr_ok && threadIdx.x == 64 && blockIdx.x == 0) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_BAD_PACKED);
+    T *y = static_cast<T *>(p.y);
+    float *part = reinterpret_cast<float *>(smem);               // [M][128], on the idle ring
+    if (warp >= 2 && warp < 6) {
+        ok = warp_all(mbar_wait(accf, 0)) && ok;
+        tcgen05_fence_after();
+        const int ch = (warp & 3) * 32 + lane, n = tile * 128 + ch;
+        const uint32_t acc = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const bool put = ok && hdr_ok && n < p.N;
+        const float wr = BLOCK == 16 ? w_row[ch] : 1.f;
+        auto give = [&](int m, float v) {
+            if (p.split > 1) part[m * 128 + ch] = v;
+            else if (put) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * wr * (DIGITS ? 1.f : a_row[m]) : v);
+        };
+        if constexpr (DIGITS) {
+#pragma unroll 1
+            for (int m = 0; m < p.M; ++m) {
+                uint32_t r[8];
+                tcgen05_ld_32x32b_x8(acc + 8 * m, r);
+                tcgen05_wait_ld();
+                float v = __uint_as_float(r[0]);
+#pragma unroll
+                for (int e = 1; e < 8; ++e) v = fmaf(v, 0.125f, __uint_as_float(r[e]));
+                if constexpr (BLOCK == 16) v *= __uint_as_float((uint32_t)max((int)(__float_as_uint(f4_to_float2<T>(row_top[m]).x) >> 23) - 8, 16) << 23);
+                give(m, v * 4.f);
+            }
+        } else {
+#pragma unroll 1
+            for (int m = 0; m < p.M; m += 8) {
+                uint32_t r[8];
+                tcgen05_ld_32x32b_x8(acc + m, r);
+                tcgen05_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (m + e < p.M) give(m + e, __uint_as_float(r[e]));
+            }
+        }
+    }
+    if (p.split > 1) {
+        cluster_sync_all();
+        const int all = p.M * 128, per = (all + p.split - 1) / p.split, i1 = min(all, per * (rank + 1));
+        for (int i = per * rank + (int)threadIdx.x; i < i1; i += kStreamThreads) {
+            const int m = i >> 7, ch = i & 127, n = tile * 128 + ch;
+            float v = 0.f;
+            for (int r = 0; r < p.split; ++r) {
+                float o;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o) : "r"(mapa_u32(ring + 4u * (uint32_t)i, (uint32_t)r)) : "memory");
+                v += o;
+            }
+            if (hdr_ok && n < p.N) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * w_row[ch] * (DIGITS ? 1.f : a_row[m]) : v);
+        }
+        __syncwarp();
+        cluster_sync_all();              // nobody leaves while others read its sums
+    }
+    if (!ok) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_TIMEOUT);
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tcgen05_fence_after();
+        tcgen05_dealloc(tmem, (uint32_t)tmem_cols);
+    }
+}
+
+// Shares of k: as few as give most SMs a CTA.
+inline int stream_split(int tiles, int units)
+{
+    int s = 1;
+    while (s < kStreamMaxSplit && tiles * (s + 1) <= 148 && units >= 2 * (s + 1)) ++s;
+    return s;
+}
+
+template <int BLOCK, typename T, bool DIGITS>
+tman_status launch_stream(F4StreamParams p, cudaStream_t s)
+{
+    auto kern = f4_stream_kernel<BLOCK, T, DIGITS>;
+    static std::atomic<bool> raised[kMaxDevices];
+    int dev = 0;
+    if (!device_info(&dev)) return TMAN_ERR_CUDA;
+    const int tiles = (p.N + kF4Tile - 1) / kF4Tile;
+    p.cols = DIGITS ? (p.M + 1) / 2 * 16 : (p.M + 15) / 16 * 16;
+    p.split = stream_split(tiles, p.units);
+    p.stage_bytes = (kF4Tile * 64 + 2 * f4_scale_bytes(BLOCK) + stream_b_bytes<BLOCK, DIGITS>(p.M, p.cols) + 127) / 128 * 128;
+    const int budget = 110 * 1024, least = p.M * 512;            // (the sums of a share lie on the ring)
+    p.stages = budget / p.stage_bytes;
+    if (p.stages > kStreamMaxStages) p.stages = kStreamMaxStages;
+    const int share = (p.units + p.split - 1) / p.split;
+    if (p.stages > share) p.stages = share;
+    int bytes = p.stages * p.stage_bytes;
+    if (bytes < least) bytes = least;
+    if ((long long)tiles * p.split > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * p.split));
+    cfg.blockDim = dim3(kStreamThreads);
+    cfg.dynamicSmemBytes = (size_t)bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.split;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = packed_write_pending(s, /*clear=*/true) ? 1 : 2;
+    return launch_with_smem(kern, 112 * 1024, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
+}
+
+}  // namespace
+}  // namespace tman

@@ -253,6 +253,67 @@ __device__ __forceinline__ uint64_t make_kmajor_sw128_desc(uint32_t smem_addr)
     return d;
 }
 
+// The same for a tile without swizzle, made of core matrices of 8 rows x 16 bytes (128 contiguous bytes): `lbo` bytes from one to the next
+// along k, `sbo` bytes to the next eight rows.
+__device__ __forceinline__ uint64_t make_kmajor_desc(uint32_t smem_addr, uint32_t lbo, uint32_t sbo)
+{
+    return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(sbo >> 4) << 32 | (uint64_t)1 << 46;
+}
+// 512 bytes (32 rows of 16) from shared memory into four columns of tensor memory, the same in each quarter of its lanes: the scales of 128
+// rows.  Ordered with the MMAs of the issuing thread.
+__device__ __forceinline__ void tcgen05_cp_scales(uint32_t taddr, uint64_t sdesc)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
+__device__ __forceinline__ void tcgen05_cp2_scales(uint32_t taddr, uint64_t sdesc)
+{
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
+// 64 values of k of e2m1 operands in shared memory with block scales in tensor memory: e8m0 per 32 values, or e4m3 per 16.
+template <int BLOCK>
+__device__ __forceinline__ void tcgen05_mma_f4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate)
+{
+    if constexpr (BLOCK == 32)
+        asm volatile(
+            "{\n.reg .pred p;\n"
+            "setp.ne.b32 p, %6, 0;\n"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+            ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    else
+        asm volatile(
+            "{\n.reg .pred p;\n"
+            "setp.ne.b32 p, %6, 0;\n"
+            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+            ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+template <int BLOCK>
+__device__ __forceinline__ void tcgen05_mma2_f4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate)
+{
+    if constexpr (BLOCK == 32)
+        asm volatile(
+            "{\n.reg .pred p;\n"
+            "setp.ne.b32 p, %6, 0;\n"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+            ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+    else
+        asm volatile(
+            "{\n.reg .pred p;\n"
+            "setp.ne.b32 p, %6, 0;\n"
+            "tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+            ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+// Instruction descriptor of the above for `rows` x `cols`: A and B e2m1, K-major; scales e8m0 (block 32) or e4m3.  `id`: which byte of a
+// row's four scales is the first of the 64 values (0 or 2; block 16 takes all four).
+__host__ __device__ constexpr uint32_t f4_idesc(int block, int rows, int cols, int id)
+{
+    return (uint32_t)id << 4 | 1u << 7 | 1u << 10 | (uint32_t)(cols >> 3) << 17 | (block == 32 ? 1u << 23 : 0u) | (uint32_t)(rows >> 4) << 24 | (uint32_t)id << 29;
+}
+
+// Programmatic dependent launch: behind grid_wait() everything that the kernels before this one in the stream wrote is there; after
+// grid_launch_next() of every CTA the next kernel may start.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // A constant the compiler keeps in a register instead of folding it into instructions (which take one immediate each).
 template <uint32_t V> __device__ __forceinline__ uint32_t opaque_u32()
 {
