@@ -89,14 +89,16 @@ def pack(codes, scales, row_scale, block):
     out[:8] = np.frombuffer(b"TMANF4MX", dtype=np.uint8)
     out[8:24] = np.array([1, rows, K, block], dtype="<u4").view(np.uint8)
     out[24:56] = np.array([o_codes, o_scales, o_rows, total], dtype="<u8").view(np.uint8)
-    units, h8 = -(-K // 128), -(-rows // 8) * 8
+    halves, h8, tiles, sb = -(-K // 128), -(-rows // 8) * 8, -(-rows // 128), 512 if block == 32 else 1024
     r, k = np.meshgrid(np.arange(rows), np.arange(0, K, 2), indexing="ij")
-    h = np.minimum(128, h8 - r // 128 * 128)
-    at = r // 128 * units * 8192 + k // 128 * (h * 64) + r % 128 // 8 * 512 + k % 128 // 32 * 128 + r % 8 * 16 + k % 32 // 2
+    u = k // 256
+    full = 2 * u + 1 < halves                      # units of 256 columns, the last perhaps of 128
+    at = u * h8 * 128 + r // 8 * np.where(full, 1024, 512) + k % 256 // 32 * 128 + r % 8 * 16 + k % 32 // 2
     out[o_codes + at] = codes[:, 0::2] | (codes[:, 1::2] << 4)
     r, b = np.meshgrid(np.arange(rows), np.arange(K // block), indexing="ij")
     per = 128 // block
-    at = (r // 128 * units + b // per) * (512 if block == 32 else 1024) + b % per // 4 * 512 + r % 32 * 16 + r % 128 // 32 * 4 + b % 4
+    u, half = b // per // 2, b // per % 2
+    at = (u * tiles * 2 + r // 128 * np.where(2 * u + 1 < halves, 2, 1) + half) * sb + b % per // 4 * 512 + r % 32 * 16 + r % 128 // 32 * 4 + b % 4
     out[o_scales + at] = scales
     if block == 16:
         out[o_rows:o_rows + 4 * rows] = np.asarray(row_scale, dtype="<f4").view(np.uint8)

@@ -282,14 +282,14 @@ static tman_status check_f4_workspace(const void *workspace, size_t ws_bytes, si
 static tman_status check_f4_rows(const void *x, int ldx, int dtype, int K)
 {
     if (!x) return TMAN_ERR_NULL;
-    if (dtype != kF4Half && dtype != kF4Bf16) return TMAN_ERR_UNSUPPORTED;
+    if (dtype != kF4TypeHalf && dtype != kF4TypeBf16) return TMAN_ERR_UNSUPPORTED;
     if (ldx < K || ldx % 8 != 0 || !aligned_to(x, 16)) return TMAN_ERR_SHAPE;
     return TMAN_OK;
 }
 static tman_status check_f4_output(const void *y, int ldy, int dtype, int N)
 {
     if (!y) return TMAN_ERR_NULL;
-    if (dtype != kF4Half && dtype != kF4Bf16) return TMAN_ERR_UNSUPPORTED;
+    if (dtype != kF4TypeHalf && dtype != kF4TypeBf16) return TMAN_ERR_UNSUPPORTED;
     return ldy < N || !aligned_to(y, 2) ? TMAN_ERR_SHAPE : TMAN_OK;
 }
 #define TMAN_F4_CHECK(call)                        \

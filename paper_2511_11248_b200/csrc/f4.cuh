@@ -5,14 +5,15 @@
 //   block 16: block scale e4m3, row scale fp32
 // Packed buffer (little endian), sections padded to 256 bytes:
 //   header  256 bytes: "TMANF4MX", u32 version = 1, rows, K, block, u64 codes_off, scales_off, rows_off, total_bytes
-//   codes   tiles of 128 rows x units of 128 columns, [tile][unit]; a tile's height h is 128, of the last tile the rest of the rows rounded
-//           up to 8.  In a unit of h x 64 bytes: byte (r/8)*512 + (k/32)*128 + (r%8)*16 + (k%32)/2, the even k in the low half.
-//           Eight rows' pieces of 16 bytes are one 128-byte core matrix of the tensor cores' K-major operands without swizzle, so that
-//           a unit, or the first rows of one, reaches shared memory by one linear bulk copy and needs no tensor map.
-//   scales  [tile][unit][128 / (4 block)][512 bytes]: byte (r%32)*16 + (r/32%4)*4 + c is the scale of block c of four: the order in
-//           which tensor memory holds the scales of 128 rows (32 lanes, one column of four bytes per 32 rows).
+//   codes   units of 256 columns (the last one 128 where that holds the rest), in each all rows, rounded up to a multiple of 8, in groups of 8.
+//           A group is 8 (or 4) core matrices of the tensor cores' K-major operands without swizzle, 8 rows x 32 columns in 128 bytes: byte
+//           (k%256/32)*128 + (r%8)*16 + (k%32)/2, the even k in the low half.
+//   scales  the same units, in each tiles of 128 rows, in each 2 (1) x 128 / (4 block) pieces of 512 bytes: byte (r%32)*16 + (r/32%4)*4 + c is
+//           the scale of block c of four: the order in which tensor memory holds the scales of 128 rows (32 lanes, a column of four bytes
+//           per 32 rows).
 //   rows    fp32, 128 a tile (block 16 only)
-// K is filled up to whole units with codes and scales of zero.
+// So any rows' codes of a unit, and the scales of adjacent tiles, reach shared memory as operands by one linear bulk copy, without a tensor
+// map.  K is filled up to a multiple of 128 with codes and scales of zero.
 #pragma once
 
 #include "common.cuh"
@@ -27,37 +28,36 @@ struct F4Header {
     uint64_t codes_off, scales_off, rows_off, total_bytes;
 };
 constexpr uint32_t kF4Version = 1;
-constexpr int kF4Unit = 128;            // columns of a unit
-constexpr int kF4Tile = 128;            // rows of a tile
+constexpr int kF4Half = 128;            // columns of half a unit
+constexpr int kF4Tile = 128;            // rows of a tile of scales
 
 struct F4Layout {
-    int tiles, units, height8;          // height8: all rows, rounded up to 8
+    int tiles, halves, height8;         // height8: all rows, rounded up to 8
     size_t codes_off, scales_off, rows_off, total;
 };
-__host__ __device__ inline int f4_scale_bytes(int block) { return block == 32 ? 512 : 1024; }      // of a unit of a tile
+__host__ __device__ constexpr int f4_scale_bytes(int block) { return block == 32 ? 512 : 1024; }      // of half a unit of a tile
 __host__ __device__ inline F4Layout f4_layout(int rows, int K, int block)
 {
     F4Layout L;
     L.tiles = (rows + kF4Tile - 1) / kF4Tile;
-    L.units = (K + kF4Unit - 1) / kF4Unit;
+    L.halves = (K + kF4Half - 1) / kF4Half;
     L.height8 = (rows + 7) / 8 * 8;
     L.codes_off = kHeaderBytes;
-    L.scales_off = L.codes_off + up256((size_t)L.units * 64 * L.height8);
-    L.rows_off = L.scales_off + (size_t)L.tiles * L.units * f4_scale_bytes(block);
+    L.scales_off = L.codes_off + up256((size_t)L.halves * 64 * L.height8);
+    L.rows_off = L.scales_off + (size_t)L.tiles * L.halves * f4_scale_bytes(block);
     L.total = L.rows_off + (block == 16 ? (size_t)L.tiles * kF4Tile * 4 : 0);
     return L;
 }
 // Byte of a code pair / of a scale, from the start of its section.
-__host__ __device__ inline size_t f4_code_at(int r, int k, int height8, int units)
+__host__ __device__ inline size_t f4_code_at(int r, int k, const F4Layout &L)
 {
-    const int t = r / kF4Tile, h = min(kF4Tile, height8 - t * kF4Tile);
-    return (size_t)t * units * (kF4Tile * 64) + (size_t)(k / kF4Unit) * (h * 64) + (r % kF4Tile / 8) * 512 + (k % kF4Unit / 32) * 128 +
-           (r % 8) * 16 + (k % 32) / 2;
+    const int u = k / (2 * kF4Half), wide = 2 * u + 1 < L.halves ? 1024 : 512;
+    return (size_t)u * L.height8 * 128 + (size_t)(r / 8) * wide + (k % (2 * kF4Half) / 32) * 128 + (r % 8) * 16 + (k % 32) / 2;
 }
-__host__ __device__ inline size_t f4_scale_at(int r, int b, int block, int units)      // b: block along K
+__host__ __device__ inline size_t f4_scale_at(int r, int b, int block, const F4Layout &L)      // b: block along K
 {
-    const int t = r / kF4Tile, per = kF4Unit / block;
-    return ((size_t)t * units + b / per) * f4_scale_bytes(block) + (b % per / 4) * 512 + (r % 32) * 16 + (r % kF4Tile / 32) * 4 + b % 4;
+    const int per = kF4Half / block, half = b / per, u = half / 2, sb = f4_scale_bytes(block), wide = 2 * u + 1 < L.halves ? 2 : 1;
+    return ((size_t)u * L.tiles * 2 + (size_t)(r / kF4Tile) * wide + half % 2) * sb + (b % per / 4) * 512 + (r % 32) * 16 + (r % kF4Tile / 32) * 4 + b % 4;
 }
 
 inline tman_status f4_check(int rows, int K, int block)
@@ -148,7 +148,7 @@ template <> __device__ __forceinline__ __half f4_from_float<__half>(float a) { r
 template <> __device__ __forceinline__ __nv_bfloat16 f4_from_float<__nv_bfloat16>(float a) { return __float2bfloat16_rn(a); }
 #endif
 
-enum { kF4Half = 0, kF4Bf16 = 1 };
+enum { kF4TypeHalf = 0, kF4TypeBf16 = 1 };
 
 // entry points implemented per file
 tman_status launch_f4_pack(const uint8_t *codes, const uint8_t *scales, const float *row_scale, int rows, int K, int block, void *packed, cudaStream_t s);

@@ -18,7 +18,7 @@ static F4StreamParams stream_params(const void *packed, const void *a, const voi
     p.w_codes = L.codes_off; p.w_scales = L.scales_off; p.w_rows = L.rows_off;
     p.a_codes = A.codes_off; p.a_scales = A.scales_off; p.a_rows = A.rows_off;
     p.M = M; p.K = K; p.N = N; p.ldx = ldx; p.ldy = ldy;
-    p.units = L.units;
+    p.halves = L.halves;
     p.height8 = L.height8;
     return p;
 }
@@ -35,7 +35,7 @@ static tman_status gemm_as(const void *packed, const void *a, void *y, int ldy, 
     p.w_codes = L.codes_off; p.w_scales = L.scales_off; p.w_rows = L.rows_off;
     p.a_codes = A.codes_off; p.a_scales = A.scales_off; p.a_rows = A.rows_off;
     p.M = M; p.K = K; p.N = N; p.ldy = ldy;
-    p.units = L.units;
+    p.halves = L.halves;
     p.w_h8 = L.height8; p.a_h8 = A.height8;
     return launch_pair<BLOCK, T>(p, s);
 }
@@ -43,12 +43,12 @@ static tman_status gemm_as(const void *packed, const void *a, void *y, int ldy, 
 tman_status launch_f4_gemv(const void *packed, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N, int block, void *ws, cudaStream_t s)
 {
     const F4StreamParams p = stream_params(packed, nullptr, x, ldx, y, ldy, M, K, N, block, ws);
-    if (dtype == kF4Half) return block == 32 ? launch_stream<32, __half, true>(p, s) : launch_stream<16, __half, true>(p, s);
+    if (dtype == kF4TypeHalf) return block == 32 ? launch_stream<32, __half, true>(p, s) : launch_stream<16, __half, true>(p, s);
     return block == 32 ? launch_stream<32, __nv_bfloat16, true>(p, s) : launch_stream<16, __nv_bfloat16, true>(p, s);
 }
 tman_status launch_f4_gemm(const void *packed, const void *a, void *y, int ldy, int dtype, int M, int K, int N, int block, void *ws, cudaStream_t s)
 {
-    if (dtype == kF4Half) return block == 32 ? gemm_as<32, __half>(packed, a, y, ldy, M, K, N, ws, s) : gemm_as<16, __half>(packed, a, y, ldy, M, K, N, ws, s);
+    if (dtype == kF4TypeHalf) return block == 32 ? gemm_as<32, __half>(packed, a, y, ldy, M, K, N, ws, s) : gemm_as<16, __half>(packed, a, y, ldy, M, K, N, ws, s);
     return block == 32 ? gemm_as<32, __nv_bfloat16>(packed, a, y, ldy, M, K, N, ws, s) : gemm_as<16, __nv_bfloat16>(packed, a, y, ldy, M, K, N, ws, s);
 }
 

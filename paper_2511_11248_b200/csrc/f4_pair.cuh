@@ -1,10 +1,12 @@
 // Products of many rows, both operands in 4 bits: y[m][n] = a_row[m] w_row[n] sum_k a[m][k] w[n][k], bound by the tensor cores.
 //
-// A pair of CTAs (cta_group::2) has a tile of 256 channels (the rows of the tensor-core tile, 128 a CTA) x up to 192 rows of a (its columns).
-// The packed layout is the operands' layout: stages of 256 values of k reach shared memory by linear bulk copies, each CTA its own
-// channels and half of the rows of a, and the scales of all of them; the scales go on to tensor memory by tcgen05.cp in front of the
-// MMAs that use them, both issued by one thread of the pair.  Two accumulators of 192 columns and two sets of scales (2 x 32 columns) share
-// tensor memory, so that a tile's epilogue runs behind the next tile's MMAs.
+// A pair of CTAs (cta_group::2) has a tile of 256 channels (the rows of the tensor-core tile, 128 a CTA) x up to 256 rows of a (its columns).
+// The packed layout is the operands' layout: units of 256 values of k reach shared memory by four linear bulk copies a CTA, its own
+// channels, half of the rows of a, and the scales of the channels and of all the rows.  The scales go on to tensor memory by tcgen05.cp in front
+// of the MMAs that use them, both issued by one thread of the pair.
+// Tensor memory: two accumulators from columns 0 and 192 on, scales from 448.  Up to 192 rows of a, a tile's epilogue runs behind the next
+// tile's MMAs; with 256 the accumulators share 64 columns, which the epilogue takes first: the next tile starts when it has them in
+// registers.
 // A tile's rows of a start at a multiple of 64: in tensor memory 32 rows' scales are a column, and the scales of an operand start at an even
 // column (an odd one is a misaligned address), so that a tile's scales are the first or the second half of the first 512-byte piece and on.
 #pragma once
@@ -16,36 +18,38 @@ namespace tman {
 namespace {
 
 constexpr int kPairThreads = 320;        // warp 0: loads, warp 1: MMAs (of the pair's first CTA), warps 2..9: epilogue
-constexpr int kPairCols = 192;           // most rows of a in a tile
-constexpr int kPairStages = 7;
-constexpr int kPairSmem = 220 * 1024;
+constexpr int kPairCols = 256;           // most rows of a in a tile
+constexpr int kPairAcc1 = 192, kPairSf = 448;
+constexpr int kPairStages = 6;
+constexpr int kPairSmem = 222 * 1024;
 
 struct F4PairParams {
     const uint8_t *w, *a;
     void *y;
     uint32_t *status;
     size_t w_codes, w_scales, w_rows, a_codes, a_scales, a_rows;
-    int M, K, N, ldy, units, w_h8, a_h8, nt, tiles_m, tiles_n, stages;
+    int M, K, N, ldy, halves, w_h8, a_h8, nt, tiles_m, tiles_n, stages;
 };
 
 template <int BLOCK> struct PairStage {
-    static constexpr int SB = BLOCK == 32 ? 512 : 1024, CHUNKS = SB / 512;
-    static constexpr uint32_t kB = 2 * 8192, kSfa = kB + 2 * (kPairCols / 2 * 64), kSfb = kSfa + 2 * SB, kBytes = kSfb + 2 * 2 * SB;
-    // (stage: [unit] channels' codes, [unit] codes of a, [unit] channels' scales, [piece][unit] scales of a)
+    static constexpr uint32_t SB = f4_scale_bytes(BLOCK), CHUNKS = SB / 512;
+    static constexpr uint32_t kB = kF4Tile * 128, kSfa = kB + kPairCols / 2 * 128, kSfb = kSfa + 2 * SB, kBytes = kSfb + 2 * 2 * SB;
 };
 
 template <int BLOCK, typename T>
 __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pair_kernel(const __grid_constant__ F4PairParams p)
 {
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t full_bar[kPairStages], empty_bar[kPairStages], accf_bar[2], acce_bar[2];
+    __shared__ __align__(8) uint64_t full_bar[kPairStages], empty_bar[kPairStages], accf_bar[2], acce_bar[2], shared_bar;
     __shared__ uint32_t tmem_slot;
     using St = PairStage<BLOCK>;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (the shuffle tells the compiler that it is uniform)
     const uint32_t rank = cluster_ctarank();
     const int worker = blockIdx.x >> 1, workers = gridDim.x >> 1, tiles = p.tiles_m * p.tiles_n;
-    const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), accf0 = smem_u32(accf_bar), acce0 = smem_u32(acce_bar), ring = smem_u32(smem);
-    const int steps = (p.units + 1) >> 1;
+    const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), accf0 = smem_u32(accf_bar), acce0 = smem_u32(acce_bar),
+                   shared0 = smem_u32(&shared_bar), ring = smem_u32(smem);
+    const int steps = (p.halves + 1) >> 1;
+    const bool overlap = p.nt > kPairAcc1;                       // the two accumulators share columns
     bool ok = true;
 
     if (threadIdx.x == 0) {
@@ -57,52 +61,69 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
             mbar_init(accf0 + 8 * b, 1);
             mbar_init(acce0 + 8 * b, 16);
         }
+        mbar_init(shared0, 8);
         fence_barrier_init();
     }
     __syncthreads();
     cluster_sync_all();
 
-    // ---- loads of a stage --------------------------------------------------------------------------
-    auto load_w = [&](int tile, int step, int s) {
-        const int rt = (tile % p.tiles_n) * 2 + (int)rank, h = min(kF4Tile, p.w_h8 - rt * kF4Tile), nu = min(2, p.units - 2 * step);
-        if (h <= 0) return;                                      // (channels behind the last)
-        const uint32_t st = ring + s * St::kBytes, bar = full0 + 8 * s;
-        const uint8_t *codes = p.w + p.w_codes + (size_t)rt * p.units * (kF4Tile * 64) + (size_t)(2 * step) * (h * 64);
-        if (h == kF4Tile) bulk_load(st, codes, (uint32_t)nu * 8192u, bar);
-        else for (int u = 0; u < nu; ++u) bulk_load(st + u * 8192, codes + u * (h * 64), (uint32_t)(h * 64), bar);
-        bulk_load(st + St::kSfa, p.w + p.w_scales + ((size_t)rt * p.units + 2 * step) * St::SB, (uint32_t)(nu * St::SB), bar);
-    };
-    auto load_a = [&](int tile, int step, int s) {
-        const int m0 = tile / p.tiles_n * p.nt, r0 = m0 + (int)rank * (p.nt >> 1), r1 = min(r0 + (p.nt >> 1), p.a_h8), nu = min(2, p.units - 2 * step);
-        const uint32_t st = ring + s * St::kBytes, bar = full0 + 8 * s;
-        for (int r = r0; r < r1;) {                              // rows of one or two tiles of the packed matrix
-            const int rt = r / kF4Tile, h = min(kF4Tile, p.a_h8 - rt * kF4Tile), n = min(r1, (rt + 1) * kF4Tile) - r;
-            const uint8_t *codes = p.a + p.a_codes + (size_t)rt * p.units * (kF4Tile * 64) + (size_t)(2 * step) * (h * 64) + (size_t)(r % kF4Tile) * 64;
-            for (int u = 0; u < nu; ++u)
-                bulk_load(st + St::kB + (uint32_t)(u * (kPairCols / 2) + r - r0) * 64u, codes + u * (h * 64), (uint32_t)(n * 64), bar);
-            r += n;
-        }
-        const int t1 = (min(m0 + p.nt, p.a_h8) + kF4Tile - 1) / kF4Tile;
-        for (int rt = m0 / kF4Tile, j = 0; rt < t1; ++rt, ++j)
-            bulk_load(st + St::kSfb + j * 2 * St::SB, p.a + p.a_scales + ((size_t)rt * p.units + 2 * step) * St::SB, (uint32_t)(nu * St::SB), bar);
-    };
-    auto bytes_of = [&](int tile, int step) {
-        const int h = min(kF4Tile, p.w_h8 - ((tile % p.tiles_n) * 2 + (int)rank) * kF4Tile), nu = min(2, p.units - 2 * step);
-        const int m0 = tile / p.tiles_n * p.nt, r0 = m0 + (int)rank * (p.nt >> 1), rows = max(min(r0 + (p.nt >> 1), p.a_h8) - r0, 0);
-        const int pieces = (min(m0 + p.nt, p.a_h8) + kF4Tile - 1) / kF4Tile - m0 / kF4Tile;
-        return (uint32_t)(nu * ((h > 0 ? h * 64 + St::SB : 0) + rows * 64 + pieces * St::SB));
-    };
     const int total = worker < tiles ? ((tiles - 1 - worker) / workers + 1) * steps : 0;       // stages of this pair
+    // (Warps 0 and 1 walk as one and work out addresses and descriptors outside of what one lane issues, so that they sit in uniform
+    // registers: 0.4 us a unit otherwise.)
+    // What a tile loads: bytes of a unit (of half a unit: half of them) and where its first unit is; units are a constant distance apart.
+    struct Loads {
+        const uint8_t *w, *ws, *a, *as;
+        uint32_t w_bytes, a_bytes, as_bytes;
+    };
+    auto loads_of = [&](int tile) {
+        Loads l;
+        const int tm = tile / p.tiles_n, rt = (tile - tm * p.tiles_n) * 2 + (int)rank, h = max(min(kF4Tile, p.w_h8 - rt * kF4Tile), 0);
+        const int m0 = tm * p.nt, r0 = m0 + (int)rank * (p.nt >> 1), rows = max(min(p.nt >> 1, p.a_h8 - r0), 0), at = m0 / kF4Tile;
+        l.w_bytes = (uint32_t)h * 128u;                          // (0: channels behind the last)
+        l.a_bytes = (uint32_t)rows * 128u;
+        l.as_bytes = (uint32_t)((min(m0 + p.nt, p.a_h8) + kF4Tile - 1) / kF4Tile - at) * (2u * St::SB);
+        l.w = p.w + p.w_codes + (size_t)rt * (kF4Tile * 128);
+        l.ws = p.w + p.w_scales + (size_t)rt * (2 * St::SB);
+        l.a = p.a + p.a_codes + (size_t)r0 * 128;
+        l.as = p.a + p.a_scales + (size_t)at * (2 * St::SB);
+        return l;
+    };
+    const size_t w_step = (size_t)p.w_h8 * 128, a_step = (size_t)p.a_h8 * 128, ws_step = (size_t)((p.w_h8 + kF4Tile - 1) / kF4Tile) * (2 * St::SB),
+                 as_step = (size_t)((p.a_h8 + kF4Tile - 1) / kF4Tile) * (2 * St::SB);
+    // A half unit's sections are half as wide: rows (tiles) lie half as far from the section's start.
+    auto load = [&](bool lead, const Loads &l, int step, int s, bool do_w, bool do_a) {
+        const uint32_t sh = 2 * step + 1 < p.halves ? 0u : 1u;
+        const uint32_t st = ring + (uint32_t)s * St::kBytes, bar = full0 + 8 * s;
+        const uint8_t *w = p.w + p.w_codes + step * w_step + ((size_t)(l.w - (p.w + p.w_codes)) >> sh);
+        const uint8_t *ws = p.w + p.w_scales + step * ws_step + ((size_t)(l.ws - (p.w + p.w_scales)) >> sh);
+        const uint8_t *a = p.a + p.a_codes + step * a_step + ((size_t)(l.a - (p.a + p.a_codes)) >> sh);
+        const uint8_t *as = p.a + p.a_scales + step * as_step + ((size_t)(l.as - (p.a + p.a_scales)) >> sh);
+        const uint32_t wb = l.w_bytes >> sh, ab = l.a_bytes >> sh, asb = l.as_bytes >> sh, wsb = wb ? 2u * St::SB >> sh : 0u;
+        if (lead) {
+            if (do_w) {
+                mbar_expect_tx(bar, wb + wsb + ab + asb);
+                if (wb) {
+                    bulk_load(st, w, wb, bar);
+                    bulk_load(st + St::kSfa, ws, wsb, bar);
+                }
+            }
+            if (do_a) {
+                if (ab) bulk_load(st + St::kB, a, ab, bar);
+                bulk_load(st + St::kSfb, as, asb, bar);
+            }
+        }
+        __syncwarp();
+    };
     int first = 0;
-    if (warp == 0 && elect_one()) {
+    if (warp == 0) {
         // weights of the first stages before the wait for the kernel ahead: nothing that may still be running writes them
+        const bool lead = elect_one();
         first = min(p.stages, min(total, steps));
-        for (int i = 0; i < first; ++i) {
-            mbar_expect_tx(full0 + 8 * i, bytes_of(worker, i));
-            load_w(worker, i, i);
+        if (first > 0) {
+            const Loads l = loads_of(worker);
+            for (int i = 0; i < first; ++i) load(lead, l, i, i, true, false);
         }
     }
-    __syncwarp();
     grid_wait();
     if (warp == 1) {
         tcgen05_alloc2(smem_u32(&tmem_slot), 512);
@@ -113,124 +134,143 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
     cluster_sync_all();                  // both CTAs hold their tensor memory
     tcgen05_fence_after();
     grid_launch_next();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
 
     if (warp == 0) {
-        if (elect_one()) {
-            int s = 0, i = 0;
-            uint32_t ph = 1;                                     // (the first pass over the ring does not wait)
-            for (int tile = worker; ok && tile < tiles; tile += workers)
-                for (int step = 0; step < steps; ++step, ++i) {
-                    if (i >= first) {
-                        if (!mbar_wait(empty0 + 8 * s, ph)) { ok = false; break; }
-                        mbar_expect_tx(full0 + 8 * s, bytes_of(tile, step));
-                        load_w(tile, step, s);
-                    }
-                    load_a(tile, step, s);
-                    if (++s == p.stages) { s = 0; ph ^= 1u; }
-                }
-        }
-        __syncwarp();
-    } else if (warp == 1) {
-        if (elect_one()) {
-            int s = 0;
-            uint32_t ph = 0;
-            if (rank != 0) {                                     // tells the first CTA when this one's part of a stage is there
-                const uint32_t lead = mapa_u32(full0, 0);
-                for (int i = 0; i < total; ++i) {
-                    if (!mbar_wait(full0 + 8 * s, ph)) { ok = false; break; }
-                    mbar_arrive_cluster(lead + 8 * s);
-                    if (++s == p.stages) { s = 0; ph ^= 1u; }
-                }
-            } else {
-                const uint32_t id0 = f4_idesc(BLOCK, 256, p.nt, 0), id1 = f4_idesc(BLOCK, 256, p.nt, BLOCK == 32 ? 2 : 0);
-                uint32_t ti = 0, set = 0;
-                for (int tile = worker; ok && tile < tiles; tile += workers, ++ti) {
-                    const uint32_t b = ti & 1u, acc = tmem + b * kPairCols;
-                    if (!mbar_wait(acce0 + 8 * b, ((ti >> 1) & 1u) ^ 1u)) { ok = false; break; }
-                    tcgen05_fence_after();
-                    const int m0 = tile / p.tiles_n * p.nt, g0 = m0 / 32 % 4, pieces = (g0 + p.nt / 32 + 3) / 4;
-                    for (int u = 0; u < p.units; ++u) {
-                        const uint32_t st = ring + s * St::kBytes, half = (uint32_t)(u & 1);
-                        if (half == 0) {
-                            if (!mbar_wait(full0 + 8 * s, ph)) { ok = false; break; }
-                            tcgen05_fence_after();
-                        }
-                        const uint32_t sfa = tmem + 2 * kPairCols + set * 32u, sfb = sfa + 4 * St::CHUNKS;
-                        set ^= 1u;
-#pragma unroll
-                        for (int c = 0; c < St::CHUNKS; ++c) {
-                            tcgen05_cp2_scales(sfa + 4 * c, make_kmajor_desc(st + St::kSfa + half * St::SB + 512 * c, 128, 128));
-#pragma unroll
-                            for (int j = 0; j < 2; ++j)
-                                if (j < pieces)
-                                    tcgen05_cp2_scales(sfb + 8 * c + 4 * j, make_kmajor_desc(st + St::kSfb + (2 * j + half) * St::SB + 512 * c, 128, 128));
-                        }
-                        const uint32_t wa = st + half * 8192u, xb = st + St::kB + half * (kPairCols / 2 * 64);
-                        tcgen05_mma2_f4<BLOCK>(acc, make_kmajor_desc(wa, 128, 512), make_kmajor_desc(xb, 128, 512), id0, sfa, sfb + g0, u > 0);
-                        tcgen05_mma2_f4<BLOCK>(acc, make_kmajor_desc(wa + 256, 128, 512), make_kmajor_desc(xb + 256, 128, 512), id1,
-                                               sfa + (BLOCK == 32 ? 0 : 4), sfb + g0 + (BLOCK == 32 ? 0 : 8), 1);
-                        if (half == 1 || u == p.units - 1) {
-                            tcgen05_commit2_both(empty0 + 8 * s);
-                            if (++s == p.stages) { s = 0; ph ^= 1u; }
-                        }
-                    }
-                    tcgen05_commit2_both(accf0 + 8 * b);
-                }
+        const bool lead = elect_one();
+        int s = 0, i = 0;
+        uint32_t ph = 1;                                         // (the first pass over the ring does not wait)
+        for (int tile = worker; ok && tile < tiles; tile += workers) {
+            const Loads l = loads_of(tile);
+            for (int step = 0; step < steps; ++step, ++i) {
+                if (i >= first && !warp_all(mbar_wait(empty0 + 8 * s, ph))) { ok = false; break; }
+                load(lead, l, step, s, i >= first, true);
+                if (++s == p.stages) { s = 0; ph ^= 1u; }
             }
         }
-        __syncwarp();
+    } else if (warp == 1 && rank != 0) {                         // tells the first CTA when this one's part of a stage is there
+        const bool lead = elect_one();
+        const uint32_t to = mapa_u32(full0, 0);
+        int s = 0;
+        uint32_t ph = 0;
+        for (int i = 0; i < total; ++i) {
+            if (!warp_all(mbar_wait(full0 + 8 * s, ph))) { ok = false; break; }
+            if (lead) mbar_arrive_cluster(to + 8 * s);
+            __syncwarp();
+            if (++s == p.stages) { s = 0; ph ^= 1u; }
+        }
+    } else if (warp == 1) {
+        const bool lead = elect_one();
+        const uint32_t id0 = f4_idesc(BLOCK, 256, p.nt, 0), id1 = f4_idesc(BLOCK, 256, p.nt, BLOCK == 32 ? 2 : 0);
+        const uint64_t sf0 = make_kmajor_desc(ring, 128, 128);                     // (+ 1: 16 bytes)
+        int s = 0;
+        uint32_t ph = 0, ti = 0;
+        for (int tile = worker; ok && tile < tiles; tile += workers, ++ti) {
+            const uint32_t b = ti & 1u, acc = tmem + b * kPairAcc1;
+            if (!warp_all(mbar_wait(acce0 + 8 * b, ((ti >> 1) & 1u) ^ 1u))) { ok = false; break; }
+            if (overlap && ti > 0 && !warp_all(mbar_wait(shared0, (ti - 1) & 1u))) { ok = false; break; }
+            const uint32_t g0 = (uint32_t)(tile / p.tiles_n * p.nt) / 32 % 4;
+            const bool two = g0 + (uint32_t)p.nt / 32 > 4;           // pieces of scales of a
+            for (int step = 0; step < steps; ++step) {
+                const uint32_t at = (uint32_t)s * (St::kBytes >> 4), nu = 2 * step + 1 < p.halves ? 2u : 1u;
+                const uint64_t op = make_kmajor_desc(ring, 128, nu * 512) + at, sf = sf0 + at;
+                if (!warp_all(mbar_wait(full0 + 8 * s, ph))) { ok = false; break; }
+                tcgen05_fence_after();
+                if (lead) {
+#pragma unroll
+                    for (uint32_t u = 0; u < 2; ++u)
+                        if (u < nu) {
+                            const uint32_t sfa = tmem + kPairSf + u * 32u, sfb = sfa + 4 * St::CHUNKS;
+#pragma unroll
+                            for (uint32_t c = 0; c < St::CHUNKS; ++c) {
+                                tcgen05_cp2_scales(sfa + 4 * c, sf + ((St::kSfa + u * St::SB + 512 * c) >> 4));
+                                tcgen05_cp2_scales(sfb + 8 * c, sf + ((St::kSfb + u * St::SB + 512 * c) >> 4));
+                                if (two) tcgen05_cp2_scales(sfb + 8 * c + 4, sf + ((St::kSfb + (nu + u) * St::SB + 512 * c) >> 4));
+                            }
+                            const uint64_t wa = op + ((u * 512) >> 4), xb = op + ((St::kB + u * 512) >> 4);
+                            tcgen05_mma2_f4<BLOCK>(acc, wa, xb, id0, sfa, sfb + g0, (step | (int)u) != 0);
+                            tcgen05_mma2_f4<BLOCK>(acc, wa + 16, xb + 16, id1, sfa + (BLOCK == 32 ? 0 : 4), sfb + g0 + (BLOCK == 32 ? 0 : 8), 1);
+                        }
+                    tcgen05_commit2_both(empty0 + 8 * s);
+                }
+                __syncwarp();
+                if (++s == p.stages) { s = 0; ph ^= 1u; }
+            }
+            if (lead) tcgen05_commit2_both(accf0 + 8 * b);
+            __syncwarp();
+        }
     } else {
-        // ---- epilogue: a warp has 32 channels (a lane each) x half of the tile's rows of a; neighbouring lanes exchange every other row, so
-        // that a lane stores two adjacent channels of one row
+        // ---- epilogue: a warp has 32 channels (a lane each) x half of the tile's rows of a, 32 at a time; neighbouring lanes exchange every
+        // other row, so that a lane stores two adjacent channels of one row
         const bool hdr_ok = f4_header_matches(p.w, p.N, p.K, BLOCK) && f4_header_matches(p.a, p.M, p.K, BLOCK);
         if (!hdr_ok && threadIdx.x == 64 && blockIdx.x == 0) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_BAD_PACKED);
-        const int quad = warp & 3, half = ((p.nt >> 1) + 7) / 8 * 8, h0 = (warp - 2) >= 4 ? half : 0, h1 = (warp - 2) >= 4 ? p.nt : half;
-        const bool odd = (lane & 1) != 0, pairs_ok = (p.N & 1) == 0 && (p.ldy & 1) == 0 && (reinterpret_cast<uintptr_t>(p.y) & 3) == 0;
-        const uint32_t acce_lead = mapa_u32(acce0, 0);
+        const int quad = warp & 3, half = p.nt >> 1;
+        const bool second = warp >= 6, odd = (lane & 1) != 0;
+        const bool pairs_ok = (p.N & 1) == 0 && (p.ldy & 1) == 0 && (reinterpret_cast<uintptr_t>(p.y) & 3) == 0;
+        const uint32_t acce_lead = mapa_u32(acce0, 0), shared_lead = mapa_u32(shared0, 0);
         const float *a_row = reinterpret_cast<const float *>(p.a + p.a_rows), *w_row = reinterpret_cast<const float *>(p.w + p.w_rows);
         uint32_t ti = 0;
         for (int tile = worker; tile < tiles; tile += workers, ++ti) {
             const uint32_t b = ti & 1u;
-            const int m0 = tile / p.tiles_n * p.nt, n = (tile % p.tiles_n) * 256 + (int)rank * 128 + quad * 32 + lane, n2 = n & ~1;
-            const int end = min(h1, p.M - m0);
-            const bool put = hdr_ok && n < p.N;
-            const float wr = BLOCK == 16 && n < p.N ? w_row[n] : 1.f;
-            const float w0 = odd ? __shfl_xor_sync(0xffffffffu, wr, 1) : wr;
-            const float w1 = odd ? wr : __shfl_xor_sync(0xffffffffu, wr, 1);
+            const int tm = tile / p.tiles_n, m0 = tm * p.nt, n = (tile - tm * p.tiles_n) * 256 + (int)rank * 128 + quad * 32 + lane, n2 = n & ~1;
+            const int end = p.M - m0, t0 = second ? half : 0;
+            const bool put = hdr_ok && n2 < p.N, put1 = n2 + 1 < p.N;
+            float w0 = 1.f, w1 = 1.f;
+            if constexpr (BLOCK == 16) {
+                w0 = w_row[min(n2, p.N - 1)];
+                w1 = w_row[min(n2 + 1, p.N - 1)];
+            }
+            T *y = static_cast<T *>(p.y) + (size_t)(m0 + (odd ? 1 : 0)) * p.ldy + n2;
+            const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + b * kPairAcc1;
+            auto store32 = [&](int t, const uint32_t (&r)[32]) {
+                float ar = 1.f;
+                if constexpr (BLOCK == 16) ar = ld_dependent(a_row + min(m0 + t + lane, p.M - 1));
+                T *yt = y + (size_t)t * p.ldy;
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? r[e] : r[e + 1], 1), keep = odd ? r[e + 1] : r[e];
+                    float c0 = __uint_as_float(odd ? got : keep), c1 = __uint_as_float(odd ? keep : got);
+                    if constexpr (BLOCK == 16) {
+                        const float f = __shfl_sync(0xffffffffu, ar, e + (odd ? 1 : 0));
+                        c0 *= w0 * f;
+                        c1 *= w1 * f;
+                    }
+                    if (t + e + (odd ? 1 : 0) < end && put) {
+                        if (pairs_ok) *reinterpret_cast<uint32_t *>(yt) = f4_from_float2<T>(c0, c1);
+                        else {
+                            yt[0] = f4_from_float<T>(c0);
+                            if (put1) yt[1] = f4_from_float<T>(c1);
+                        }
+                    }
+                    yt += 2 * (size_t)p.ldy;
+                }
+            };
             ok = warp_all(mbar_wait(accf0 + 8 * b, (ti >> 1) & 1u));
             if (!ok) break;
             tcgen05_fence_after();
-            const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + b * kPairCols;
-#pragma unroll 1
-            for (int t = h0; t < end; t += 8) {
-                uint32_t r[8];
-                tcgen05_ld_32x32b_x8(acc + (uint32_t)t, r);
-                float ar[4];
-                if constexpr (BLOCK == 16) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) ar[e] = ld_dependent(a_row + min(m0 + t + 2 * e + (odd ? 1 : 0), p.M - 1));
-                }
+            int done0 = t0, done1 = t0;                          // columns taken before the others
+            if (overlap && second == (b == 0)) {
+                // the columns that the next tile's accumulator has too: all in registers, then that tile may start
+                const int t = second ? kPairAcc1 : 0;
+                uint32_t r0[32], r1[32];
+                tcgen05_ld_32x32b_x32(acc + (uint32_t)t, r0);
+                tcgen05_ld_32x32b_x32(acc + (uint32_t)t + 32u, r1);
                 tcgen05_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t keep = odd ? r[2 * e + 1] : r[2 * e], got = __shfl_xor_sync(0xffffffffu, odd ? r[2 * e] : r[2 * e + 1], 1);
-                    float c0 = __uint_as_float(odd ? got : keep), c1 = __uint_as_float(odd ? keep : got);
-                    if constexpr (BLOCK == 16) {
-                        c0 *= w0 * ar[e];
-                        c1 *= w1 * ar[e];
-                    }
-                    const int tt = t + 2 * e + (odd ? 1 : 0);
-                    if (tt < end) {
-                        T *y = static_cast<T *>(p.y) + (size_t)(m0 + tt) * p.ldy + n2;
-                        if (pairs_ok) {
-                            if (put) *reinterpret_cast<uint32_t *>(y) = f4_from_float2<T>(c0, c1);
-                        } else if (hdr_ok) {
-                            if (n2 < p.N) y[0] = f4_from_float<T>(c0);
-                            if (n2 + 1 < p.N) y[1] = f4_from_float<T>(c1);
-                        }
-                    }
-                }
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(shared_lead);
+                if (t < end) store32(t, r0);
+                if (t + 32 < end) store32(t + 32, r1);
+                done0 = t;
+                done1 = t + 64;
+            }
+#pragma unroll 1
+            for (int t = t0; t < t0 + half && t < end; t += 32) {
+                if (t >= done0 && t < done1) continue;
+                uint32_t r[32];
+                tcgen05_ld_32x32b_x32(acc + (uint32_t)t, r);
+                tcgen05_wait_ld();
+                store32(t, r);
             }
             tcgen05_fence_before();
             __syncwarp();
@@ -247,15 +287,16 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
     }
 }
 
-// Rows of a in a tile: the multiple of 64 with the least modelled time, rounds of tiles x (units x time of a unit + a tile's fixed part).
-inline int pair_rows(int M, int units, int tiles_n, int workers)
+// Rows of a in a tile: the multiple of 64 with the least modelled time, rounds of tiles x (units x time of a unit + a tile's own time).  The
+// loads, about 57 bytes a clock and SM, bound a unit, so that it takes 0.28 us with 128 rows and 0.33 with 256 (32-value blocks; 2048 x 3584 x
+// 18944 with 128 / 192 / 256 rows a tile: 79.7 / 61.8 / 53.2 us, 8192 x 18944 x 3584: 282 / 213 / 183).
+inline int pair_rows(int M, int steps, int tiles_n, int workers)
 {
     int best = 64;
     double least = 1e300;
     for (int nt = 64; nt <= kPairCols; nt += 64) {
         const long long tiles = (long long)((M + nt - 1) / nt) * tiles_n, rounds = (tiles + workers - 1) / workers;
-        const double unit = nt > 128 ? 0.00060 * nt : 0.077;
-        const double us = (double)rounds * (units * unit + 0.3) + 0.005 * nt;
+        const double us = (double)rounds * (steps * (0.245 + 0.00032 * nt) + 0.1 + 0.0075 * nt);
         if (us < least - 1e-9) { least = us; best = nt; }
     }
     return best;
@@ -271,7 +312,11 @@ tman_status launch_pair(F4PairParams p, cudaStream_t s)
     if (!info) return TMAN_ERR_CUDA;
     const int workers = info->sms.load(std::memory_order_relaxed) / 2;
     p.tiles_n = (p.N + 255) / 256;
-    p.nt = pair_rows(p.M, p.units, p.tiles_n, workers);
+#ifdef F4_NT
+    p.nt = F4_NT;
+#else
+    p.nt = pair_rows(p.M, (p.halves + 1) / 2, p.tiles_n, workers);
+#endif
     p.tiles_m = (p.M + p.nt - 1) / p.nt;
     const long long tiles = (long long)p.tiles_m * p.tiles_n;
     if (tiles > 0x7FFFFFFF) return TMAN_ERR_SHAPE;

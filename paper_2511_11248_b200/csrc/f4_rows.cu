@@ -18,12 +18,12 @@ __global__ void __launch_bounds__(256) f4_relayout_kernel(uint8_t *codes, uint8_
         if (i == 0) atomicCAS(status, 0u, (uint32_t)TMAN_ERR_BAD_PACKED);
         return;
     }
-    const int pieces = L.units * (kF4Unit / 16);
+    const int pieces = L.halves * (kF4Half / 16);
     const int r = (int)(i / pieces), k = (int)(i % pieces) * 16;
     if (r >= L.tiles * kF4Tile) return;
     const int nb = K / BLOCK, b = k / BLOCK;
     if (r < L.height8) {
-        uint8_t *c = packed + L.codes_off + f4_code_at(r, k, L.height8, L.units);
+        uint8_t *c = packed + L.codes_off + f4_code_at(r, k, L);
         uint8_t *plain = codes + ((size_t)r * K + k) / 2;
         const bool in = r < rows && k < K;
         if constexpr (TO_PACKED) {
@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(256) f4_relayout_kernel(uint8_t *codes, uint8_
         }
     }
     if (k % (4 * BLOCK) == 0) {
-        uint8_t *c = packed + L.scales_off + f4_scale_at(r, b, BLOCK, L.units);
+        uint8_t *c = packed + L.scales_off + f4_scale_at(r, b, BLOCK, L);
         for (int e = 0; e < 4; ++e) {
             const bool in = r < rows && b + e < nb;
             if constexpr (TO_PACKED) c[e] = in ? scales[(size_t)r * nb + b + e] : 0;
@@ -56,7 +56,7 @@ template <bool TO_PACKED>
 static tman_status launch_relayout(uint8_t *codes, uint8_t *scales, float *row_scale, int rows, int K, int block, void *packed, uint32_t *status, cudaStream_t s)
 {
     const F4Layout L = f4_layout(rows, K, block);
-    const size_t threads = (size_t)L.tiles * kF4Tile * L.units * (kF4Unit / 16), grid = (threads + 255) / 256;
+    const size_t threads = (size_t)L.tiles * kF4Tile * L.halves * (kF4Half / 16), grid = (threads + 255) / 256;
     if (grid > 0x7FFFFFFFull) return TMAN_ERR_SHAPE;
     auto kern = block == 32 ? f4_relayout_kernel<32, TO_PACKED> : f4_relayout_kernel<16, TO_PACKED>;
     kern<<<(unsigned)grid, 256, 0, s>>>(codes, scales, row_scale, rows, K, static_cast<uint8_t *>(packed), L, status);
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(256) f4_quantize_kernel(const T *x, int ldx, i
         inv_row = __fdiv_rn(1.f, rs);
         if (threadIdx.x == 0) reinterpret_cast<float *>(packed + L.rows_off)[r] = rs;
     }
-    const int vectors = L.units * (kF4Unit / 8);
+    const int vectors = L.halves * (kF4Half / 8);
     for (int at = threadIdx.x; at < (vectors + 31) / 32 * 32; at += 256) {          // (whole warps: lanes of a block exchange)
         float f[8];
         load(at, f);
@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(256) f4_quantize_kernel(const T *x, int ldx, i
         if (at >= vectors) continue;
         const int k = at * 8;
         const uint32_t scale = k < K ? f4_block_scale<BLOCK>(top, fine, inv_row) : 0u;
-        if (r < L.height8) *reinterpret_cast<uint32_t *>(packed + L.codes_off + f4_code_at(r, k, L.height8, L.units)) = f4_block_codes<BLOCK>(f, scale, inv_row);
-        if (k % BLOCK == 0) packed[L.scales_off + f4_scale_at(r, k / BLOCK, BLOCK, L.units)] = (uint8_t)scale;
+        if (r < L.height8) *reinterpret_cast<uint32_t *>(packed + L.codes_off + f4_code_at(r, k, L)) = f4_block_codes<BLOCK>(f, scale, inv_row);
+        if (k % BLOCK == 0) packed[L.scales_off + f4_scale_at(r, k / BLOCK, BLOCK, L)] = (uint8_t)scale;
     }
 }
 
@@ -200,7 +200,7 @@ static tman_status launch_quantize_as(const void *x, int ldx, int rows, int K, v
 
 tman_status launch_f4_quantize(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, cudaStream_t s)
 {
-    if (dtype == kF4Half) return block == 32 ? launch_quantize_as<32, __half>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __half>(x, ldx, rows, K, packed, s);
+    if (dtype == kF4TypeHalf) return block == 32 ? launch_quantize_as<32, __half>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __half>(x, ldx, rows, K, packed, s);
     return block == 32 ? launch_quantize_as<32, __nv_bfloat16>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __nv_bfloat16>(x, ldx, rows, K, packed, s);
 }
 
@@ -215,8 +215,8 @@ __global__ void __launch_bounds__(256) f4_dequant_kernel(const uint8_t *packed, 
     const int r = blockIdx.x;
     const float rs = BLOCK == 16 ? reinterpret_cast<const float *>(packed + L.rows_off)[r] : 1.f;
     for (int k = threadIdx.x * 8; k < K; k += 256 * 8) {
-        const uint32_t c = *reinterpret_cast<const uint32_t *>(packed + L.codes_off + f4_code_at(r, k, L.height8, L.units));
-        const float s = f4_scale_value<BLOCK>(packed[L.scales_off + f4_scale_at(r, k / BLOCK, BLOCK, L.units)]) * rs;
+        const uint32_t c = *reinterpret_cast<const uint32_t *>(packed + L.codes_off + f4_code_at(r, k, L));
+        const float s = f4_scale_value<BLOCK>(packed[L.scales_off + f4_scale_at(r, k / BLOCK, BLOCK, L)]) * rs;
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -236,7 +236,7 @@ static tman_status launch_dequant_as(const void *packed, int rows, int K, void *
 
 tman_status launch_f4_dequant(const void *packed, int rows, int K, int block, void *x, int ldx, int dtype, uint32_t *status, cudaStream_t s)
 {
-    if (dtype == kF4Half) return block == 32 ? launch_dequant_as<32, __half>(packed, rows, K, x, ldx, status, s) : launch_dequant_as<16, __half>(packed, rows, K, x, ldx, status, s);
+    if (dtype == kF4TypeHalf) return block == 32 ? launch_dequant_as<32, __half>(packed, rows, K, x, ldx, status, s) : launch_dequant_as<16, __half>(packed, rows, K, x, ldx, status, s);
     return block == 32 ? launch_dequant_as<32, __nv_bfloat16>(packed, rows, K, x, ldx, status, s) : launch_dequant_as<16, __nv_bfloat16>(packed, rows, K, x, ldx, status, s);
 }
 

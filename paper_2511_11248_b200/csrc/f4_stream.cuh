@@ -27,8 +27,11 @@ namespace {
 constexpr int kStreamThreads = 320;      // warp 0: loads, warp 1: MMAs, warps 2..9: digits, epilogue
 constexpr int kStreamMaxRows = 128;      // of a packed x
 constexpr int kStreamMaxSplit = 8;
-constexpr int kStreamMaxStages = 24;
-constexpr int kDigitLbo = 144, kDigitSbo = 4 * kDigitLbo;      // (a bank's width more than the core matrices: the digits' stores meet no conflict)
+constexpr int kStreamMaxStages = 12;
+// Digits in shared memory: core matrices 16 bytes further apart than they are long, rows of x 64 bytes (mod 128), half units another 64, so
+// that the stores of a warp (four bytes of 32 places along k) meet no bank twice.
+constexpr int kDigitLbo = 144, kDigitSbo = 4 * kDigitLbo;
+__host__ __device__ constexpr int digit_half(int M) { return (M + 1) / 2 * 2 * kDigitSbo + 64; }
 
 struct F4StreamParams {
     const uint8_t *w, *a;                // packed weights, packed x
@@ -36,11 +39,11 @@ struct F4StreamParams {
     void *y;
     uint32_t *status;
     size_t w_codes, w_scales, w_rows, a_codes, a_scales, a_rows;
-    int M, K, N, ldx, ldy, units, height8, split, stages, stage_bytes, cols;
+    int M, K, N, ldx, ldy, halves, height8, split, stages, stage_bytes, cols;
 };
 
-template <int BLOCK, bool DIGITS>
-__host__ __device__ inline int stream_b_bytes(int M, int cols) { return DIGITS ? (M + 1) / 2 * 2 * kDigitSbo : cols * 64; }
+template <bool DIGITS>
+__host__ __device__ inline int stream_b_bytes(int M, int cols) { return DIGITS ? 2 * digit_half(M) : cols * 128; }
 
 // Balanced octal digits of eight numbers, as e2m1 codes: word j of the result holds digit j of number i in bits 4 i.
 // y[i] = X + sum_{j<7} 4 8^j + 2 8^7, so that octal digit j of y is n_j + 4 (of the top one n_7 + 2).
@@ -83,24 +86,23 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
     __shared__ __align__(8) uint64_t full_bar[kStreamMaxStages], empty_bar[kStreamMaxStages], acc_bar;
     __shared__ uint32_t tmem_slot, row_top[8];
     __shared__ float w_row[128], a_row[kStreamMaxRows];
-    constexpr int SB = BLOCK == 32 ? 512 : 1024, CHUNKS = SB / 512;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = blockIdx.x % p.split, tile = blockIdx.x / p.split;
-    const int u0 = (int)((long long)p.units * rank / p.split), nu = (int)((long long)p.units * (rank + 1) / p.split) - u0;
-    const int h = min(kF4Tile, p.height8 - tile * kF4Tile);
-    const int pairs = (p.M + 1) / 2, b_bytes = stream_b_bytes<BLOCK, DIGITS>(p.M, p.cols);
+    constexpr uint32_t SB = f4_scale_bytes(BLOCK), CHUNKS = SB / 512;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (the shuffle tells the compiler that it is uniform)
+    const int rank = blockIdx.x % p.split, tile = blockIdx.x / p.split, steps = (p.halves + 1) >> 1;
+    const int u0 = (int)((long long)steps * rank / p.split), nu = (int)((long long)steps * (rank + 1) / p.split) - u0;     // units of this share
+    const int b_bytes = stream_b_bytes<DIGITS>(p.M, p.cols);
     const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), accf = smem_u32(&acc_bar), ring = smem_u32(smem);
-    const uint32_t off_sfa = kF4Tile * 64, off_b = off_sfa + SB, off_sfb = off_b + (uint32_t)b_bytes;
-    const int tmem_cols = p.cols <= 32 ? 64 : p.cols <= 96 ? 128 : 256;
+    const uint32_t off_sfa = kF4Tile * 128, off_b = off_sfa + 2 * SB, off_sfb = off_b + (uint32_t)b_bytes;
+    const int tmem_cols = p.cols <= 64 ? 128 : 256;
     bool ok = true;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.stages; ++s) {
-            mbar_init(full0 + 8 * s, DIGITS ? 1 + pairs : 1);
+            mbar_init(full0 + 8 * s, DIGITS ? 1 + p.M : 1);
             mbar_init(empty0 + 8 * s, 1);
         }
         mbar_init(accf, 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_barrier_init();
     }
     if (threadIdx.x < 8) row_top[threadIdx.x] = 0u;
     if (warp == 1) {
@@ -110,67 +112,80 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
 
+    // (Warps 0 and 1 walk as one, one lane issues: addresses and descriptors in uniform registers.)
     if (warp == 0) {
-        if (elect_one()) {
-            const uint8_t *codes = p.w + p.w_codes + (size_t)tile * p.units * (kF4Tile * 64) + (size_t)u0 * (h * 64);
-            const uint8_t *scales = p.w + p.w_scales + ((size_t)tile * p.units + u0) * SB;
-            const int a_h8 = (p.M + 7) / 8 * 8;
-            const uint8_t *a_codes = p.a + p.a_codes + (size_t)u0 * (a_h8 * 64), *a_scales = p.a + p.a_scales + (size_t)u0 * SB;
-            const uint32_t tx = (uint32_t)(h * 64 + SB) + (DIGITS ? 0u : (uint32_t)(a_h8 * 64 + SB));
-            auto load_w = [&](int i, int s) {
-                const uint32_t st = ring + (uint32_t)(s * p.stage_bytes), bar = full0 + 8 * s;
-                mbar_expect_tx(bar, tx);
-                bulk_load(st, codes + (size_t)i * (h * 64), (uint32_t)(h * 64), bar);
-                bulk_load(st + off_sfa, scales + (size_t)i * SB, SB, bar);
-            };
-            auto load_a = [&](int i, int s) {
-                const uint32_t st = ring + (uint32_t)(s * p.stage_bytes), bar = full0 + 8 * s;
-                bulk_load(st + off_b, a_codes + (size_t)i * (a_h8 * 64), (uint32_t)(a_h8 * 64), bar);
-                bulk_load(st + off_sfb, a_scales + (size_t)i * SB, SB, bar);
-            };
-            // weights of the first stages before the wait for the kernel ahead: nothing that may still be running writes them
-            const int first = min(nu, p.stages);
-            for (int i = 0; i < first; ++i) load_w(i, i);
-            if constexpr (!DIGITS) {
-                grid_wait();
-                for (int i = 0; i < first; ++i) load_a(i, i);
-            }
-            int s = 0;
-            uint32_t ph = 0;
-            for (int i = first; i < nu; ++i) {
-                if (!mbar_wait(empty0 + 8 * s, ph)) { ok = false; break; }
-                load_w(i, s);
-                if constexpr (!DIGITS) load_a(i, s);
-                if (++s == p.stages) { s = 0; ph ^= 1u; }
-            }
-        }
-        __syncwarp();
-    } else if (warp == 1) {
-        if (elect_one()) {
-            const uint32_t id0 = f4_idesc(BLOCK, 128, p.cols, 0), id1 = f4_idesc(BLOCK, 128, p.cols, BLOCK == 32 ? 2 : 0);
-            const uint32_t sf0 = tmem + (uint32_t)p.cols;
-            const uint32_t lbo = DIGITS ? kDigitLbo : 128, sbo = DIGITS ? kDigitSbo : 512;
-            int s = 0;
-            uint32_t ph = 0;
-            for (int i = 0; i < nu; ++i) {
-                if (!mbar_wait(full0 + 8 * s, ph)) { ok = false; break; }
-                tcgen05_fence_after();
-                const uint32_t st = ring + (uint32_t)(s * p.stage_bytes), sfa = sf0 + (uint32_t)(i & 1) * 16u, sfb = sfa + 8u;
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) {
-                    tcgen05_cp_scales(sfa + 4 * c, make_kmajor_desc(st + off_sfa + 512 * c, 128, 128));
-                    tcgen05_cp_scales(sfb + 4 * c, make_kmajor_desc(st + off_sfb + 512 * c, 128, 128));
+        const bool lead = elect_one();
+        const int w_tiles = (p.height8 + kF4Tile - 1) / kF4Tile, a_h8 = (p.M + 7) / 8 * 8;
+        const uint32_t wb_full = (uint32_t)min(kF4Tile, p.height8 - tile * kF4Tile) * 128u, ab_full = DIGITS ? 0u : (uint32_t)a_h8 * 128u;
+        auto load = [&](int i, int s, bool do_w, bool do_a) {
+            const int u = u0 + i;
+            const uint32_t sh = 2 * u + 1 < p.halves ? 0u : 1u;  // a half unit's sections are half as wide
+            const uint8_t *w = p.w + p.w_codes + (size_t)u * p.height8 * 128 + ((size_t)tile * (kF4Tile * 128) >> sh);
+            const uint8_t *ws = p.w + p.w_scales + (size_t)u * w_tiles * (2 * SB) + ((size_t)tile * (2 * SB) >> sh);
+            const uint8_t *a = p.a + p.a_codes + (size_t)u * a_h8 * 128, *as = p.a + p.a_scales + (size_t)u * (2 * SB);
+            const uint32_t wb = wb_full >> sh, ab = ab_full >> sh, sb = 2 * SB >> sh, st = ring + (uint32_t)(s * p.stage_bytes), bar = full0 + 8 * s;
+            if (lead) {
+                if (do_w) {
+                    mbar_expect_tx(bar, DIGITS ? wb + sb : wb + ab + 2 * sb);
+                    bulk_load(st, w, wb, bar);
+                    bulk_load(st + off_sfa, ws, sb, bar);
                 }
-                tcgen05_mma_f4<BLOCK>(tmem, make_kmajor_desc(st, 128, 512), make_kmajor_desc(st + off_b, lbo, sbo), id0, sfa, sfb, i > 0);
-                tcgen05_mma_f4<BLOCK>(tmem, make_kmajor_desc(st + 256, 128, 512), make_kmajor_desc(st + off_b + 2 * lbo, lbo, sbo), id1,
-                                      sfa + (BLOCK == 32 ? 0 : 4), sfb + (BLOCK == 32 ? 0 : 4), 1);
-                tcgen05_commit(empty0 + 8 * s);
-                if (++s == p.stages) { s = 0; ph ^= 1u; }
+                if (do_a) {
+                    bulk_load(st + off_b, a, ab, bar);
+                    bulk_load(st + off_sfb, as, sb, bar);
+                }
             }
-            tcgen05_commit(accf);
+            __syncwarp();
+        };
+        // weights of the first stages before the wait for the kernel ahead: nothing that may still be running writes them
+        const int first = min(nu, p.stages);
+        for (int i = 0; i < first; ++i) load(i, i, true, false);
+        if constexpr (!DIGITS) {
+            grid_wait();
+            for (int i = 0; i < first; ++i) load(i, i, false, true);
         }
+        int s = 0;
+        uint32_t ph = 0;
+        for (int i = first; i < nu; ++i) {
+            if (!warp_all(mbar_wait(empty0 + 8 * s, ph))) { ok = false; break; }
+            load(i, s, true, !DIGITS);
+            if (++s == p.stages) { s = 0; ph ^= 1u; }
+        }
+    } else if (warp == 1) {
+        const bool lead = elect_one();
+        const uint32_t id0 = f4_idesc(BLOCK, 128, p.cols, 0), id1 = f4_idesc(BLOCK, 128, p.cols, BLOCK == 32 ? 2 : 0);
+        const uint64_t sf0 = make_kmajor_desc(ring, 128, 128);                     // (+ 1: 16 bytes)
+        const uint32_t b_half = DIGITS ? (uint32_t)digit_half(p.M) : 512u, b_chunk = DIGITS ? kDigitLbo : 128;
+        int s = 0;
+        uint32_t ph = 0;
+        for (int i = 0; i < nu; ++i) {
+            const uint32_t at = (uint32_t)(s * p.stage_bytes) >> 4, two = 2 * (u0 + i) + 1 < p.halves ? 2u : 1u;
+            const uint64_t wd = make_kmajor_desc(ring, 128, two * 512) + at, sf = sf0 + at;
+            const uint64_t xd = make_kmajor_desc(ring + off_b, b_chunk, DIGITS ? kDigitSbo : two * 512) + at;
+            if (!warp_all(mbar_wait(full0 + 8 * s, ph))) { ok = false; break; }
+            tcgen05_fence_after();
+            if (lead) {
+#pragma unroll
+                for (uint32_t u = 0; u < 2; ++u)
+                    if (u < two) {
+                        const uint32_t sfa = tmem + (uint32_t)p.cols + u * 16u, sfb = sfa + 8u;
+#pragma unroll
+                        for (uint32_t c = 0; c < CHUNKS; ++c) {
+                            tcgen05_cp_scales(sfa + 4 * c, sf + ((off_sfa + u * SB + 512 * c) >> 4));
+                            tcgen05_cp_scales(sfb + 4 * c, sf + ((off_sfb + u * SB + 512 * c) >> 4));
+                        }
+                        const uint64_t wa = wd + ((u * 512) >> 4), xb = xd + ((u * b_half) >> 4);
+                        tcgen05_mma_f4<BLOCK>(tmem, wa, xb, id0, sfa, sfb, (i | (int)u) != 0);
+                        tcgen05_mma_f4<BLOCK>(tmem, wa + 16, xb + ((2 * b_chunk) >> 4), id1, sfa + (BLOCK == 32 ? 0 : 4), sfb + (BLOCK == 32 ? 0 : 4), 1);
+                    }
+                tcgen05_commit(empty0 + 8 * s);
+            }
+            __syncwarp();
+            if (++s == p.stages) { s = 0; ph ^= 1u; }
+        }
+        if (lead) tcgen05_commit(accf);
         __syncwarp();
     } else {
         const int pt = threadIdx.x - 64;
@@ -184,9 +199,9 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
             const int l16 = lane & 15;
             if constexpr (BLOCK == 16) {
                 // the largest magnitude of each row of this share of k (of a row that holds an infinity or a NaN: whatever comes out)
-                const int k1 = min(p.K, (u0 + nu) * kF4Unit);
+                const int k1 = min(p.K, (u0 + nu) * (2 * kF4Half));
                 uint32_t mx[8] = {};
-                for (int k = u0 * kF4Unit + pt * 8; k < k1; k += 256 * 8) {
+                for (int k = u0 * (2 * kF4Half) + pt * 8; k < k1; k += 256 * 8) {
                     uint4 v[8];
 #pragma unroll
                     for (int m = 0; m < 8; ++m)
@@ -204,17 +219,21 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
                     }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             }
-            const int jobs = nu * pairs;
+            // a job: a row's 256 values of a unit, eight a lane
+            const int jobs = nu * p.M;
             auto fetch = [&](int j) {
-                const int m = 2 * (j % pairs) + (lane >> 4), k = (u0 + j / pairs) * kF4Unit + l16 * 8;
-                return m < p.M && k < p.K ? ld_dependent(reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx + k)) : make_uint4(0u, 0u, 0u, 0u);
+                const int m = j % p.M, k = (u0 + j / p.M) * (2 * kF4Half) + lane * 8;
+                return k < p.K ? ld_dependent(reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx + k)) : make_uint4(0u, 0u, 0u, 0u);
             };
+            // A wait for a free slot names its turn by parity alone: it holds only where the turn before is known to have passed.  So a warp's
+            // units lie at most a round of the ring apart: the unit before, whose slot's turn it has waited for, is at least as late.
+            const int teams = min(8, p.stages * p.M);
             uint4 next = make_uint4(0u, 0u, 0u, 0u);
-            if (warp - 2 < jobs) next = fetch(warp - 2);
-            for (int j = warp - 2; j < jobs; j += 8) {
+            if (warp - 2 < min(jobs, teams)) next = fetch(warp - 2);
+            for (int j = warp - 2; j < jobs && warp - 2 < teams; j += teams) {
                 const uint4 cur = next;
-                if (j + 8 < jobs) next = fetch(j + 8);
-                const int i = j / pairs, m = 2 * (j % pairs) + (lane >> 4), s = i % p.stages;
+                if (j + teams < jobs) next = fetch(j + teams);
+                const int i = j / p.M, m = j % p.M, s = i % p.stages;
                 const uint32_t w[4] = {cur.x, cur.y, cur.z, cur.w};
                 float f[8];
                 float top = 0.f;
@@ -237,7 +256,7 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
                     e2 = max((int)eb, std::is_same<T, __half>::value ? 103 : 1);
                     byte = eb == 255u ? 255u : (uint32_t)e2;
                 } else {
-                    const uint32_t rt = row_top[m < p.M ? m : 0];
+                    const uint32_t rt = row_top[m];
                     const int r2 = max((int)(__float_as_uint(f4_to_float2<T>(rt).x) >> 23) - 8, 16);     // the row's power of two, + 127
                     e2 = min(max((int)eb, r2 - 9), r2 + 8);
                     const int d = e2 - r2;                       // -9 .. 8
@@ -267,12 +286,14 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
                     if (!ok) break;
                 }
                 uint8_t *st = smem + (size_t)s * p.stage_bytes;
-                uint8_t *b = st + off_b + m * kDigitSbo + (l16 >> 2) * kDigitLbo + (l16 & 3) * 4;
+                if (lane < 16 || 2 * (u0 + i) + 1 < p.halves) {
+                    uint8_t *b = st + off_b + (lane >> 4) * digit_half(p.M) + m * kDigitSbo + (l16 >> 2) * kDigitLbo + (l16 & 3) * 4;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) *reinterpret_cast<uint32_t *>(b + e * 16) = d[e];
-                if (BLOCK == 16 || l16 < 8) {
-                    const int t = 8 * m + (l16 & 7);
-                    *reinterpret_cast<uint32_t *>(st + off_sfb + (l16 >> 3) * 512 + (t & 31) * 16 + (t >> 5) * 4) = word;
+                    for (int e = 0; e < 8; ++e) *reinterpret_cast<uint32_t *>(b + e * 16) = d[e];
+                    if (BLOCK == 16 || l16 < 8) {
+                        const int t = 8 * m + (l16 & 7);
+                        *reinterpret_cast<uint32_t *>(st + off_sfb + ((lane >> 4) * CHUNKS + (l16 >> 3)) * 512 + (t & 31) * 16 + (t >> 5) * 4) = word;
+                    }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -348,10 +369,10 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
 }
 
 // Shares of k: as few as give most SMs a CTA.
-inline int stream_split(int tiles, int units)
+inline int stream_split(int tiles, int units)      // units of 256
 {
     int s = 1;
-    while (s < kStreamMaxSplit && tiles * (s + 1) <= 148 && units >= 2 * (s + 1)) ++s;
+    while (s < kStreamMaxSplit && tiles * (s + 1) <= 148 && units >= s + 1) ++s;
     return s;
 }
 
@@ -364,12 +385,14 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     if (!device_info(&dev)) return TMAN_ERR_CUDA;
     const int tiles = (p.N + kF4Tile - 1) / kF4Tile;
     p.cols = DIGITS ? (p.M + 1) / 2 * 16 : (p.M + 15) / 16 * 16;
-    p.split = stream_split(tiles, p.units);
-    p.stage_bytes = (kF4Tile * 64 + 2 * f4_scale_bytes(BLOCK) + stream_b_bytes<BLOCK, DIGITS>(p.M, p.cols) + 127) / 128 * 128;
-    const int budget = 110 * 1024, least = p.M * 512;            // (the sums of a share lie on the ring)
+    const int steps = (p.halves + 1) / 2;
+    p.split = stream_split(tiles, steps);
+    p.stage_bytes = (kF4Tile * 128 + 4 * f4_scale_bytes(BLOCK) + stream_b_bytes<DIGITS>(p.M, p.cols) + 127) / 128 * 128;
+    // half an SM, so that the next call's CTAs fill their rings beside this one's; more where that holds few stages
+    const int budget = p.stage_bytes * 4 <= 110 * 1024 ? 110 * 1024 : 210 * 1024, least = p.M * 512;      // (the sums of a share lie on the ring)
     p.stages = budget / p.stage_bytes;
     if (p.stages > kStreamMaxStages) p.stages = kStreamMaxStages;
-    const int share = (p.units + p.split - 1) / p.split;
+    const int share = (steps + p.split - 1) / p.split;
     if (p.stages > share) p.stages = share;
     int bytes = p.stages * p.stage_bytes;
     if (bytes < least) bytes = least;
@@ -388,7 +411,7 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = packed_write_pending(s, /*clear=*/true) ? 1 : 2;
-    return launch_with_smem(kern, 112 * 1024, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
+    return launch_with_smem(kern, 210 * 1024, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
 }
 
 }  // namespace
