@@ -24,14 +24,17 @@
 namespace tman {
 namespace {
 
-constexpr int kStreamThreads = 320;      // warp 0: loads, warp 1: MMAs, warps 2..9: digits, epilogue
+constexpr int kDigitWarps = 16;
+__host__ __device__ constexpr int stream_threads(bool digits) { return digits ? 64 + 32 * kDigitWarps : 192; }      // warp 0: loads, 1: MMAs, others: digits, epilogue
 constexpr int kStreamMaxRows = 128;      // of a packed x
 constexpr int kStreamMaxSplit = 8;
+constexpr int kStreamPushRows = 16;
+constexpr int kStreamHalfSm = 111 * 1024, kStreamAllSm = 220 * 1024;
 constexpr int kStreamMaxStages = 12;
-// Digits in shared memory: core matrices 16 bytes further apart than they are long, rows of x 64 bytes (mod 128), half units another 64, so
-// that the stores of a warp (four bytes of 32 places along k) meet no bank twice.
+// Digits in shared memory: core matrices 16 bytes further apart than they are long, half units 64 bytes (mod 128), so that the stores of a warp
+// (four bytes of 32 places along k) meet no bank twice.  Of an odd M the tile's last eight columns are whatever lies behind.
 constexpr int kDigitLbo = 144, kDigitSbo = 4 * kDigitLbo;
-__host__ __device__ constexpr int digit_half(int M) { return (M + 1) / 2 * 2 * kDigitSbo + 64; }
+__host__ __device__ constexpr int digit_half(int M) { return M * kDigitSbo + (M % 2 ? 0 : 64); }
 
 struct F4StreamParams {
     const uint8_t *w, *a;                // packed weights, packed x
@@ -80,11 +83,11 @@ __device__ __forceinline__ void digit_codes(const uint32_t (&y)[8], uint32_t (&o
 }
 
 template <int BLOCK, typename T, bool DIGITS>
-__global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_constant__ F4StreamParams p)
+__global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_stream_kernel(const __grid_constant__ F4StreamParams p)
 {
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t full_bar[kStreamMaxStages], empty_bar[kStreamMaxStages], acc_bar;
-    __shared__ uint32_t tmem_slot, row_top[8];
+    __shared__ __align__(8) uint64_t full_bar[kStreamMaxStages], empty_bar[kStreamMaxStages], acc_bar, sums_bar;
+    __shared__ uint32_t tmem_slot, row_top[8], bad_header;
     __shared__ float w_row[128], a_row[kStreamMaxRows];
     constexpr uint32_t SB = f4_scale_bytes(BLOCK), CHUNKS = SB / 512;
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (the shuffle tells the compiler that it is uniform)
@@ -94,6 +97,10 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
     const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), accf = smem_u32(&acc_bar), ring = smem_u32(smem);
     const uint32_t off_sfa = kF4Tile * 128, off_b = off_sfa + 2 * SB, off_sfb = off_b + (uint32_t)b_bytes;
     const int tmem_cols = p.cols <= 64 ? 128 : 256;
+    // Sums of a tile's shares: of few rows every CTA sends its own to the CTA that adds up a channel, [share][row][own channel] behind its ring;
+    // of more rows the adding CTA fetches them.
+    const bool push = p.split > 1 && p.M <= kStreamPushRows;
+    const int per = (128 + p.split - 1) / p.split, own0 = per * rank, own_n = min(per, 128 - own0);      // channels added up here
     bool ok = true;
 
     if (threadIdx.x == 0) {
@@ -102,7 +109,10 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
             mbar_init(empty0 + 8 * s, 1);
         }
         mbar_init(accf, 1);
+        mbar_init(smem_u32(&sums_bar), 1);
+        if (push) mbar_expect_tx(smem_u32(&sums_bar), (uint32_t)(p.split * p.M * own_n) * 4u);
         fence_barrier_init();
+        bad_header = 0u;
     }
     if (threadIdx.x < 8) row_top[threadIdx.x] = 0u;
     if (warp == 1) {
@@ -111,6 +121,7 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
     }
     tcgen05_fence_before();
     __syncthreads();
+    cluster_arrive();                    // (waited for before the sums are sent)
     tcgen05_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
 
@@ -189,10 +200,12 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
         __syncwarp();
     } else {
         const int pt = threadIdx.x - 64;
+        if (pt == 0 && !f4_header_matches(p.w, p.N, p.K, BLOCK)) bad_header = 1u;
         if (BLOCK == 16 && pt < 128) w_row[pt] = tile * 128 + pt < p.N ? reinterpret_cast<const float *>(p.w + p.w_rows)[tile * 128 + pt] : 0.f;
         grid_wait();
         grid_launch_next();
         if constexpr (!DIGITS) {
+            if (pt == 32 && !f4_header_matches(p.a, p.M, p.K, BLOCK)) bad_header = 1u;
             if (BLOCK == 16 && pt < p.M) a_row[pt] = ld_dependent(reinterpret_cast<const float *>(p.a + p.a_rows) + pt);
         } else {
             const T *x = static_cast<const T *>(p.x);
@@ -200,40 +213,42 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
             if constexpr (BLOCK == 16) {
                 // the largest magnitude of each row of this share of k (of a row that holds an infinity or a NaN: whatever comes out)
                 const int k1 = min(p.K, (u0 + nu) * (2 * kF4Half));
-                uint32_t mx[8] = {};
-                for (int k = u0 * (2 * kF4Half) + pt * 8; k < k1; k += 256 * 8) {
-                    uint4 v[8];
+#pragma unroll 1
+                for (int m0 = 0; m0 < p.M; m0 += 4) {
+                    uint32_t mx[4] = {};
+                    for (int k = u0 * (2 * kF4Half) + pt * 8; k < k1; k += 32 * kDigitWarps * 8) {
+                        uint4 v[4];
 #pragma unroll
-                    for (int m = 0; m < 8; ++m)
-                        if (m < p.M) v[m] = ld_dependent(reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx + k));
+                        for (int e = 0; e < 4; ++e) v[e] = ld_dependent(reinterpret_cast<const uint4 *>(x + (size_t)min(m0 + e, p.M - 1) * p.ldx + k));
 #pragma unroll
-                    for (int m = 0; m < 8; ++m)
-                        if (m < p.M)
-                            mx[m] = __vmaxu2(mx[m], __vmaxu2(__vmaxu2(v[m].x & 0x7FFF7FFFu, v[m].y & 0x7FFF7FFFu), __vmaxu2(v[m].z & 0x7FFF7FFFu, v[m].w & 0x7FFF7FFFu)));
-                }
-#pragma unroll
-                for (int m = 0; m < 8; ++m)
-                    if (m < p.M) {
-                        const uint32_t top = __reduce_max_sync(0xffffffffu, max(mx[m] & 0xFFFFu, mx[m] >> 16));
-                        if (lane == 0) atomicMax(&row_top[m], top);
+                        for (int e = 0; e < 4; ++e)
+                            mx[e] = __vmaxu2(mx[e], __vmaxu2(__vmaxu2(v[e].x & 0x7FFF7FFFu, v[e].y & 0x7FFF7FFFu), __vmaxu2(v[e].z & 0x7FFF7FFFu, v[e].w & 0x7FFF7FFFu)));
                     }
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t top = __reduce_max_sync(0xffffffffu, max(mx[e] & 0xFFFFu, mx[e] >> 16));
+                        if (lane == 0) atomicMax(&row_top[min(m0 + e, p.M - 1)], top);
+                    }
+                }
+                asm volatile("bar.sync 1, %0;" ::"n"(32 * kDigitWarps) : "memory");
             }
-            // a job: a row's 256 values of a unit, eight a lane
-            const int jobs = nu * p.M;
-            auto fetch = [&](int j) {
-                const int m = j % p.M, k = (u0 + j / p.M) * (2 * kF4Half) + lane * 8;
-                return k < p.K ? ld_dependent(reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx + k)) : make_uint4(0u, 0u, 0u, 0u);
+            // A warp has a row, and of its units every `teams`-th; a lane eight of a unit's 256 values.  A wait for a free slot names its turn by parity
+            // alone: it holds only where the turn before is known to have passed.  So a warp's units lie at most a round of the ring
+            // apart: the unit before, whose slot's turn it has waited for, is at least as late.
+            const int teams = min(kDigitWarps / p.M, p.stages), team = (warp - 2) / p.M, m = (warp - 2) - team * p.M;
+            const uint4 *xm = reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx) + lane;
+            auto fetch = [&](int i) {
+                const int at = (u0 + i) * (2 * kF4Half / 8);
+                return i < nu && at + lane < p.K / 8 ? ld_dependent(xm + at) : make_uint4(0u, 0u, 0u, 0u);
             };
-            // A wait for a free slot names its turn by parity alone: it holds only where the turn before is known to have passed.  So a warp's
-            // units lie at most a round of the ring apart: the unit before, whose slot's turn it has waited for, is at least as late.
-            const int teams = min(8, p.stages * p.M);
             uint4 next = make_uint4(0u, 0u, 0u, 0u);
-            if (warp - 2 < min(jobs, teams)) next = fetch(warp - 2);
-            for (int j = warp - 2; j < jobs && warp - 2 < teams; j += teams) {
+            if (team < teams) next = fetch(team);
+            int s = team;
+            uint32_t ph = 1;                                     // (the first round of the ring does not wait)
+            for (int i = team; i < nu && team < teams; i += teams, s += teams) {
+                if (s >= p.stages) { s -= p.stages; ph ^= 1u; }
                 const uint4 cur = next;
-                if (j + teams < jobs) next = fetch(j + teams);
-                const int i = j / p.M, m = j % p.M, s = i % p.stages;
+                next = fetch(i + teams);
                 const uint32_t w[4] = {cur.x, cur.y, cur.z, cur.w};
                 float f[8];
                 float top = 0.f;
@@ -281,10 +296,8 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
                 const int src = BLOCK == 32 ? (lane & 16) : (lane & 24);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) word |= __shfl_sync(0xffffffffu, byte, src + b * (BLOCK / 8)) << (8 * b);
-                if (i >= p.stages) {
-                    ok = warp_all(mbar_wait(empty0 + 8 * s, (uint32_t)(i / p.stages - 1) & 1u));
-                    if (!ok) break;
-                }
+                ok = warp_all(mbar_wait(empty0 + 8 * s, ph));
+                if (!ok) break;
                 uint8_t *st = smem + (size_t)s * p.stage_bytes;
                 if (lane < 16 || 2 * (u0 + i) + 1 < p.halves) {
                     uint8_t *b = st + off_b + (lane >> 4) * digit_half(p.M) + m * kDigitSbo + (l16 >> 2) * kDigitLbo + (l16 & 3) * 4;
@@ -303,11 +316,13 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
     }
 
     // ---- epilogue: warps 2..5, a channel a lane -------------------------------------------------
-    __syncthreads();                     // row scales and row_top are there; roles are done
-    const bool hdr_ok = f4_header_matches(p.w, p.N, p.K, BLOCK) && (DIGITS || f4_header_matches(p.a, p.M, p.K, BLOCK));
+    __syncthreads();                     // row scales and the rest in shared memory are there; roles are done
+    cluster_wait();
+    const bool hdr_ok = bad_header == 0u;
     if (!hdr_ok && threadIdx.x == 64 && blockIdx.x == 0) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_BAD_PACKED);
     T *y = static_cast<T *>(p.y);
     float *part = reinterpret_cast<float *>(smem);               // [M][128], on the idle ring
+    const float *sums = reinterpret_cast<const float *>(smem + (size_t)p.stages * p.stage_bytes);
     if (warp >= 2 && warp < 6) {
         ok = warp_all(mbar_wait(accf, 0)) && ok;
         tcgen05_fence_after();
@@ -315,8 +330,11 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
         const uint32_t acc = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const bool put = ok && hdr_ok && n < p.N;
         const float wr = BLOCK == 16 ? w_row[ch] : 1.f;
+        const int to = ch / per;
+        const uint32_t to_sums = mapa_u32(smem_u32(sums), (uint32_t)to) + (uint32_t)((rank * p.M) * per + ch - to * per) * 4u, to_bar = mapa_u32(smem_u32(&sums_bar), (uint32_t)to);
         auto give = [&](int m, float v) {
-            if (p.split > 1) part[m * 128 + ch] = v;
+            if (push) store_cluster(to_sums + (uint32_t)(m * per) * 4u, v, to_bar);
+            else if (p.split > 1) part[m * 128 + ch] = v;
             else if (put) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * wr * (DIGITS ? 1.f : a_row[m]) : v);
         };
         if constexpr (DIGITS) {
@@ -343,15 +361,29 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
             }
         }
     }
-    if (p.split > 1) {
+    if (push) {
+        if (warp >= 2 && warp < 6) {
+            // (Every CTA sends its sums, whatever its own waits say, within their limit of a second each: waited for several times as
+            // long, so that no CTA is gone when sums for it arrive.)
+            bool all = false;
+            for (int i = 0; i < 8 && !all; ++i) all = warp_all(mbar_wait(smem_u32(&sums_bar), 0));
+            ok = ok && all;
+            for (int i = threadIdx.x - 64; i < p.M * own_n; i += 128) {
+                const int m = i / own_n, c = i - m * own_n, n = tile * 128 + own0 + c;
+                float v = 0.f;
+                for (int r = 0; r < p.split; ++r) v += sums[(r * p.M + m) * per + c];
+                if (ok && hdr_ok && n < p.N) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * w_row[own0 + c] * (DIGITS ? 1.f : a_row[m]) : v);
+            }
+        }
+    } else if (p.split > 1) {
+        __syncwarp();
         cluster_sync_all();
-        const int all = p.M * 128, per = (all + p.split - 1) / p.split, i1 = min(all, per * (rank + 1));
-        for (int i = per * rank + (int)threadIdx.x; i < i1; i += kStreamThreads) {
-            const int m = i >> 7, ch = i & 127, n = tile * 128 + ch;
+        for (int i = threadIdx.x; i < p.M * own_n; i += stream_threads(DIGITS)) {
+            const int m = i / own_n, ch = own0 + i - m * own_n, n = tile * 128 + ch;
             float v = 0.f;
             for (int r = 0; r < p.split; ++r) {
                 float o;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o) : "r"(mapa_u32(ring + 4u * (uint32_t)i, (uint32_t)r)) : "memory");
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o) : "r"(mapa_u32(ring + 4u * (uint32_t)(m * 128 + ch), (uint32_t)r)) : "memory");
                 v += o;
             }
             if (hdr_ok && n < p.N) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * w_row[ch] * (DIGITS ? 1.f : a_row[m]) : v);
@@ -368,11 +400,11 @@ __global__ void __launch_bounds__(kStreamThreads) f4_stream_kernel(const __grid_
     }
 }
 
-// Shares of k: as few as give most SMs a CTA.
-inline int stream_split(int tiles, int units)      // units of 256
+// Shares of k: as many as give every SM a CTA at most (4096 x 4096, one row: four shares 3.9 us, eight, two CTAs an SM, 5.6).
+inline int stream_split(int tiles, int units, int sms)      // units of 256
 {
     int s = 1;
-    while (s < kStreamMaxSplit && tiles * (s + 1) <= 148 && units >= s + 1) ++s;
+    while (s < kStreamMaxSplit && tiles * (s + 1) <= sms && units >= s + 1) ++s;
     return s;
 }
 
@@ -382,24 +414,26 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     auto kern = f4_stream_kernel<BLOCK, T, DIGITS>;
     static std::atomic<bool> raised[kMaxDevices];
     int dev = 0;
-    if (!device_info(&dev)) return TMAN_ERR_CUDA;
+    const DeviceInfo *info = device_info(&dev);
+    if (!info) return TMAN_ERR_CUDA;
     const int tiles = (p.N + kF4Tile - 1) / kF4Tile;
     p.cols = DIGITS ? (p.M + 1) / 2 * 16 : (p.M + 15) / 16 * 16;
     const int steps = (p.halves + 1) / 2;
-    p.split = stream_split(tiles, steps);
+    p.split = stream_split(tiles, steps, info->sms.load(std::memory_order_relaxed));
     p.stage_bytes = (kF4Tile * 128 + 4 * f4_scale_bytes(BLOCK) + stream_b_bytes<DIGITS>(p.M, p.cols) + 127) / 128 * 128;
-    // half an SM, so that the next call's CTAs fill their rings beside this one's; more where that holds few stages
-    const int budget = p.stage_bytes * 4 <= 110 * 1024 ? 110 * 1024 : 210 * 1024, least = p.M * 512;      // (the sums of a share lie on the ring)
-    p.stages = budget / p.stage_bytes;
+    // Half an SM's shared memory, so that the next call's CTAs fill their rings beside this one's; all of it where half holds few stages.
+    const int budget = p.stage_bytes * (DIGITS ? 3 : 4) <= kStreamHalfSm ? kStreamHalfSm : kStreamAllSm, least = p.M * 512;      // (the sums that others fetch lie on the ring)
+    const int sums = p.split > 1 && p.M <= kStreamPushRows ? (128 + 8) * p.M * 4 : 0;
+    p.stages = (budget - sums) / p.stage_bytes;
     if (p.stages > kStreamMaxStages) p.stages = kStreamMaxStages;
     const int share = (steps + p.split - 1) / p.split;
     if (p.stages > share) p.stages = share;
-    int bytes = p.stages * p.stage_bytes;
+    int bytes = p.stages * p.stage_bytes + sums;
     if (bytes < least) bytes = least;
     if ((long long)tiles * p.split > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * p.split));
-    cfg.blockDim = dim3(kStreamThreads);
+    cfg.blockDim = dim3((unsigned)stream_threads(DIGITS));
     cfg.dynamicSmemBytes = (size_t)bytes;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -411,7 +445,7 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = packed_write_pending(s, /*clear=*/true) ? 1 : 2;
-    return launch_with_smem(kern, 210 * 1024, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
+    return launch_with_smem(kern, kStreamAllSm, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
 }
 
 }  // namespace
