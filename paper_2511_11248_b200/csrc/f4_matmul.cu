@@ -25,7 +25,7 @@ static F4StreamParams stream_params(const void *packed, const void *a, const voi
 template <int BLOCK, typename T>
 static tman_status gemm_as(const void *packed, const void *a, void *y, int ldy, int M, int K, int N, void *ws, cudaStream_t s)
 {
-    if (M <= kStreamMaxRows) return launch_stream<BLOCK, T, false>(stream_params(packed, a, nullptr, 0, y, ldy, M, K, N, BLOCK, ws), s);
+    if (stream_wins(M, N)) return launch_stream<BLOCK, T, false>(stream_params(packed, a, nullptr, 0, y, ldy, M, K, N, BLOCK, ws), s);
     const F4Layout L = f4_layout(N, K, BLOCK), A = f4_layout(M, K, BLOCK);
     F4PairParams p = {};
     p.w = static_cast<const uint8_t *>(packed);

@@ -3,7 +3,9 @@
 #include "f4.cuh"
 #include "sm100_ptx.cuh"
 
+#include <mutex>
 #include <type_traits>
+#include <vector>
 
 namespace tman {
 
@@ -83,6 +85,29 @@ tman_status launch_f4_unpack(const void *packed, int rows, int K, int block, uin
 }
 
 // ---- quantization of rows ----------------------------------------------------------------------
+// The kernels let their successor start once their predecessor has ended, so that a product behind them fetches its weights meanwhile; what they
+// write is read only behind the successor's wait.  Unless it is the successor's weights: a product on the stream whose weights are the last
+// thing quantized there is launched in plain stream order.  (An earlier quantization has ended when a later one has let anything start.)
+struct F4Write { cudaStream_t stream; const void *packed; };
+static std::mutex g_f4_mutex;
+static std::vector<F4Write> g_f4_writes;         // the last one of each stream
+
+static void note_f4_write(cudaStream_t s, const void *packed)
+{
+    std::lock_guard<std::mutex> lock(g_f4_mutex);
+    for (F4Write &w : g_f4_writes)
+        if (w.stream == s) { w.packed = packed; return; }
+    g_f4_writes.push_back({s, packed});
+}
+
+bool f4_write_pending(cudaStream_t s, const void *packed)
+{
+    std::lock_guard<std::mutex> lock(g_f4_mutex);
+    for (F4Write &w : g_f4_writes)
+        if (w.stream == s && w.packed == packed) { w.packed = nullptr; return true; }
+    return false;
+}
+
 // One block's scale byte and the codes of eight of its values.  top: the largest magnitude of the block; fine: all its values are finite;
 // inv_row: 1 / r, a power of two.
 //   block 32: scale 2^e, e = floor(log2 top) - 2 (at least -127): x 2^-e is exact, one rounding.
@@ -166,6 +191,7 @@ template <int BLOCK, typename T, int V>
 __global__ void __launch_bounds__(32 * kRowsWarps) f4_quantize_kernel(const T *x, int ldx, int rows, int K, uint8_t *packed, const __grid_constant__ F4Layout L, int parts)
 {
     grid_wait();
+    grid_launch_next();                  // (see note_f4_write)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q = lane & 3;
     const int part = blockIdx.x % parts, g = blockIdx.x / parts, row = g * 8 + r;
     if (blockIdx.x == 0 && threadIdx.x < 64) reinterpret_cast<uint32_t *>(packed)[threadIdx.x] = f4_header_word(threadIdx.x, rows, K, BLOCK, L);
@@ -229,6 +255,7 @@ __global__ void __launch_bounds__(THREADS) f4_quantize16_kernel(const T *x, int 
     constexpr int WARPS = THREADS / 32;
     __shared__ uint32_t tops[WARPS];
     grid_wait();
+    grid_launch_next();                  // (see note_f4_write)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
     if (blockIdx.x == 0 && threadIdx.x < 64) reinterpret_cast<uint32_t *>(packed)[threadIdx.x] = f4_header_word(threadIdx.x, rows, K, 16, L);
     const uint4 *src = reinterpret_cast<const uint4 *>(x + (size_t)row * ldx) + threadIdx.x;
@@ -294,6 +321,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) f4_row_scales_kernel(const T 
 {
     __shared__ uint32_t tops[kRowsWarps];
     grid_wait();
+    grid_launch_next();                  // (see note_f4_write)
     const uint4 *src = reinterpret_cast<const uint4 *>(x + (size_t)blockIdx.x * ldx);
     uint32_t top = 0u;
     for (int i = threadIdx.x; i < K / 8; i += 32 * kRowsWarps) top = max(top, finite_top<T>(ld_dependent(src + i)));
@@ -358,6 +386,7 @@ static tman_status launch_quantize_as(const void *xv, int ldx, int rows, int K, 
 
 tman_status launch_f4_quantize(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, cudaStream_t s)
 {
+    note_f4_write(s, packed);
     if (dtype == kF4TypeHalf) return block == 32 ? launch_quantize_as<32, __half>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __half>(x, ldx, rows, K, packed, s);
     return block == 32 ? launch_quantize_as<32, __nv_bfloat16>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __nv_bfloat16>(x, ldx, rows, K, packed, s);
 }
@@ -369,6 +398,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) f4_dequant_kernel(const uint8
                                                                      uint32_t *status)
 {
     grid_wait();
+    grid_launch_next();                  // (see note_f4_write)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q = lane & 3;
     const int part = blockIdx.x % parts, g = blockIdx.x / parts, row = g * 8 + r, u = part * kRowsWarps + warp;      // unit
     const int chunks = min(8, L.halves * 4 - u * 8);

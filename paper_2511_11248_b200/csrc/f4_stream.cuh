@@ -26,9 +26,8 @@ namespace {
 
 constexpr int kDigitWarps = 16;
 __host__ __device__ constexpr int stream_threads(bool digits) { return digits ? 64 + 32 * kDigitWarps : 192; }      // warp 0: loads, 1: MMAs, others: digits, epilogue
-constexpr int kStreamMaxRows = 128;      // of a packed x
+constexpr int kStreamMaxRows = 64;       // of a packed x
 constexpr int kStreamMaxSplit = 8;
-constexpr int kStreamPushRows = 16;
 constexpr int kStreamHalfSm = 111 * 1024, kStreamAllSm = 220 * 1024;
 constexpr int kStreamMaxStages = 12;
 // Digits in shared memory: core matrices 16 bytes further apart than they are long, half units 64 bytes (mod 128), so that the stores of a warp
@@ -97,9 +96,8 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), accf = smem_u32(&acc_bar), ring = smem_u32(smem);
     const uint32_t off_sfa = kF4Tile * 128, off_b = off_sfa + 2 * SB, off_sfb = off_b + (uint32_t)b_bytes;
     const int tmem_cols = p.cols <= 64 ? 128 : 256;
-    // Sums of a tile's shares: of few rows every CTA sends its own to the CTA that adds up a channel, [share][row][own channel] behind its ring;
-    // of more rows the adding CTA fetches them.
-    const bool push = p.split > 1 && p.M <= kStreamPushRows;
+    // Sums of a tile's shares: every CTA sends its own to the CTA that adds up a channel, [share][row][own channel] behind its ring.
+    const bool push = p.split > 1;
     const int per = (128 + p.split - 1) / p.split, own0 = per * rank, own_n = min(per, 128 - own0);      // channels added up here
     bool ok = true;
 
@@ -321,7 +319,6 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     const bool hdr_ok = bad_header == 0u;
     if (!hdr_ok && threadIdx.x == 64 && blockIdx.x == 0) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_BAD_PACKED);
     T *y = static_cast<T *>(p.y);
-    float *part = reinterpret_cast<float *>(smem);               // [M][128], on the idle ring
     const float *sums = reinterpret_cast<const float *>(smem + (size_t)p.stages * p.stage_bytes);
     if (warp >= 2 && warp < 6) {
         ok = warp_all(mbar_wait(accf, 0)) && ok;
@@ -334,7 +331,6 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
         const uint32_t to_sums = mapa_u32(smem_u32(sums), (uint32_t)to) + (uint32_t)((rank * p.M) * per + ch - to * per) * 4u, to_bar = mapa_u32(smem_u32(&sums_bar), (uint32_t)to);
         auto give = [&](int m, float v) {
             if (push) store_cluster(to_sums + (uint32_t)(m * per) * 4u, v, to_bar);
-            else if (p.split > 1) part[m * 128 + ch] = v;
             else if (put) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * wr * (DIGITS ? 1.f : a_row[m]) : v);
         };
         if constexpr (DIGITS) {
@@ -351,18 +347,18 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
             }
         } else {
 #pragma unroll 1
-            for (int m = 0; m < p.M; m += 8) {
-                uint32_t r[8];
-                tcgen05_ld_32x32b_x8(acc + m, r);
+            for (int m = 0; m < p.M; m += 16) {
+                uint32_t r[16];
+                tcgen05_ld_32x32b_x16(acc + m, r);
                 tcgen05_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
+                for (int e = 0; e < 16; ++e)
                     if (m + e < p.M) give(m + e, __uint_as_float(r[e]));
             }
         }
     }
-    if (push) {
-        if (warp >= 2 && warp < 6) {
+    if (push && warp >= 2 && warp < 6) {
+        {
             // (Every CTA sends its sums, whatever its own waits say, within their limit of a second each: waited for several times as
             // long, so that no CTA is gone when sums for it arrive.)
             bool all = false;
@@ -375,21 +371,6 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                 if (ok && hdr_ok && n < p.N) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * w_row[own0 + c] * (DIGITS ? 1.f : a_row[m]) : v);
             }
         }
-    } else if (p.split > 1) {
-        __syncwarp();
-        cluster_sync_all();
-        for (int i = threadIdx.x; i < p.M * own_n; i += stream_threads(DIGITS)) {
-            const int m = i / own_n, ch = own0 + i - m * own_n, n = tile * 128 + ch;
-            float v = 0.f;
-            for (int r = 0; r < p.split; ++r) {
-                float o;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o) : "r"(mapa_u32(ring + 4u * (uint32_t)(m * 128 + ch), (uint32_t)r)) : "memory");
-                v += o;
-            }
-            if (hdr_ok && n < p.N) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * w_row[ch] * (DIGITS ? 1.f : a_row[m]) : v);
-        }
-        __syncwarp();
-        cluster_sync_all();              // nobody leaves while others read its sums
     }
     if (!ok) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_TIMEOUT);
     tcgen05_fence_before();
@@ -408,6 +389,14 @@ inline int stream_split(int tiles, int units, int sms)      // units of 256
     return s;
 }
 
+// Whether a packed x of M rows goes here rather than to pairs of CTAs with a tile each (32-value blocks, us, here / there):
+//   K x N           4096 x 14336               14336 x 4096                   4096 x 1024                4096 x 28672
+//   M = 16          6.4 / 8.1                  6.6 / 18.4                     3.2 / 7.2                  11.3 / 13.8
+//   M = 48          8.2 / 8.2                  9.4 / 18.6                     4.9 / 7.3                  13.8 / 14.1
+//   M = 64          9.2 / 8.3                  11.5 / 18.7                    5.8 / 7.3                  14.8 / 14.1
+//   M = 96          11.9 / 8.7                 17.2 / 18.8                    10.2 / 7.3                 24.9 / 14.4
+inline bool stream_wins(int M, int N) { return M <= 48 || (M <= kStreamMaxRows && (N + kF4Tile - 1) / kF4Tile <= 74); }
+
 template <int BLOCK, typename T, bool DIGITS>
 tman_status launch_stream(F4StreamParams p, cudaStream_t s)
 {
@@ -422,14 +411,13 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     p.split = stream_split(tiles, steps, info->sms.load(std::memory_order_relaxed));
     p.stage_bytes = (kF4Tile * 128 + 4 * f4_scale_bytes(BLOCK) + stream_b_bytes<DIGITS>(p.M, p.cols) + 127) / 128 * 128;
     // Half an SM's shared memory, so that the next call's CTAs fill their rings beside this one's; all of it where half holds few stages.
-    const int budget = p.stage_bytes * (DIGITS ? 3 : 4) <= kStreamHalfSm ? kStreamHalfSm : kStreamAllSm, least = p.M * 512;      // (the sums that others fetch lie on the ring)
-    const int sums = p.split > 1 && p.M <= kStreamPushRows ? (128 + 8) * p.M * 4 : 0;
+    const int budget = p.stage_bytes * (DIGITS ? 3 : 4) <= kStreamHalfSm ? kStreamHalfSm : kStreamAllSm;
+    const int sums = p.split > 1 ? (128 + 8) * p.M * 4 : 0;
     p.stages = (budget - sums) / p.stage_bytes;
     if (p.stages > kStreamMaxStages) p.stages = kStreamMaxStages;
     const int share = (steps + p.split - 1) / p.split;
     if (p.stages > share) p.stages = share;
-    int bytes = p.stages * p.stage_bytes + sums;
-    if (bytes < least) bytes = least;
+    const int bytes = p.stages * p.stage_bytes + sums;
     if ((long long)tiles * p.split > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * p.split));
@@ -444,7 +432,7 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = packed_write_pending(s, /*clear=*/true) ? 1 : 2;
+    cfg.numAttrs = packed_write_pending(s, /*clear=*/true) || f4_write_pending(s, p.w) ? 1 : 2;
     return launch_with_smem(kern, kStreamAllSm, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
 }
 
