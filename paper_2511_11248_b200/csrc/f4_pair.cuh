@@ -14,6 +14,8 @@
 #include "f4.cuh"
 #include "sm100_ptx.cuh"
 
+#include <type_traits>
+
 namespace tman {
 namespace {
 
@@ -22,6 +24,7 @@ constexpr int kPairCols = 256;           // most rows of a in a tile
 constexpr int kPairAcc1 = 192, kPairSf = 448;
 constexpr int kPairStages = 6;
 constexpr int kPairSmem = 222 * 1024;
+constexpr double kPairSharesUs = 2.0;     // of sending and adding up the shares' sums, beside 0.004 a row
 constexpr size_t kPairStreamBytes = (size_t)64 << 20;
 
 struct F4PairParams {
@@ -29,7 +32,8 @@ struct F4PairParams {
     void *y;
     uint32_t *status;
     size_t w_codes, w_scales, w_rows, a_codes, a_scales, a_rows;
-    int M, K, N, ldy, halves, w_h8, a_h8, nt, tiles_m, tiles_n, rows_fastest, stream_y, stages;
+    int M, K, N, ldy, halves, w_h8, a_h8, nt, tiles_m, tiles_n, rows_fastest, stream_y, stages, split_sh;
+    uint32_t tile_mul;                   // 2^32 / (the tiles that are numbered first), rounded up; 0: one, or too many tiles for it
 };
 
 template <int BLOCK> struct PairStage {
@@ -38,22 +42,25 @@ template <int BLOCK> struct PairStage {
 };
 
 template <int BLOCK, typename T>
-__global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pair_kernel(const __grid_constant__ F4PairParams p)
+__global__ void __launch_bounds__(kPairThreads) f4_pair_kernel(const __grid_constant__ F4PairParams p)
 {
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t full_bar[kPairStages], empty_bar[kPairStages], accf_bar[2], acce_bar[2], shared_bar;
+    __shared__ __align__(8) uint64_t full_bar[kPairStages], empty_bar[kPairStages], accf_bar[2], acce_bar[2], shared_bar, sums_bar;
     __shared__ uint32_t tmem_slot;
     using St = PairStage<BLOCK>;
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (the shuffle tells the compiler that it is uniform)
-    const uint32_t rank = cluster_ctarank();
-    const int worker = blockIdx.x >> 1, workers = gridDim.x >> 1, tiles = p.tiles_m * p.tiles_n;
+    // a cluster: the pairs with the shares of k of a tile, one tile each (split > 1), or one pair that walks over tiles
+    const uint32_t crank = cluster_ctarank(), rank = crank & 1u, share = crank >> 1;
+    const int worker = blockIdx.x >> (1 + p.split_sh), workers = gridDim.x >> (1 + p.split_sh), tiles = p.tiles_m * p.tiles_n, split = 1 << p.split_sh;
     const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), accf0 = smem_u32(accf_bar), acce0 = smem_u32(acce_bar),
                    shared0 = smem_u32(&shared_bar), ring = smem_u32(smem);
-    const int steps = (p.halves + 1) >> 1;
+    const int all_steps = (p.halves + 1) >> 1, step0 = all_steps * (int)share >> p.split_sh, steps = (all_steps * (int)(share + 1) >> p.split_sh) - step0;
     const bool overlap = p.nt > kPairAcc1;                       // the two accumulators share columns
-    // a tile's place among the rows and the channels
-    auto tile_m = [&](int tile) { return p.rows_fastest ? tile % p.tiles_m : tile / p.tiles_n; };
-    auto tile_n = [&](int tile) { return p.rows_fastest ? tile / p.tiles_m : tile % p.tiles_n; };
+    // a tile's place among the rows and the channels (a division by a variable costs the first loads of a call a sixth of a microsecond)
+    const int inner = p.rows_fastest ? p.tiles_m : p.tiles_n;
+    auto outer_of = [&](int tile) { return p.tile_mul ? (int)__umulhi((uint32_t)tile, p.tile_mul) : inner == 1 ? tile : tile / inner; };
+    auto tile_m = [&](int tile) { const int o = outer_of(tile); return p.rows_fastest ? tile - o * inner : o; };
+    auto tile_n = [&](int tile) { const int o = outer_of(tile); return p.rows_fastest ? o : tile - o * inner; };
     bool ok = true;
 
     if (threadIdx.x == 0) {
@@ -66,6 +73,8 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
             mbar_init(acce0 + 8 * b, 16);
         }
         mbar_init(shared0, 8);
+        mbar_init(smem_u32(&sums_bar), 1);
+        if (split > 1) mbar_expect_tx(smem_u32(&sums_bar), (uint32_t)p.nt * 512u);
         fence_barrier_init();
     }
     __syncthreads();
@@ -95,7 +104,8 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
     const size_t w_step = (size_t)p.w_h8 * 128, a_step = (size_t)p.a_h8 * 128, ws_step = (size_t)((p.w_h8 + kF4Tile - 1) / kF4Tile) * (2 * St::SB),
                  as_step = (size_t)((p.a_h8 + kF4Tile - 1) / kF4Tile) * (2 * St::SB);
     // A half unit's sections are half as wide: rows (tiles) lie half as far from the section's start.
-    auto load = [&](bool lead, const Loads &l, int step, int s, bool do_w, bool do_a) {
+    auto load = [&](bool lead, const Loads &l, int i, int s, bool do_w, bool do_a) {
+        const int step = step0 + i;
         const uint32_t sh = 2 * step + 1 < p.halves ? 0u : 1u;
         const uint32_t st = ring + (uint32_t)s * St::kBytes, bar = full0 + 8 * s;
         const uint8_t *w = p.w + p.w_codes + step * w_step + ((size_t)(l.w - (p.w + p.w_codes)) >> sh);
@@ -139,6 +149,13 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
     tcgen05_fence_after();
     grid_launch_next();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
+    bool hdr_ok = true;
+    if (warp >= 2) {
+        hdr_ok = f4_header_matches(p.w, p.N, p.K, BLOCK) && f4_header_matches(p.a, p.M, p.K, BLOCK);
+        if (!hdr_ok && threadIdx.x == 64 && blockIdx.x == 0) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_BAD_PACKED);
+    }
+    const float *a_row = reinterpret_cast<const float *>(p.a + p.a_rows), *w_row = reinterpret_cast<const float *>(p.w + p.w_rows);
+    const bool pairs_ok = (p.N & 1) == 0 && (p.ldy & 1) == 0 && (reinterpret_cast<uintptr_t>(p.y) & 3) == 0;
 
     if (warp == 0) {
         const bool lead = elect_one();
@@ -154,7 +171,7 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
         }
     } else if (warp == 1 && rank != 0) {                         // tells the first CTA when this one's part of a stage is there
         const bool lead = elect_one();
-        const uint32_t to = mapa_u32(full0, 0);
+        const uint32_t to = mapa_u32(full0, crank & ~1u);
         int s = 0;
         uint32_t ph = 0;
         for (int i = 0; i < total; ++i) {
@@ -167,6 +184,7 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
         const bool lead = elect_one();
         const uint32_t id0 = f4_idesc(BLOCK, 256, p.nt, 0), id1 = f4_idesc(BLOCK, 256, p.nt, BLOCK == 32 ? 2 : 0);
         const uint64_t sf0 = make_kmajor_desc(ring, 128, 128);                     // (+ 1: 16 bytes)
+        const uint16_t both = (uint16_t)(3u << crank);
         int s = 0;
         uint32_t ph = 0, ti = 0;
         for (int tile = worker; ok && tile < tiles; tile += workers, ++ti) {
@@ -176,7 +194,7 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
             const uint32_t g0 = (uint32_t)(tile_m(tile) * p.nt) / 32 % 4;
             const bool two = g0 + (uint32_t)p.nt / 32 > 4;           // pieces of scales of a
             for (int step = 0; step < steps; ++step) {
-                const uint32_t at = (uint32_t)s * (St::kBytes >> 4), nu = 2 * step + 1 < p.halves ? 2u : 1u;
+                const uint32_t at = (uint32_t)s * (St::kBytes >> 4), nu = 2 * (step0 + step) + 1 < p.halves ? 2u : 1u;
                 const uint64_t op = make_kmajor_desc(ring, 128, nu * 512) + at, sf = sf0 + at;
                 if (!warp_all(mbar_wait(full0 + 8 * s, ph))) { ok = false; break; }
                 tcgen05_fence_after();
@@ -195,30 +213,28 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
                             tcgen05_mma2_f4<BLOCK>(acc, wa, xb, id0, sfa, sfb + g0, (step | (int)u) != 0);
                             tcgen05_mma2_f4<BLOCK>(acc, wa + 16, xb + 16, id1, sfa + (BLOCK == 32 ? 0 : 4), sfb + g0 + (BLOCK == 32 ? 0 : 8), 1);
                         }
-                    tcgen05_commit2_both(empty0 + 8 * s);
+                    tcgen05_commit2(empty0 + 8 * s, both);
                 }
                 __syncwarp();
                 if (++s == p.stages) { s = 0; ph ^= 1u; }
             }
-            if (lead) tcgen05_commit2_both(accf0 + 8 * b);
+            if (lead) tcgen05_commit2(accf0 + 8 * b, both);
             __syncwarp();
         }
-    } else {
+    } else if (split == 1) {
         // ---- epilogue: a warp has 32 channels (a lane each) x half of the tile's rows of a, 32 at a time; neighbouring lanes exchange every
         // other row, so that a lane stores two adjacent channels of one row
-        const bool hdr_ok = f4_header_matches(p.w, p.N, p.K, BLOCK) && f4_header_matches(p.a, p.M, p.K, BLOCK);
-        if (!hdr_ok && threadIdx.x == 64 && blockIdx.x == 0) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_BAD_PACKED);
         const int quad = warp & 3, half = p.nt >> 1;
         const bool second = warp >= 6, odd = (lane & 1) != 0;
-        const bool pairs_ok = (p.N & 1) == 0 && (p.ldy & 1) == 0 && (reinterpret_cast<uintptr_t>(p.y) & 3) == 0;
-        const uint32_t acce_lead = mapa_u32(acce0, 0), shared_lead = mapa_u32(shared0, 0);
-        const float *a_row = reinterpret_cast<const float *>(p.a + p.a_rows), *w_row = reinterpret_cast<const float *>(p.w + p.w_rows);
+        const uint32_t acce_lead = mapa_u32(acce0, crank & ~1u), shared_lead = mapa_u32(shared0, crank & ~1u);
+        const uint64_t y_policy = p.stream_y ? policy_evict_first() : policy_evict_normal();
         uint32_t ti = 0;
         for (int tile = worker; tile < tiles; tile += workers, ++ti) {
             const uint32_t b = ti & 1u;
             const int m0 = tile_m(tile) * p.nt, n = tile_n(tile) * 256 + (int)rank * 128 + quad * 32 + lane, n2 = n & ~1;
             const int end = p.M - m0, t0 = second ? half : 0;
-            const bool put = hdr_ok && n2 < p.N, put1 = n2 + 1 < p.N;
+            const bool put = hdr_ok && n2 < p.N, put1 = n2 + 1 < p.N, whole = warp_all(put && put1 && pairs_ok);
+            const size_t row2 = 2 * (size_t)p.ldy;
             float w0 = 1.f, w1 = 1.f;
             if constexpr (BLOCK == 16) {
                 w0 = w_row[min(n2, p.N - 1)];
@@ -226,8 +242,11 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
             }
             T *y = static_cast<T *>(p.y) + (size_t)(m0 + (odd ? 1 : 0)) * p.ldy + n2;
             const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + b * kPairAcc1;
-            auto store32 = [&](int t, const uint32_t (&r)[32]) {
-                float ar = 1.f;
+            // WHOLE: 32 rows of pairs of channels; else what there is of them.  (One place in the code each: a call that does one tile a pair
+            // meets it with a cold instruction cache, 256 x 4096 x 14336 11.7 us with nine copies.)
+            auto store32 = [&](auto whole_c, int t, const uint32_t (&r)[32]) {
+                constexpr bool WHOLE = decltype(whole_c)::value;
+                [[maybe_unused]] float ar = 1.f;
                 if constexpr (BLOCK == 16) ar = ld_dependent(a_row + min(m0 + t + lane, p.M - 1));
                 T *yt = y + (size_t)t * p.ldy;
 #pragma unroll
@@ -239,47 +258,95 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
                         c0 *= w0 * f;
                         c1 *= w1 * f;
                     }
-                    if (t + e + (odd ? 1 : 0) < end && put) {
-                        if (pairs_ok && p.stream_y) __stcs(reinterpret_cast<uint32_t *>(yt), f4_from_float2<T>(c0, c1));
-                        else if (pairs_ok) *reinterpret_cast<uint32_t *>(yt) = f4_from_float2<T>(c0, c1);
-                        else {
-                            yt[0] = f4_from_float<T>(c0);
-                            if (put1) yt[1] = f4_from_float<T>(c1);
-                        }
+                    if constexpr (WHOLE) st_policy(yt, f4_from_float2<T>(c0, c1), y_policy);
+                    else if (t + e + (odd ? 1 : 0) < end && put) {
+                        yt[0] = f4_from_float<T>(c0);
+                        if (put1) yt[1] = f4_from_float<T>(c1);
                     }
-                    yt += 2 * (size_t)p.ldy;
+                    yt += row2;
                 }
             };
             ok = warp_all(mbar_wait(accf0 + 8 * b, (ti >> 1) & 1u));
             if (!ok) break;
             tcgen05_fence_after();
-            int done0 = t0, done1 = t0;                          // columns taken before the others
-            if (overlap && second == (b == 0)) {
-                // the columns that the next tile's accumulator has too: all in registers, then that tile may start
-                const int t = second ? kPairAcc1 : 0;
-                uint32_t r0[32], r1[32];
-                tcgen05_ld_32x32b_x32(acc + (uint32_t)t, r0);
-                tcgen05_ld_32x32b_x32(acc + (uint32_t)t + 32u, r1);
-                tcgen05_wait_ld();
-                tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(shared_lead);
-                if (t < end) store32(t, r0);
-                if (t + 32 < end) store32(t + 32, r1);
-                done0 = t;
-                done1 = t + 64;
-            }
+            // The columns that the next tile's accumulator has too come first: when all of them are in registers, that tile may start.
+            const bool first = overlap && second == (b == 0);
+            const int groups = half >> 5, g0 = first && second ? 2 : 0;      // (of 32 columns; the second warps' shared ones are their last two)
+            uint32_t r[32], next[32];
 #pragma unroll 1
-            for (int t = t0; t < t0 + half && t < end; t += 32) {
-                if (t >= done0 && t < done1) continue;
-                uint32_t r[32];
-                tcgen05_ld_32x32b_x32(acc + (uint32_t)t, r);
-                tcgen05_wait_ld();
-                store32(t, r);
+            for (int g = 0; g < groups; ++g) {
+                const int t = t0 + 32 * ((g + g0) % groups);
+                if (t >= end && !first) continue;
+                if (first && g == 1) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) r[e] = next[e];
+                } else {
+                    tcgen05_ld_32x32b_x32(acc + (uint32_t)t, r);
+                    if (first && g == 0) tcgen05_ld_32x32b_x32(acc + (uint32_t)t + 32u, next);
+                    tcgen05_wait_ld();
+                }
+                if (first && g == 0) {
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(shared_lead);
+                }
+                if (whole && t + 32 <= end) store32(std::true_type(), t, r);
+                else if (t < end) store32(std::false_type(), t, r);
             }
             tcgen05_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(acce_lead + 8 * b);
+        }
+    }
+    if (split > 1) {
+        // ---- shares of a tile: column c of the tile is added up by share c / own in the CTA of the same channels; everyone sends it its sums,
+        // [share][own column][channel] on the ring, which is idle everywhere once all accumulators are complete
+        if (warp >= 2) {
+            ok = warp_all(mbar_wait(accf0, 0)) && ok;
+            tcgen05_fence_after();
+        }
+        __syncwarp();
+        cluster_sync_all();
+        const int own = p.nt >> p.split_sh, m0 = tile_m(worker) * p.nt + (int)share * own, n0 = tile_n(worker) * 256 + (int)rank * 128;
+        if (warp >= 2) {
+            const int quad = warp & 3, half = p.nt >> 1, t0 = warp >= 6 ? half : 0;
+#pragma unroll 1
+            for (int t = t0; t < t0 + half; t += 16) {           // (16 columns are of one share: nt is a multiple of 64, split 2 or 4)
+                uint32_t r[16];
+                tcgen05_ld_32x32b_x16(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)t, r);
+                const int to = t / own;
+                const uint32_t cta = (uint32_t)to * 2u + rank, bar = mapa_u32(smem_u32(&sums_bar), cta),
+                               dst = mapa_u32(ring, cta) + (uint32_t)((((int)share * own + t - to * own) * 128 + quad * 32 + lane) * 4);
+                tcgen05_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) store_cluster(dst + 512u * e, __uint_as_float(r[e]), bar);
+            }
+            bool all = false;
+            for (int i = 0; i < 8 && !all; ++i) all = warp_all(mbar_wait(smem_u32(&sums_bar), 0));
+            ok = ok && all;
+            const float *sums = reinterpret_cast<const float *>(smem);
+            for (int i = threadIdx.x - 64; i < own * 64; i += kPairThreads - 64) {
+                const int c = i >> 6, ch = (i & 63) * 2, m = m0 + c, n = n0 + ch;
+                float v0 = 0.f, v1 = 0.f;
+                for (int r = 0; r < split; ++r) {
+                    const float2 v = *reinterpret_cast<const float2 *>(sums + (r * own + c) * 128 + ch);
+                    v0 += v.x;
+                    v1 += v.y;
+                }
+                if (ok && hdr_ok && m < p.M && n < p.N) {
+                    if constexpr (BLOCK == 16) {
+                        const float f = ld_dependent(a_row + m);
+                        v0 *= f * w_row[n];
+                        v1 *= f * w_row[min(n + 1, p.N - 1)];
+                    }
+                    T *y = static_cast<T *>(p.y) + (size_t)m * p.ldy + n;
+                    if (pairs_ok) *reinterpret_cast<uint32_t *>(y) = f4_from_float2<T>(v0, v1);
+                    else {
+                        y[0] = f4_from_float<T>(v0);
+                        if (n + 1 < p.N) y[1] = f4_from_float<T>(v1);
+                    }
+                }
+            }
         }
     }
     if (!ok) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_TIMEOUT);
@@ -292,19 +359,48 @@ __global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1) f4_pai
     }
 }
 
-// Rows of a in a tile: the multiple of 64 with the least modelled time, rounds of tiles x (units x time of a unit + a tile's own time).  The
-// loads, about 57 bytes a clock and SM, bound a unit, so that it takes 0.28 us with 128 rows and 0.33 with 256 (32-value blocks; 2048 x 3584 x
-// 18944 with 128 / 192 / 256 rows a tile: 79.7 / 61.8 / 53.2 us, 8192 x 18944 x 3584: 282 / 213 / 183).
-inline int pair_rows(int M, int steps, int tiles_n, int workers)
+// Rows of a in a tile, a multiple of 64, and shares of k of a tile: what has the least modelled time.  The loads, about 57 bytes a clock and SM,
+// bound a unit, so that it takes 0.28 us with 128 rows and 0.33 with 256 (32-value blocks; 2048 x 3584 x 18944 with 128 / 192 / 256 rows a
+// tile: 79.7 / 61.8 / 53.2 us, 8192 x 18944 x 3584: 282 / 213 / 183).  Whole tiles go round the pairs; shares are for few tiles, one a
+// cluster of pairs.
+struct PairPlan { int nt, split; };
+inline PairPlan pair_plan(int M, int steps, int tiles_n, int workers, const int (&clusters)[2])      // clusters of two and of four pairs held at once
 {
-    int best = 64;
+    PairPlan best = {64, 1};
     double least = 1e300;
     for (int nt = 64; nt <= kPairCols; nt += 64) {
         const long long tiles = (long long)((M + nt - 1) / nt) * tiles_n, rounds = (tiles + workers - 1) / workers;
-        const double us = (double)rounds * (steps * (0.245 + 0.00032 * nt) + 0.1 + 0.0075 * nt);
-        if (us < least - 1e-9) { least = us; best = nt; }
+        const double unit = 0.245 + 0.00032 * nt, tile = 0.1 + 0.0075 * nt;
+        for (int split = 1; split <= 4; split *= 2) {
+            if (split > 1 && (tiles > clusters[split >> 2] || steps < 2 * split)) continue;
+            const double us = split == 1 ? (double)rounds * (steps * unit + tile) : (steps + split - 1) / split * unit + tile + kPairSharesUs + 0.004 * nt;
+            if (us < least - 1e-9) { least = us; best = {nt, split}; }
+        }
     }
     return best;
+}
+
+// Clusters of `ctas` CTAs of the kernel that the current device holds at once (0: none, or the query failed).
+template <typename Kernel> inline int pair_clusters(Kernel kern, int ctas)
+{
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)ctas;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas * 64);
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = kPairSmem;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    return n;
 }
 
 template <int BLOCK, typename T>
@@ -317,7 +413,16 @@ tman_status launch_pair(F4PairParams p, cudaStream_t s)
     if (!info) return TMAN_ERR_CUDA;
     const int workers = info->sms.load(std::memory_order_relaxed) / 2;
     p.tiles_n = (p.N + 255) / 256;
-    p.nt = pair_rows(p.M, (p.halves + 1) / 2, p.tiles_n, workers);
+    static std::atomic<int> held[kMaxDevices][2];                // + 1 (0: not asked yet)
+    int clusters[2];
+    for (int i = 0; i < 2; ++i) {
+        int n = held[dev][i].load(std::memory_order_relaxed);
+        if (n == 0) held[dev][i].store(n = pair_clusters(kern, 4 << i) + 1, std::memory_order_relaxed);
+        clusters[i] = n - 1;
+    }
+    const PairPlan plan = pair_plan(p.M, (p.halves + 1) / 2, p.tiles_n, workers, clusters);
+    p.nt = plan.nt;
+    p.split_sh = plan.split >> 1;        // 0, 1, 2
     p.tiles_m = (p.M + p.nt - 1) / p.nt;
     const long long tiles = (long long)p.tiles_m * p.tiles_n;
     if (tiles > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
@@ -327,20 +432,26 @@ tman_status launch_pair(F4PairParams p, cudaStream_t s)
     const auto bytes = [&](long long tm, long long tn) { return (double)tm * p.nt + (double)tn * 256; };
     const auto up = [](long long a, long long b) { return (a + b - 1) / b; };
     p.rows_fastest = bytes(p.tiles_m < round ? p.tiles_m : round, up(round, p.tiles_m)) < bytes(up(round, p.tiles_n), p.tiles_n < round ? p.tiles_n : round);
+    const uint32_t inner = (uint32_t)(p.rows_fastest ? p.tiles_m : p.tiles_n);
+    p.tile_mul = inner > 1 && tiles < 65536 ? 0xFFFFFFFFu / inner + 1u : 0u;
     // An output that does not fit L2 beside the operands leaves it early (8192 x 4096 x 14336 184 -> 172 us; 4096 x 14336 x 4096 would go 97 -> 105).
     p.stream_y = (size_t)p.M * p.N * 2 > kPairStreamBytes ? 1 : 0;
     p.stages = kPairSmem / (int)PairStage<BLOCK>::kBytes;
     if (p.stages > kPairStages) p.stages = kPairStages;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * (tiles < workers ? tiles : workers)));
+    cfg.gridDim = dim3((unsigned)((2 << p.split_sh) * (tiles < workers ? tiles : workers)));
     cfg.blockDim = dim3(kPairThreads);
     cfg.dynamicSmemBytes = (size_t)p.stages * PairStage<BLOCK>::kBytes;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (2u << p.split_sh);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = packed_write_pending(s, /*clear=*/true) || f4_write_pending(s, p.w) ? 0 : 1;
+    cfg.numAttrs = packed_write_pending(s, /*clear=*/true) || f4_write_pending(s, p.w) ? 1 : 2;
     return launch_with_smem(kern, kPairSmem, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
 }
 

@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     constexpr uint32_t SB = f4_scale_bytes(BLOCK), CHUNKS = SB / 512;
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;      // (the shuffle tells the compiler that it is uniform)
     const int rank = blockIdx.x % p.split, tile = blockIdx.x / p.split, steps = (p.halves + 1) >> 1;
-    const int u0 = (int)((long long)steps * rank / p.split), nu = (int)((long long)steps * (rank + 1) / p.split) - u0;     // units of this share
+    const int u0 = steps * rank / p.split, nu = steps * (rank + 1) / p.split - u0;     // units of this share
     const int b_bytes = stream_b_bytes<DIGITS>(p.M, p.cols);
     const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), accf = smem_u32(&acc_bar), ring = smem_u32(smem);
     const uint32_t off_sfa = kF4Tile * 128, off_b = off_sfa + 2 * SB, off_sfb = off_b + (uint32_t)b_bytes;
@@ -431,6 +431,7 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
+    // (also a cluster of one: without the attribute the next call's CTAs do not spread over the SMs, 1 x 3584 x 18944 7.1 -> 8.9 us)
     cfg.attrs = attr;
     cfg.numAttrs = packed_write_pending(s, /*clear=*/true) || f4_write_pending(s, p.w) ? 1 : 2;
     return launch_with_smem(kern, kStreamAllSm, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });

@@ -127,6 +127,12 @@ __device__ __forceinline__ void tcgen05_commit2_both(uint32_t bar)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
+// (the pair's CTAs in a larger cluster: bits of the ranks)
+__device__ __forceinline__ void tcgen05_commit2(uint32_t bar, uint16_t ctas)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"(ctas) : "memory");
+}
 __device__ __forceinline__ void tcgen05_mma2_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
@@ -325,6 +331,24 @@ __device__ __forceinline__ void tcgen05_mma2_f4(uint32_t d_tmem, uint64_t adesc,
 __host__ __device__ constexpr uint32_t f4_idesc(int block, int rows, int cols, int id)
 {
     return (uint32_t)id << 4 | 1u << 7 | 1u << 10 | (uint32_t)(cols >> 3) << 17 | (block == 32 ? 1u << 23 : 0u) | (uint32_t)(rows >> 4) << 24 | (uint32_t)id << 29;
+}
+
+// Stores with a say about how long L2 keeps them.
+__device__ __forceinline__ uint64_t policy_evict_first()
+{
+    uint64_t v;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(v));
+    return v;
+}
+__device__ __forceinline__ uint64_t policy_evict_normal()
+{
+    uint64_t v;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(v));
+    return v;
+}
+__device__ __forceinline__ void st_policy(void *at, uint32_t v, uint64_t policy)
+{
+    asm volatile("st.global.L2::cache_hint.u32 [%0], %1, %2;" ::"l"(at), "r"(v), "l"(policy) : "memory");
 }
 
 // Programmatic dependent launch: behind grid_wait() everything that the kernels before this one in the stream wrote is there; after

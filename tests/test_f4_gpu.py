@@ -277,3 +277,10 @@ def test_headers_that_do_not_match_leave_the_output():
     B.tman_unpack_f4(other, N, K, block, c, s, None, ws)
     assert B.tman_read_status(ws) == 5
     assert bool((y == 3.0).all()) and bool((out == 3.0).all()) and bool((c == 9).all()) and bool((s == 9).all())
+
+
+# few tiles and a long reduction: shares of k of a tile on a cluster of pairs of CTAs
+@pytest.mark.parametrize("block", [32, 16])
+@pytest.mark.parametrize("M,K,N", [(65, 4096, 256), (100, 2048, 1000), (129, 8256, 300), (250, 14336, 513), (600, 5152, 96), (1030, 2080, 250)])
+def test_gemm_of_few_tiles(M, K, N, block):
+    test_gemm(M, K, N, block, "bf16")
