@@ -441,7 +441,7 @@ tman_status launch_pair(F4PairParams p, cudaStream_t s)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((2 << p.split_sh) * (tiles < workers ? tiles : workers)));
     cfg.blockDim = dim3(kPairThreads);
-    cfg.dynamicSmemBytes = (size_t)p.stages * PairStage<BLOCK>::kBytes;
+    cfg.dynamicSmemBytes = kPairSmem;    // (all of it: no CTA that needs tensor memory beside one of these, which hold all of that)
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -28,7 +28,7 @@ constexpr int kDigitWarps = 16;
 __host__ __device__ constexpr int stream_threads(bool digits) { return digits ? 64 + 32 * kDigitWarps : 192; }      // warp 0: loads, 1: MMAs, others: digits, epilogue
 constexpr int kStreamMaxRows = 64;       // of a packed x
 constexpr int kStreamMaxSplit = 8;
-constexpr int kStreamHalfSm = 111 * 1024, kStreamAllSm = 220 * 1024;
+constexpr int kStreamHalfSm = 111 * 1024, kStreamAllSm = 220 * 1024, kStreamLeastSmem = 57 * 1024;
 constexpr int kStreamMaxStages = 12;
 // Digits in shared memory: core matrices 16 bytes further apart than they are long, half units 64 bytes (mod 128), so that the stores of a warp
 // (four bytes of 32 places along k) meet no bank twice.  Of an odd M the tile's last eight columns are whatever lies behind.
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     const int b_bytes = stream_b_bytes<DIGITS>(p.M, p.cols);
     const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), accf = smem_u32(&acc_bar), ring = smem_u32(smem);
     const uint32_t off_sfa = kF4Tile * 128, off_b = off_sfa + 2 * SB, off_sfb = off_b + (uint32_t)b_bytes;
-    const int tmem_cols = p.cols <= 64 ? 128 : 256;
+    constexpr uint32_t tmem_cols = 128;      // up to 64 of sums, two sets of scales (16 each) behind them
     // Sums of a tile's shares: every CTA sends its own to the CTA that adds up a channel, [share][row][own channel] behind its ring.
     const bool push = p.split > 1;
     const int per = (128 + p.split - 1) / p.split, own0 = per * rank, own_n = min(per, 128 - own0);      // channels added up here
@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     }
     if (threadIdx.x < 8) row_top[threadIdx.x] = 0u;
     if (warp == 1) {
-        tcgen05_alloc(smem_u32(&tmem_slot), (uint32_t)tmem_cols);
+        tcgen05_alloc(smem_u32(&tmem_slot), tmem_cols);
         tcgen05_relinquish();
     }
     tcgen05_fence_before();
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     __syncthreads();
     if (warp == 1) {
         tcgen05_fence_after();
-        tcgen05_dealloc(tmem, (uint32_t)tmem_cols);
+        tcgen05_dealloc(tmem, tmem_cols);
     }
 }
 
@@ -417,7 +417,10 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     if (p.stages > kStreamMaxStages) p.stages = kStreamMaxStages;
     const int share = (steps + p.split - 1) / p.split;
     if (p.stages > share) p.stages = share;
-    const int bytes = p.stages * p.stage_bytes + sums;
+    // (at least a quarter of an SM's, so that no more CTAs share an SM than its tensor memory has room for: CTAs of a cluster wait for one another,
+    // which one that waits for tensor memory must not hold up)
+    int bytes = p.stages * p.stage_bytes + sums;
+    if (bytes < kStreamLeastSmem) bytes = kStreamLeastSmem;
     if ((long long)tiles * p.split > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * p.split));

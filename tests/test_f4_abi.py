@@ -117,3 +117,65 @@ def test_oracle_quantization_of_known_blocks():
     assert s[0, 0] == 128 and list(fo.E2M1[c[0, :4]]) == [6, -1.5, 0.5, 0]
     c, s, r = fo.quantize(x, 16)                   # row scale: 12 <= 2688 r -> 2^-7; block scale 12 / 6 x 128 = 256
     assert r[0] == 2.0 ** -7 and fo.e4m3_values()[s[0, 0]] == 256 and s[0, 1] == 0 and list(fo.E2M1[c[0, :4]]) == [6, -1.5, 0.5, 0]
+
+
+# ---- what no run shows -------------------------------------------------------------------------------------------------------------------
+
+
+def _digit_ring(M, stages, units, rng, warps=16):
+    """The decode kernel's ring: digit warps (row m, every `teams`-th unit), the loading warp and the multiplying one take turns in any order that
+    their waits allow.  A wait for a free slot sees parity alone.  Returns what went wrong."""
+    teams = min(warps // M, stages)
+    actors = [(t, m) for t in range(teams) for m in range(M)]
+    at = {w: w[0] for w in actors}
+    freed, arrived, loaded, consumed = [0] * stages, [0] * units, 0, 0
+    free = lambda i: i < stages or (freed[i % stages] & 1) != ((i // stages - 1) & 1)
+    while consumed < units:
+        moves = [w for w in actors if at[w] < units and free(at[w])]
+        if loaded < units and free(loaded):
+            moves.append("load")
+        if loaded > consumed and arrived[consumed] == M:
+            moves.append("multiply")
+        if not moves:
+            return "stuck"
+        move = moves[rng.integers(len(moves))]
+        i = loaded if move == "load" else at.get(move, 0)
+        if move != "multiply" and i - stages >= consumed:
+            return "slot overwritten"
+        if move == "load":
+            loaded += 1
+        elif move == "multiply":
+            freed[consumed % stages] += 1
+            consumed += 1
+        else:
+            arrived[i] += 1
+            at[move] += teams
+    return "done"
+
+
+@pytest.mark.parametrize("M", range(1, 9))
+def test_ring_of_the_decode_kernel(M):
+    rng = np.random.default_rng(M)
+    for stages in range(1, 8):
+        for units in (1, 2, 5, 9, 16, 33):
+            assert _digit_ring(M, stages, units, rng) == "done"
+
+
+def test_what_a_predecessor_wrote_is_read_behind_the_wait_by_ordinary_loads():
+    import os
+    import re
+    from paper_2511_11248_b200 import build
+    kernels = {}
+    for name in ("f4_rows.cu", "f4_stream.cuh", "f4_pair.cuh"):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(build.CSRC, name)).read())
+        assert not re.search(r"__ldg\(|ld\.global\.nc|__ldlu\(|const [^,()]*__restrict__", text), name
+        for m in re.finditer(r"__global__ void[^;{]*?(\w+_kernel)\s*\([^)]*\)\s*\{(?P<body>.*?)\n\}", text, re.S):
+            kernels[m[1]] = m["body"]
+    early = {k for k, body in kernels.items() if "grid_wait();" in body}
+    assert early == {"f4_quantize_kernel", "f4_quantize16_kernel", "f4_row_scales_kernel", "f4_dequant_kernel", "f4_stream_kernel", "f4_pair_kernel"}
+    for k in early:
+        body = kernels[k]
+        before = body[:body.index("grid_wait();")]
+        assert "grid_launch_next" not in before, k
+        # in front of the wait only weights are loaded and only shared memory written
+        assert not re.search(r"load_a\(|p\.x\b|ld_dependent|atomicCAS\(p\.status", before), k
