@@ -48,37 +48,35 @@ template <bool DIGITS>
 __host__ __device__ inline int stream_b_bytes(int M, int cols) { return DIGITS ? 2 * digit_half(M) : cols * 128; }
 
 // Balanced octal digits of eight numbers, as e2m1 codes: word j of the result holds digit j of number i in bits 4 i.
-// y[i] = X + sum_{j<7} 4 8^j + 2 8^7, so that octal digit j of y is n_j + 4 (of the top one n_7 + 2).
+// y[i] = X + sum_{j<7} 4 8^j + 2 8^7, so that octal digit j of y is n_j + 4 (of the top one n_7 + 2).  Spread into nibbles, the digits are
+// byte selectors into a table of eight codes.
 __device__ __forceinline__ void digit_codes(const uint32_t (&y)[8], uint32_t (&out)[8])
 {
-    uint32_t c[8];
+    // codes of n = -4 .. 3, of an even number in the low half of a byte, of an odd one in the high half
+    const uint32_t t0 = opaque_u32<0x090A0B0Cu>(), t1 = opaque_u32<0x03020100u>(), u0 = opaque_u32<0x90A0B0C0u>(), u1 = opaque_u32<0x30201000u>();
+    uint32_t lo[4], hi[4];                       // of two numbers: digits 0..3 and 4..7, a byte each
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        // octal digits into nibbles
-        uint32_t v = y[i] + (y[i] & 0x00FFF000u) * 15u;
-        v += (v & 0x0FC00FC0u) * 3u;
-        v += (v & 0x38383838u) + 0x20000000u;
-        // f = n + 4 into sign and magnitude: f & 3 for n >= 0; 8 + (4 - f) = 9 + (f ^ 3) below
-        const uint32_t neg = ~(v >> 2) & 0x11111111u;
-        c[i] = ((v & 0x33333333u) ^ (neg * 3u)) + neg * 9u;
-    }
-    // transpose: nibbles of pairs, then bytes
-    uint32_t even[4], odd[4];
+    for (int i = 0; i < 8; i += 2) {
+        uint32_t v[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        even[i] = bsel(0x0F0F0F0Fu, c[2 * i], c[2 * i + 1] << 4);
-        odd[i] = bsel(0x0F0F0F0Fu, c[2 * i] >> 4, c[2 * i + 1]);
+        for (int e = 0; e < 2; ++e) {
+            v[e] = y[i + e] + (y[i + e] & 0x00FFF000u) * 15u;
+            v[e] += (v[e] & 0x0FC00FC0u) * 3u;
+            v[e] += (v[e] & 0x38383838u) + 0x20000000u;
+        }
+        lo[i / 2] = __byte_perm(t0, t1, v[0]) | __byte_perm(u0, u1, v[1]);
+        hi[i / 2] = __byte_perm(t0, t1, v[0] >> 16) | __byte_perm(u0, u1, v[1] >> 16);
     }
     auto bytes = [](const uint32_t (&w)[4], uint32_t *o) {
         const uint32_t a = __byte_perm(w[0], w[1], 0x5140), b = __byte_perm(w[2], w[3], 0x5140);
         const uint32_t d = __byte_perm(w[0], w[1], 0x7362), e = __byte_perm(w[2], w[3], 0x7362);
         o[0] = __byte_perm(a, b, 0x5410);
-        o[2] = __byte_perm(a, b, 0x7632);
-        o[4] = __byte_perm(d, e, 0x5410);
-        o[6] = __byte_perm(d, e, 0x7632);
+        o[1] = __byte_perm(a, b, 0x7632);
+        o[2] = __byte_perm(d, e, 0x5410);
+        o[3] = __byte_perm(d, e, 0x7632);
     };
-    bytes(even, out);
-    bytes(odd, out + 1);
+    bytes(lo, out);
+    bytes(hi, out + 4);
 }
 
 template <int BLOCK, typename T, bool DIGITS>
@@ -176,18 +174,23 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
             if (!warp_all(mbar_wait(full0 + 8 * s, ph))) { ok = false; break; }
             tcgen05_fence_after();
             if (lead) {
+                // (scales of both halves, then the products: the scales' copies follow one another)
+                const uint32_t sfa = tmem + (uint32_t)p.cols, sfb = sfa + 8u;
+#pragma unroll
+                for (uint32_t u = 0; u < 2; ++u)
+                    if (u < two)
+#pragma unroll
+                        for (uint32_t c = 0; c < CHUNKS; ++c) {
+                            tcgen05_cp_scales(sfa + 16 * u + 4 * c, sf + ((off_sfa + u * SB + 512 * c) >> 4));
+                            tcgen05_cp_scales(sfb + 16 * u + 4 * c, sf + ((off_sfb + u * SB + 512 * c) >> 4));
+                        }
 #pragma unroll
                 for (uint32_t u = 0; u < 2; ++u)
                     if (u < two) {
-                        const uint32_t sfa = tmem + (uint32_t)p.cols + u * 16u, sfb = sfa + 8u;
-#pragma unroll
-                        for (uint32_t c = 0; c < CHUNKS; ++c) {
-                            tcgen05_cp_scales(sfa + 4 * c, sf + ((off_sfa + u * SB + 512 * c) >> 4));
-                            tcgen05_cp_scales(sfb + 4 * c, sf + ((off_sfb + u * SB + 512 * c) >> 4));
-                        }
                         const uint64_t wa = wd + ((u * 512) >> 4), xb = xd + ((u * b_half) >> 4);
-                        tcgen05_mma_f4<BLOCK>(tmem, wa, xb, id0, sfa, sfb, (i | (int)u) != 0);
-                        tcgen05_mma_f4<BLOCK>(tmem, wa + 16, xb + ((2 * b_chunk) >> 4), id1, sfa + (BLOCK == 32 ? 0 : 4), sfb + (BLOCK == 32 ? 0 : 4), 1);
+                        const uint32_t second = BLOCK == 32 ? 0 : 4;
+                        tcgen05_mma_f4<BLOCK>(tmem, wa, xb, id0, sfa + 16 * u, sfb + 16 * u, (i | (int)u) != 0);
+                        tcgen05_mma_f4<BLOCK>(tmem, wa + 16, xb + ((2 * b_chunk) >> 4), id1, sfa + 16 * u + second, sfb + 16 * u + second, 1);
                     }
                 tcgen05_commit(empty0 + 8 * s);
             }
@@ -208,6 +211,17 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
         } else {
             const T *x = static_cast<const T *>(p.x);
             const int l16 = lane & 15;
+            // A warp has a row, and of its units every `teams`-th; a lane eight of a unit's 256 values.  A wait for a free slot names its turn by parity
+            // alone: it holds only where the turn before is known to have passed.  So a warp's units lie at most a round of the ring
+            // apart: the unit before, whose slot's turn it has waited for, is at least as late.
+            const int teams = min(kDigitWarps / p.M, p.stages), team = (warp - 2) / p.M, m = (warp - 2) - team * p.M;
+            const uint4 *xm = reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx) + lane;
+            auto fetch = [&](int i) {
+                const int at = (u0 + i) * (2 * kF4Half / 8);
+                return i < nu && at + lane < p.K / 8 ? ld_dependent(xm + at) : make_uint4(0u, 0u, 0u, 0u);
+            };
+            uint4 next = make_uint4(0u, 0u, 0u, 0u);
+            if (team < teams) next = fetch(team);
             if constexpr (BLOCK == 16) {
                 // the largest magnitude of each row of this share of k (of a row that holds an infinity or a NaN: whatever comes out)
                 const int k1 = min(p.K, (u0 + nu) * (2 * kF4Half));
@@ -230,17 +244,6 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                 }
                 asm volatile("bar.sync 1, %0;" ::"n"(32 * kDigitWarps) : "memory");
             }
-            // A warp has a row, and of its units every `teams`-th; a lane eight of a unit's 256 values.  A wait for a free slot names its turn by parity
-            // alone: it holds only where the turn before is known to have passed.  So a warp's units lie at most a round of the ring
-            // apart: the unit before, whose slot's turn it has waited for, is at least as late.
-            const int teams = min(kDigitWarps / p.M, p.stages), team = (warp - 2) / p.M, m = (warp - 2) - team * p.M;
-            const uint4 *xm = reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx) + lane;
-            auto fetch = [&](int i) {
-                const int at = (u0 + i) * (2 * kF4Half / 8);
-                return i < nu && at + lane < p.K / 8 ? ld_dependent(xm + at) : make_uint4(0u, 0u, 0u, 0u);
-            };
-            uint4 next = make_uint4(0u, 0u, 0u, 0u);
-            if (team < teams) next = fetch(team);
             int s = team;
             uint32_t ph = 1;                                     // (the first round of the ring does not wait)
             for (int i = team; i < nu && team < teams; i += teams, s += teams) {
@@ -249,20 +252,17 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                 next = fetch(i + teams);
                 const uint32_t w[4] = {cur.x, cur.y, cur.z, cur.w};
                 float f[8];
-                float top = 0.f;
-                bool fine = true;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float2 v = f4_to_float2<T>(w[e]);
                     f[2 * e] = v.x;
                     f[2 * e + 1] = v.y;
-                    fine = fine && fabsf(v.x) < __int_as_float(0x7F800000) && fabsf(v.y) < __int_as_float(0x7F800000);
-                    top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
                 }
-                // largest magnitude of the block: exponents order like integers, and those of what is not finite above all others
-                uint32_t eb = fine ? __float_as_uint(top) >> 23 : 255u;
+                // the block's largest magnitude as a bit pattern (they order like the values, infinities and NaN above all others), its exponent
+                uint32_t t2 = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
 #pragma unroll
-                for (int o = BLOCK / 16; o; o >>= 1) eb = max(eb, __shfl_xor_sync(0xffffffffu, eb, o));
+                for (int o = BLOCK / 16; o; o >>= 1) t2 = __vmaxu2(t2, __shfl_xor_sync(0xffffffffu, t2, o));
+                const uint32_t eb = __float_as_uint(f4_to_float2<T>(max(t2 & 0xFFFFu, t2 >> 16)).x) >> 23;
                 uint32_t byte;                                   // the block's scale
                 int e2;                                          // E + 127
                 if constexpr (BLOCK == 32) {
@@ -290,10 +290,10 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                 }
                 uint32_t d[8];
                 digit_codes(yb, d);
-                uint32_t word = 0;                               // four blocks' scales
-                const int src = BLOCK == 32 ? (lane & 16) : (lane & 24);
-#pragma unroll
-                for (int b = 0; b < 4; ++b) word |= __shfl_sync(0xffffffffu, byte, src + b * (BLOCK / 8)) << (8 * b);
+                // four blocks' scales: lanes of a block 4 (2) apart, four blocks in 16 (8) lanes
+                uint32_t word = byte << (BLOCK == 32 ? 2 * (lane & 12) : 4 * (lane & 6));
+                word |= __shfl_xor_sync(0xffffffffu, word, BLOCK / 8);
+                word |= __shfl_xor_sync(0xffffffffu, word, BLOCK / 4);
                 ok = warp_all(mbar_wait(empty0 + 8 * s, ph));
                 if (!ok) break;
                 uint8_t *st = smem + (size_t)s * p.stage_bytes;
