@@ -250,7 +250,8 @@ tman_status tman_mpgemv_static(const void *packed, size_t packed_bytes, const vo
  * (No counterpart in the paper.)  Matrices of e2m1 values (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; sign in bit 3 of the
  * code) with a scale per block of `block` consecutive k of a row:
  *   block = 32   scale e8m0, 2^(byte - 127), 255 is NaN; row scales are 1 and not stored
- *   block = 16   scale e4m3, times an fp32 scale per row (a checkpoint's one scale per matrix: the same number in every row)
+ *   block = 16   scale e4m3 (not negative: bytes below 128, 127 is NaN), times an fp32 scale per row (a checkpoint's one scale per
+ *                matrix: the same number in every row)
  * A matrix has `rows` rows of K values; weights are [N][K], one row per output channel, quantized activations [M][K].  Both are held in
  * the same packed buffer, which the products read by linear copies (layout: csrc/f4.cuh).
  *   - rows >= 1, any number; K a multiple of block (else TMAN_ERR_SHAPE).  dtype: 0 = fp16, 1 = bf16 (else TMAN_ERR_UNSUPPORTED).
@@ -290,11 +291,17 @@ tman_status tman_quantize_rows_f4(const void *x, int ldx, int dtype, int rows, i
 tman_status tman_dequant_rows_f4(const void *packed, size_t packed_bytes, int rows, int K, int block, void *x, int ldx, int dtype,
                                  void *workspace, size_t ws_bytes, tman_stream_t stream);
 
-/* Decode: y[m][n] = sum_k x[m][k] w[n][k] for 16-bit activations, M in [1, 8]; x and y have the type `dtype`. */
+/* Decode: y[m][n] = sum_k x[m][k] w[n][k] for 16-bit activations, M in [1, 8]; x and y have the type `dtype`.
+ * Precision: within a block of k the activations are fixed-point numbers of 22 bits (off by at most 2^-21 of the block's largest
+ * magnitude; with block = 16, of 2^-17 of the largest magnitude of the row's share of k that a CTA has, where the block's own is
+ * smaller), multiplied with the weights exactly; sums in fp32, in an order that does not depend on timing.  A row with an infinity or a
+ * NaN gives NaN in every channel.  Nothing is kept in the workspace but the status word. */
 tman_status tman_mpgemv_f4(const void *packed, size_t packed_bytes, const void *x, int ldx, void *y, int ldy, int dtype,
                            int M, int K, int N, int block, void *workspace, size_t ws_bytes, tman_stream_t stream);
 
-/* Both operands in 4 bits: y[m][n] = sum_k a[m][k] w[n][k], M >= 1, `a` packed (tman_quantize_rows_f4) with the weights' block. */
+/* Both operands in 4 bits: y[m][n] = sum_k a[m][k] w[n][k], M >= 1, `a` packed (tman_quantize_rows_f4) with the weights' block; y has the
+ * type `dtype`.  Products exact, sums in fp32 in an order that does not depend on timing.  A block of a that stands for NaN makes its
+ * row NaN.  Nothing is kept in the workspace but the status word. */
 tman_status tman_mpgemm_f4(const void *packed, size_t packed_bytes, const void *a_packed, size_t a_bytes, void *y, int ldy, int dtype,
                            int M, int K, int N, int block, void *workspace, size_t ws_bytes, tman_stream_t stream);
 

@@ -48,12 +48,9 @@ def quantize(x, block):
         scales = np.where(fine, scales, 255).astype(np.uint8)
     else:
         m = a.max((1, 2))
-        for i in range(rows):
-            if m[i] > 0:
-                k = -126
-                while m[i] > 2688.0 * 2.0 ** k:
-                    k += 1
-                r[i] = 2.0 ** k
+        r = np.where(m > 0, 2.0 ** -126, 1.0)
+        while (small := (m > 0) & (m > 2688.0 * r)).any():
+            r = np.where(small, 2.0 * r, r)
         grid = e4m3_values()[:127]
         scales = nearest(a.max(-1) / (6.0 * r[:, None]), grid).astype(np.uint8)
         unit = grid[scales] * r[:, None]

@@ -76,6 +76,11 @@ __device__ inline bool f4_header_matches(const void *packed, int rows, int K, in
     const uint32_t *h = reinterpret_cast<const uint32_t *>(packed);
     return h[0] == 0x4E414D54u && h[1] == 0x584D3446u && h[2] == kF4Version && h[3] == (uint32_t)rows && h[4] == (uint32_t)K && h[5] == (uint32_t)block;
 }
+// The same of words that are there already.
+__device__ inline bool f4_header_is(const uint4 &h, const uint2 &g, int rows, int K, int block)
+{
+    return h.x == 0x4E414D54u && h.y == 0x584D3446u && h.z == kF4Version && h.w == (uint32_t)rows && g.x == (uint32_t)K && g.y == (uint32_t)block;
+}
 // Word t (0..63) of a header.
 __device__ inline uint32_t f4_header_word(int t, int rows, int K, int block, const F4Layout &L)
 {

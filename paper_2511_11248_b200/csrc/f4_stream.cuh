@@ -9,11 +9,22 @@
 // or 32 values with largest magnitude in [2^E, 2^(E+1)) every x is the fixed-point number 2^(E-20) X, X = round(x 2^(20-E)) < 2^21, off by
 // at most 2^(E-21); X = sum_j n_j 8^j with eight digits n_j in [-4, 4], and n_j / 2 is an e2m1 value.  Column 8 m + j holds the digits n_j of
 // row m, the block's scale (2^E as e8m0; as e4m3 relative to a power of two of the row) is the columns' block scale, and
-// x w = 4 sum_j 8^(j-7) (column j): products of digits and weights are exact, sums are in fp32.  Eight warps cut x up while the weights arrive.
+// x w = 4 sum_j 8^(j-7) (column j): products of digits and weights are exact, sums are in fp32.  Sixteen
+// warps cut x up while the weights arrive.
 //
 // Otherwise: x is a packed 4-bit matrix, whose units are loaded as they are.
 //
 // The CTAs of a tile's shares of k form a cluster and add their sums through each other's shared memory, in the order of the shares.
+//
+// What bounds it, one row in a graph of calls, each after the one before (32-value blocks; the weights' bytes alone take 4.8 us): 4096 x 14336
+// 7.6 us, 14336 x 4096 7.2, 4096 x 28672 11.3 of 9.5, 4096 x 4096 3.9 of 1.4, 4096 x 1024 3.2 of 0.3.  About 3 us a call pass between the
+// wait for the kernel ahead and the first product (x from L2, its digits) and between the last one and the end of the kernel; in between
+// the bytes in flight bound it: rings of 74 / 111 / 220 KB a CTA give 8.9 / 7.6 / 7.3 us for 4096 x 14336 and 9.1 / 7.2 / 8.6 for 14336 x 4096
+// (with all of an SM's memory the next call cannot fetch its weights beside this one).  Eight rows take 9.8 and 10.4, 16-value blocks 0.5 to 2 us
+// more: a slot holds more of x and fewer weights, and a row's largest magnitude is looked for first.
+// Tried and slower: the weights' later units prefetched into L2 before the wait (8.6 -> 9.0), separate rings for weights and x, also with two
+// tiles a CTA (7.5 -> 8.4, eight rows 9.7 -> 12.2: a second wait and commit a unit), two CTAs an SM (4096 x 4096 3.9 -> 5.6), sums fetched
+// from the other CTAs between two cluster barriers instead of sent (5.2 -> 3.9 for 4096 x 4096 with the headers checked early).
 #pragma once
 
 #include "f4.cuh"
@@ -201,8 +212,16 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
         __syncwarp();
     } else {
         const int pt = threadIdx.x - 64;
-        if (pt == 0 && !f4_header_matches(p.w, p.N, p.K, BLOCK)) bad_header = 1u;
-        if (BLOCK == 16 && pt < 128) w_row[pt] = tile * 128 + pt < p.N ? reinterpret_cast<const float *>(p.w + p.w_rows)[tile * 128 + pt] : 0.f;
+        // The weights' header and row scales: asked for before the wait, like the weights, and looked at when the products are under way.  Past the
+        // L1, which an early launch does not empty of what an earlier call left there.
+        uint4 head0 = make_uint4(0u, 0u, 0u, 0u);
+        uint2 head1 = make_uint2(0u, 0u);
+        float row_scale = 0.f;
+        if (pt == 0) {
+            head0 = __ldcg(reinterpret_cast<const uint4 *>(p.w));
+            head1 = __ldcg(reinterpret_cast<const uint2 *>(p.w + 16));
+        }
+        if (BLOCK == 16 && pt < 128 && tile * 128 + pt < p.N) row_scale = __ldcg(reinterpret_cast<const float *>(p.w + p.w_rows) + tile * 128 + pt);
         grid_wait();
         grid_launch_next();
         if constexpr (!DIGITS) {
@@ -311,6 +330,8 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                 if (lane == 0) mbar_arrive(full0 + 8 * s);
             }
         }
+        if (pt == 0 && !f4_header_is(head0, head1, p.N, p.K, BLOCK)) bad_header = 1u;
+        if (BLOCK == 16 && pt < 128) w_row[pt] = row_scale;
     }
 
     // ---- epilogue: warps 2..5, a channel a lane -------------------------------------------------

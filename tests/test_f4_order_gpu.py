@@ -244,3 +244,39 @@ def test_offsets_beyond_32_bits(block):
     B.tman_dequant_rows_f4(again, N, K, block, out, K, 0, ws)
     want = fo.values(*fo.quantize(torch.from_numpy(w).to(torch.float16).double().numpy(), block), block)
     assert torch.equal(out[at].cpu(), torch.from_numpy(want).to(torch.float16))
+
+
+@pytest.mark.parametrize("block", [32, 16])
+@pytest.mark.parametrize("M", [2, 40, 300])
+def test_weights_rewritten_between_calls(M, block):
+    """One weight buffer written anew before every product, by a quantization, a packing or a copy, with another quantization in between, so that
+    the product may start early: every product is of what was written last."""
+    rng = np.random.default_rng(10 + M)
+    K, N = 512, 2600
+    w = [to_device(rng.standard_normal((N, K)) * 10.0 ** (i - 2), K, torch.float16) for i in range(3)]
+    dev, held = to_device(activations(M, K, rng), K, torch.float16)
+    packed, a = H.alloc_f4(N, K, block), H.alloc_f4(M, K, block)
+    images, plain = [], []
+    for x, h in w:
+        B.tman_quantize_rows_f4(x, K, 0, N, K, block, packed)
+        images.append(packed.clone())
+        c, s, r = fo.quantize(h, block)
+        plain.append((torch.from_numpy(c[:, 0::2] | (c[:, 1::2] << 4)).cuda(), torch.from_numpy(s).cuda(), torch.from_numpy(r).float().cuda()))
+    ws = H.alloc_workspace_f4(B.OP_GEMM, M, K, N, block)
+    outs = [H.alloc_matrix(M, N, torch.float16) for _ in range(9)]
+    for i, y in enumerate(outs):
+        if i % 2 == 0:
+            B.tman_quantize_rows_f4(w[i % 3][0], K, 0, N, K, block, packed)
+        elif i % 4 == 1:
+            B.tman_pack_f4(*plain[i % 3], N, K, block, packed)
+        else:
+            packed.copy_(images[i % 3])
+        B.tman_quantize_rows_f4(dev, K, 0, M, K, block, a)
+        if M <= 8:
+            B.tman_mpgemv_f4(packed, dev, K, y, N, 0, M, K, N, block, ws)
+        else:
+            B.tman_mpgemm_f4(packed, a, y, N, 0, M, K, N, block, ws)
+    torch.cuda.synchronize()
+    x = held if M <= 8 else fo.values(*fo.quantize(held, block), block)
+    for i, y in enumerate(outs):
+        check_product(y, x, fo.values(*fo.quantize(w[i % 3][1], block), block), block, "f16", exact_operands=M > 8)
