@@ -233,33 +233,26 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
             // A warp has a row, and of its units every `teams`-th; a lane eight of a unit's 256 values.  A wait for a free slot names its turn by parity
             // alone: it holds only where the turn before is known to have passed.  So a warp's units lie at most a round of the ring
             // apart: the unit before, whose slot's turn it has waited for, is at least as late.
-            const int teams = min(kDigitWarps / p.M, p.stages), team = (warp - 2) / p.M, m = (warp - 2) - team * p.M;
+            const int all_teams = kDigitWarps / p.M, teams = min(all_teams, p.stages), team = (warp - 2) / p.M, m = (warp - 2) - team * p.M;
             const uint4 *xm = reinterpret_cast<const uint4 *>(x + (size_t)m * p.ldx) + lane;
             auto fetch = [&](int i) {
                 const int at = (u0 + i) * (2 * kF4Half / 8);
                 return i < nu && at + lane < p.K / 8 ? ld_dependent(xm + at) : make_uint4(0u, 0u, 0u, 0u);
             };
+            auto top_of = [](uint32_t t, const uint4 &v) {
+                return __vmaxu2(t, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
+            };
             uint4 next = make_uint4(0u, 0u, 0u, 0u);
-            if (team < teams) next = fetch(team);
+            if (team < all_teams) next = fetch(team);
             if constexpr (BLOCK == 16) {
-                // the largest magnitude of each row of this share of k (of a row that holds an infinity or a NaN: whatever comes out)
-                const int k1 = min(p.K, (u0 + nu) * (2 * kF4Half));
-#pragma unroll 1
-                for (int m0 = 0; m0 < p.M; m0 += 4) {
-                    uint32_t mx[4] = {};
-                    for (int k = u0 * (2 * kF4Half) + pt * 8; k < k1; k += 32 * kDigitWarps * 8) {
-                        uint4 v[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = ld_dependent(reinterpret_cast<const uint4 *>(x + (size_t)min(m0 + e, p.M - 1) * p.ldx + k));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            mx[e] = __vmaxu2(mx[e], __vmaxu2(__vmaxu2(v[e].x & 0x7FFF7FFFu, v[e].y & 0x7FFF7FFFu), __vmaxu2(v[e].z & 0x7FFF7FFFu, v[e].w & 0x7FFF7FFFu)));
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t top = __reduce_max_sync(0xffffffffu, max(mx[e] & 0xFFFFu, mx[e] >> 16));
-                        if (lane == 0) atomicMax(&row_top[min(m0 + e, p.M - 1)], top);
-                    }
+                // the largest magnitude of each row of this share of k (of a row that holds an infinity or a NaN: whatever comes out); every value is
+                // asked for once a CTA: all CTAs read the same few lines
+                if (team < all_teams) {
+                    uint32_t t = top_of(0u, next);
+#pragma unroll 4
+                    for (int i = team + all_teams; i < nu; i += all_teams) t = top_of(t, fetch(i));
+                    t = __reduce_max_sync(0xffffffffu, max(t & 0xFFFFu, t >> 16));
+                    if (lane == 0) atomicMax(&row_top[m], t);
                 }
                 asm volatile("bar.sync 1, %0;" ::"n"(32 * kDigitWarps) : "memory");
             }
@@ -278,7 +271,7 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                     f[2 * e + 1] = v.y;
                 }
                 // the block's largest magnitude as a bit pattern (they order like the values, infinities and NaN above all others), its exponent
-                uint32_t t2 = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
+                uint32_t t2 = top_of(0u, cur);
 #pragma unroll
                 for (int o = BLOCK / 16; o; o >>= 1) t2 = __vmaxu2(t2, __shfl_xor_sync(0xffffffffu, t2, o));
                 const uint32_t eb = __float_as_uint(f4_to_float2<T>(max(t2 & 0xFFFFu, t2 >> 16)).x) >> 23;
