@@ -39,10 +39,12 @@ constexpr int kDigitWarps = 16;
 __host__ __device__ constexpr int stream_threads(bool digits) { return digits ? 64 + 32 * kDigitWarps : 192; }      // warp 0: loads, 1: MMAs, others: digits, epilogue
 constexpr int kStreamMaxRows = 64;       // of a packed x
 constexpr int kStreamMaxSplit = 8;
-constexpr int kStreamHalfSm = 111 * 1024, kStreamAllSm = 220 * 1024, kStreamLeastSmem = 57 * 1024;
+constexpr int kStreamHalfSm = 114176,      // (with 1.5 KB that are static and 1 KB of the system's)
+               kStreamAllSm = 220 * 1024, kStreamLeastSmem = 57 * 1024;
 constexpr int kStreamMaxStages = 12;
 // Digits in shared memory: core matrices 16 bytes further apart than they are long, half units 64 bytes (mod 128), so that the stores of a warp
-// (four bytes of 32 places along k) meet no bank twice.  Of an odd M the tile's last eight columns are whatever lies behind.
+// (four bytes of 32 places along k) meet no bank twice.  Of an odd M the tile's last eight columns are whatever lies behind, of the second half
+// unit the 576 bytes from the scales on, which a stage therefore has.
 constexpr int kDigitLbo = 144, kDigitSbo = 4 * kDigitLbo;
 __host__ __device__ constexpr int digit_half(int M) { return M * kDigitSbo + (M % 2 ? 0 : 64); }
 
@@ -57,6 +59,10 @@ struct F4StreamParams {
 
 template <bool DIGITS>
 __host__ __device__ inline int stream_b_bytes(int M, int cols) { return DIGITS ? 2 * digit_half(M) : cols * 128; }
+// Scales of a unit of x in a stage.  Of digits, at most 64 columns, the scales of 64 values of k take two of the four columns that one copy brings
+// to tensor memory: two 512-byte pieces in one.
+__host__ __device__ constexpr int stream_sfb_bytes(int block, bool digits) { return digits ? (block == 32 ? 640 : 1024) : 2 * f4_scale_bytes(block); }
+static_assert(stream_sfb_bytes(32, true) >= kDigitSbo && stream_sfb_bytes(16, true) >= kDigitSbo, "what an odd M's last columns read lies in the stage");
 
 // Balanced octal digits of eight numbers, as e2m1 codes: word j of the result holds digit j of number i in bits 4 i.
 // y[i] = X + sum_{j<7} 4 8^j + 2 8^7, so that octal digit j of y is n_j + 4 (of the top one n_7 + 2).  Spread into nibbles, the digits are
@@ -193,15 +199,17 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
 #pragma unroll
                         for (uint32_t c = 0; c < CHUNKS; ++c) {
                             tcgen05_cp_scales(sfa + 16 * u + 4 * c, sf + ((off_sfa + u * SB + 512 * c) >> 4));
-                            tcgen05_cp_scales(sfb + 16 * u + 4 * c, sf + ((off_sfb + u * SB + 512 * c) >> 4));
+                            if constexpr (!DIGITS) tcgen05_cp_scales(sfb + 16 * u + 4 * c, sf + ((off_sfb + u * SB + 512 * c) >> 4));
+                            else if (c == 0 && (BLOCK == 16 || u == 0)) tcgen05_cp_scales(sfb + 16 * u, sf + ((off_sfb + 512 * u) >> 4));
                         }
 #pragma unroll
                 for (uint32_t u = 0; u < 2; ++u)
                     if (u < two) {
                         const uint64_t wa = wd + ((u * 512) >> 4), xb = xd + ((u * b_half) >> 4);
-                        const uint32_t second = BLOCK == 32 ? 0 : 4;
-                        tcgen05_mma_f4<BLOCK>(tmem, wa, xb, id0, sfa + 16 * u, sfb + 16 * u, (i | (int)u) != 0);
-                        tcgen05_mma_f4<BLOCK>(tmem, wa + 16, xb + ((2 * b_chunk) >> 4), id1, sfa + 16 * u + second, sfb + 16 * u + second, 1);
+                        const uint32_t fb = DIGITS && BLOCK == 32 ? sfb + 2 * u : sfb + 16 * u;
+                        tcgen05_mma_f4<BLOCK>(tmem, wa, xb, id0, sfa + 16 * u, fb, (i | (int)u) != 0);
+                        tcgen05_mma_f4<BLOCK>(tmem, wa + 16, xb + ((2 * b_chunk) >> 4), id1, sfa + 16 * u + (BLOCK == 32 ? 0 : 4),
+                                              fb + (BLOCK == 32 ? 0 : DIGITS ? 2 : 4), 1);
                     }
                 tcgen05_commit(empty0 + 8 * s);
             }
@@ -315,7 +323,8 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                     for (int e = 0; e < 8; ++e) *reinterpret_cast<uint32_t *>(b + e * 16) = d[e];
                     if (BLOCK == 16 || l16 < 8) {
                         const int t = 8 * m + (l16 & 7);
-                        *reinterpret_cast<uint32_t *>(st + off_sfb + ((lane >> 4) * CHUNKS + (l16 >> 3)) * 512 + (t & 31) * 16 + (t >> 5) * 4) = word;
+                        *reinterpret_cast<uint32_t *>(st + off_sfb + (BLOCK == 32 ? (lane >> 4) * 8 : (lane >> 4) * 512 + (l16 >> 3) * 8) + (t & 31) * 16 +
+                                                      (t >> 5) * 4) = word;
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -423,7 +432,7 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     p.cols = DIGITS ? (p.M + 1) / 2 * 16 : (p.M + 15) / 16 * 16;
     const int steps = (p.halves + 1) / 2;
     p.split = stream_split(tiles, steps, info->sms.load(std::memory_order_relaxed));
-    p.stage_bytes = (kF4Tile * 128 + 4 * f4_scale_bytes(BLOCK) + stream_b_bytes<DIGITS>(p.M, p.cols) + 127) / 128 * 128;
+    p.stage_bytes = (kF4Tile * 128 + 2 * f4_scale_bytes(BLOCK) + stream_sfb_bytes(BLOCK, DIGITS) + stream_b_bytes<DIGITS>(p.M, p.cols) + 127) / 128 * 128;
     // Half an SM's shared memory, so that the next call's CTAs fill their rings beside this one's; all of it where half holds few stages.
     const int budget = p.stage_bytes * (DIGITS ? 3 : 4) <= kStreamHalfSm ? kStreamHalfSm : kStreamAllSm;
     const int sums = p.split > 1 ? (128 + 8) * p.M * 4 : 0;
