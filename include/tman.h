@@ -257,7 +257,7 @@ tman_status tman_mpgemv_static(const void *packed, size_t packed_bytes, const vo
  *   - rows >= 1, any number; K a multiple of block (else TMAN_ERR_SHAPE).  dtype: 0 = fp16, 1 = bf16 (else TMAN_ERR_UNSUPPORTED).
  *   - ldx, ldy: values from a row of x or y to the next, at least the row's length.  x is 16-byte aligned and ldx a multiple of 8
  *     (TMAN_ERR_SHAPE); y of the products needs the alignment of its type only.
- *   - packed and workspace are 256-byte aligned.  The rules on the stream order of packed buffers below hold for these too;
+ *   - packed and workspace are 256-byte aligned.  The rules on the stream order of packed buffers above hold for these too;
  *     tman_pack_f4 and tman_quantize_rows_f4 may be followed by any call. */
 
 /* Bytes of the packed buffer of `rows` rows. */

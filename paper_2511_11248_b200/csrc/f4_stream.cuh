@@ -17,14 +17,14 @@
 // The CTAs of a tile's shares of k form a cluster and add their sums through each other's shared memory, in the order of the shares.
 //
 // What bounds it, one row in a graph of calls, each after the one before (32-value blocks; the weights' bytes alone take 4.8 us): 4096 x 14336
-// 7.6 us, 14336 x 4096 7.2, 4096 x 28672 11.3 of 9.5, 4096 x 4096 3.9 of 1.4, 4096 x 1024 3.2 of 0.3.  About 3 us a call pass between the
+// 7.5 us, 14336 x 4096 7.2, 4096 x 28672 10.8 to 11.3 of 9.5, 4096 x 4096 3.9 of 1.4, 4096 x 1024 3.2 of 0.3.  About 3 us a call pass between the
 // wait for the kernel ahead and the first product (x from L2, its digits) and between the last one and the end of the kernel; in between
-// the bytes in flight bound it: rings of 74 / 111 / 220 KB a CTA give 8.9 / 7.6 / 7.3 us for 4096 x 14336 and 9.1 / 7.2 / 8.6 for 14336 x 4096
-// (with all of an SM's memory the next call cannot fetch its weights beside this one).  Eight rows take 9.8 and 10.4, 16-value blocks 0.5 to 2 us
-// more: a slot holds more of x and fewer weights, and a row's largest magnitude is looked for first.
+// the weights' bytes in flight bound it: rings of 74 / 111 / 220 KB a CTA give 8.9 / 7.6 / 7.3 us for 4096 x 14336 and 9.1 / 7.2 / 8.6 for 14336 x
+// 4096 (with all of an SM's memory the next call cannot fetch its weights beside this one).  More rows leave a ring fewer stages: two, four and
+// eight take 7.9, 8.2 and 9.8 us, in 16-value blocks of 14336 x 4096 8.2, 10.4 and 12.2.
 // Tried and slower: the weights' later units prefetched into L2 before the wait (8.6 -> 9.0), separate rings for weights and x, also with two
 // tiles a CTA (7.5 -> 8.4, eight rows 9.7 -> 12.2: a second wait and commit a unit), two CTAs an SM (4096 x 4096 3.9 -> 5.6), sums fetched
-// from the other CTAs between two cluster barriers instead of sent (5.2 -> 3.9 for 4096 x 4096 with the headers checked early).
+// from the other CTAs between two cluster barriers instead of sent (4096 x 4096 5.2, sent and with the headers checked early 3.9).
 #pragma once
 
 #include "f4.cuh"
@@ -381,18 +381,16 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
         }
     }
     if (push && warp >= 2 && warp < 6) {
-        {
-            // (Every CTA sends its sums, whatever its own waits say, within their limit of a second each: waited for several times as
-            // long, so that no CTA is gone when sums for it arrive.)
-            bool all = false;
-            for (int i = 0; i < 8 && !all; ++i) all = warp_all(mbar_wait(smem_u32(&sums_bar), 0));
-            ok = ok && all;
-            for (int i = threadIdx.x - 64; i < p.M * own_n; i += 128) {
-                const int m = i / own_n, c = i - m * own_n, n = tile * 128 + own0 + c;
-                float v = 0.f;
-                for (int r = 0; r < p.split; ++r) v += sums[(r * p.M + m) * per + c];
-                if (ok && hdr_ok && n < p.N) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * w_row[own0 + c] * (DIGITS ? 1.f : a_row[m]) : v);
-            }
+        // (Every CTA sends its sums, whatever its own waits say, within their limit of a second each: waited for several times as
+        // long, so that no CTA is gone when sums for it arrive.)
+        bool all = false;
+        for (int i = 0; i < 8 && !all; ++i) all = warp_all(mbar_wait(smem_u32(&sums_bar), 0));
+        ok = ok && all;
+        for (int i = threadIdx.x - 64; i < p.M * own_n; i += 128) {
+            const int m = i / own_n, c = i - m * own_n, n = tile * 128 + own0 + c;
+            float v = 0.f;
+            for (int r = 0; r < p.split; ++r) v += sums[(r * p.M + m) * per + c];
+            if (ok && hdr_ok && n < p.N) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * w_row[own0 + c] * (DIGITS ? 1.f : a_row[m]) : v);
         }
     }
     if (!ok) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_TIMEOUT);

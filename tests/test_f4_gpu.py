@@ -203,6 +203,15 @@ def test_gemv(M, K, N, block, ty):
         check_product(y[:, :N], held, fo.values(codes, scales, rs, block), block, ty, exact_operands=False)
 
 
+# As many tiles as there are SMs or more, so that one CTA has all of k, and rings that are full (K of 16 units and more): of an odd M the products'
+# last columns reach behind the digits of the last stage.
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("block", [32, 16])
+@pytest.mark.parametrize("M,K,N", [(1, 4096, 14336), (3, 4096, 18944), (5, 4096, 18944), (7, 4352, 18945), (8, 1376, 18944), (1, 5152, 19001)])
+def test_gemv_with_a_full_ring_and_whole_rows_of_k(M, K, N, block, ty):
+    test_gemv(M, K, N, block, ty)
+
+
 GEMM = [(1, 32, 1), (1, 4096, 1024), (2, 288, 130), (9, 160, 200), (16, 1056, 1001), (33, 640, 257), (100, 512, 384), (128, 1024, 264), (129, 2080, 136), (200, 4096, 96),
         (257, 96, 513), (300, 1184, 1000), (520, 256, 72), (1030, 768, 520), (17, 18944, 200)]
 
