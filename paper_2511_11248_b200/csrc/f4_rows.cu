@@ -1,11 +1,10 @@
 // Microscaled 4-bit floating point: packing and unpacking of a checkpoint's matrix, quantization of rows, dequantization.
 // Memory-bound: every value is read and written once.
 #include "f4.cuh"
+#include "f4_marks.h"
 #include "sm100_ptx.cuh"
 
-#include <mutex>
 #include <type_traits>
-#include <vector>
 
 namespace tman {
 
@@ -88,24 +87,26 @@ tman_status launch_f4_unpack(const void *packed, int rows, int K, int block, uin
 // The kernels let their successor start once their predecessor has ended, so that a product behind them fetches its weights meanwhile; what they
 // write is read only behind the successor's wait.  Unless it is the successor's weights: a product on the stream whose weights are the last
 // thing quantized there is launched in plain stream order.  (An earlier quantization has ended when a later one has let anything start.)
-struct F4Write { cudaStream_t stream; const void *packed; };
-static std::mutex g_f4_mutex;
-static std::vector<F4Write> g_f4_writes;         // the last one of each stream
+static F4Marks g_f4_marks;
 
-static void note_f4_write(cudaStream_t s, const void *packed)
+static tman_status note_f4_write(cudaStream_t s, const void *packed)
 {
-    std::lock_guard<std::mutex> lock(g_f4_mutex);
-    for (F4Write &w : g_f4_writes)
-        if (w.stream == s) { w.packed = packed; return; }
-    g_f4_writes.push_back({s, packed});
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return TMAN_ERR_CUDA;
+    g_f4_marks.note(dev, reinterpret_cast<uintptr_t>(s), packed);
+    return TMAN_OK;
 }
 
+// (Another stream's quantization is ordered before the product by an event, a full dependency.  While a graph is captured the launch's attribute
+// could loosen the edges to all that is ahead of it: plain order there too.)
 bool f4_write_pending(cudaStream_t s, const void *packed)
 {
-    std::lock_guard<std::mutex> lock(g_f4_mutex);
-    for (F4Write &w : g_f4_writes)
-        if (w.stream == s && w.packed == packed) { w.packed = nullptr; return true; }
-    return false;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return true;
+    const F4Marks::Found found = g_f4_marks.take(dev, reinterpret_cast<uintptr_t>(s), packed);
+    if (found != F4Marks::kElsewhere) return found == F4Marks::kHere;
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    return cudaStreamIsCapturing(s, &st) != cudaSuccess || st != cudaStreamCaptureStatusNone;
 }
 
 // One block's scale byte and the codes of eight of its values.  top: the largest magnitude of the block; fine: all its values are finite;
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) f4_quantize_kernel(const T *x
 }
 
 // Block 16: the row's largest magnitude comes first.  A CTA has a row, a warp a unit of 256 columns at a time, a lane V times eight values, which
-// stay in registers between the two.  Bound by the issue of its operations (about ten a value).  (Rows in shared memory, brought by bulk
+// stay in registers between the two.  Bound by the issue of its operations (about 117 instructions for eight values).  (Rows in shared memory, brought by bulk
 // copies while the pair before is worked on: 2048 x 14336 24.7 us, 8192 x 18944 115; two rows a CTA in registers 19.8 and 123; two
 // passes, the second from L2, 26.7 and 127; eight rows a cluster of CTAs with the maxima through distributed shared memory 37.4 and 188.)
 template <typename T, int V, int THREADS>
@@ -386,7 +387,8 @@ static tman_status launch_quantize_as(const void *xv, int ldx, int rows, int K, 
 
 tman_status launch_f4_quantize(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, cudaStream_t s)
 {
-    note_f4_write(s, packed);
+    const tman_status noted = note_f4_write(s, packed);
+    if (noted != TMAN_OK) return noted;
     if (dtype == kF4TypeHalf) return block == 32 ? launch_quantize_as<32, __half>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __half>(x, ldx, rows, K, packed, s);
     return block == 32 ? launch_quantize_as<32, __nv_bfloat16>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __nv_bfloat16>(x, ldx, rows, K, packed, s);
 }

@@ -179,3 +179,32 @@ def test_what_a_predecessor_wrote_is_read_behind_the_wait_by_ordinary_loads():
         assert "grid_launch_next" not in before, k
         # in front of the wait only weights are loaded and only shared memory written
         assert not re.search(r"load_a\(|p\.x\b|ld_dependent|atomicCAS\(p\.status", before), k
+
+
+def test_marks_of_quantized_buffers_tell_streams_devices_and_threads_apart(tmp_path):
+    import subprocess
+    from paper_2511_11248_b200 import build
+    (tmp_path / "m.cpp").write_text("""
+#include "f4_marks.h"
+#include <thread>
+using M = tman::F4Marks;
+int main()
+{
+    M m;
+    int a = 0, b = 0;
+    m.note(0, 0, &a); m.note(1, 0, &b);                       // the default stream of two devices
+    if (m.take(0, 0, &a) != M::kHere || m.take(0, 0, &a) != M::kNone) return 1;
+    if (m.take(0, 0, &b) != M::kNone || m.take(1, 0, &b) != M::kHere) return 2;
+    m.note(0, 1, &a);                                          // the default stream by its other name
+    if (m.take(0, 0, &a) != M::kHere) return 3;
+    m.note(0, 2, &a);                                          // the per-thread stream of two threads
+    std::thread([&] { m.note(0, 2, &b); }).join();
+    if (m.take(0, 2, &a) != M::kHere || m.take(0, 2, &b) != M::kElsewhere) return 4;
+    m.note(0, 64, &a); m.note(0, 64, &b);                      // the last one of a stream
+    if (m.take(0, 64, &a) != M::kNone || m.take(0, 128, &b) != M::kElsewhere || m.take(0, 64, &b) != M::kHere) return 5;
+    return 0;
+}
+""")
+    exe = tmp_path / "m"
+    subprocess.run(["g++", "-std=c++17", "-pthread", "-I", build.CSRC, str(tmp_path / "m.cpp"), "-o", str(exe)], check=True)
+    assert subprocess.run([str(exe)]).returncode == 0

@@ -280,3 +280,34 @@ def test_weights_rewritten_between_calls(M, block):
     x = held if M <= 8 else fo.values(*fo.quantize(held, block), block)
     for i, y in enumerate(outs):
         check_product(y, x, fo.values(*fo.quantize(w[i % 3][1], block), block), block, "f16", exact_operands=M > 8)
+
+
+@pytest.mark.parametrize("block", [32, 16])
+@pytest.mark.parametrize("M", [2, 300])
+def test_a_captured_product_of_weights_quantized_on_another_stream(M, block):
+    """One graph, two streams joined by events: every replay's product is of the weights that this replay quantized."""
+    rng = np.random.default_rng(20 + M)
+    K, N = 1024, 2600
+    dev, held = to_device(activations(M, K, rng), K, torch.float16)
+    src = torch.zeros((N, K), dtype=torch.float16, device="cuda")
+    packed, a = H.alloc_f4(N, K, block), H.alloc_f4(M, K, block)
+    ws, y = H.alloc_workspace_f4(B.OP_GEMM, M, K, N, block), H.alloc_matrix(M, N, torch.float16)
+    B.tman_quantize_rows_f4(dev, K, 0, M, K, block, a)
+    B.tman_quantize_rows_f4(src, K, 0, N, K, block, packed)
+    B.tman_mpgemm_f4(packed, a, y, N, 0, M, K, N, block, ws)
+    torch.cuda.synchronize()
+    main, side, g = torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=main):
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            B.tman_quantize_rows_f4(src, K, 0, N, K, block, packed, stream=side)
+        main.wait_stream(side)
+        B.tman_mpgemm_f4(packed, a, y, N, 0, M, K, N, block, ws, stream=main)
+    x = fo.values(*fo.quantize(held, block), block)
+    for i in range(3):
+        w, h = to_device(rng.standard_normal((N, K)) * 4.0 ** -i, K, torch.float16)
+        src.copy_(w)
+        g.replay()
+        torch.cuda.synchronize()
+        assert B.tman_read_status(ws) == 0
+        check_product(y, x, fo.values(*fo.quantize(h, block), block), block, "f16", exact_operands=True)
