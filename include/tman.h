@@ -286,7 +286,8 @@ tman_status tman_unpack_f4(const void *packed, size_t packed_bytes, int rows, in
 tman_status tman_quantize_rows_f4(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, size_t packed_bytes,
                                   tman_stream_t stream);
 
-/* The values a packed matrix stands for, rounded once to fp16 or bf16.  x is the output, rows as for the input of
+/* The values a packed matrix stands for, rounded to fp16 or bf16; before, block scale x row scale and its product with the code are rounded to
+ * fp32, which changes nothing where row scales are powers of two, as a quantization makes them.  x is the output, rows as for the input of
  * tman_quantize_rows_f4. */
 tman_status tman_dequant_rows_f4(const void *packed, size_t packed_bytes, int rows, int K, int block, void *x, int ldx, int dtype,
                                  void *workspace, size_t ws_bytes, tman_stream_t stream);
@@ -301,7 +302,7 @@ tman_status tman_mpgemv_f4(const void *packed, size_t packed_bytes, const void *
 
 /* Both operands in 4 bits: y[m][n] = sum_k a[m][k] w[n][k], M >= 1, `a` packed (tman_quantize_rows_f4) with the weights' block; y has the
  * type `dtype`.  Products exact, sums in fp32 in an order that does not depend on timing.  A block of a that stands for NaN makes its
- * row NaN.  Nothing is kept in the workspace but the status word. */
+ * row NaN.  With block = 16 the sum is multiplied with the weights' row scale and then with a's, both in fp32.  Nothing is kept in the workspace but the status word. */
 tman_status tman_mpgemm_f4(const void *packed, size_t packed_bytes, const void *a_packed, size_t a_bytes, void *y, int ldy, int dtype,
                            int M, int K, int N, int block, void *workspace, size_t ws_bytes, tman_stream_t stream);
 

@@ -255,8 +255,8 @@ __global__ void __launch_bounds__(kPairThreads) f4_pair_kernel(const __grid_cons
                     float c0 = __uint_as_float(odd ? got : keep), c1 = __uint_as_float(odd ? keep : got);
                     if constexpr (BLOCK == 16) {
                         const float f = __shfl_sync(0xffffffffu, ar, e + (odd ? 1 : 0));
-                        c0 *= w0 * f;
-                        c1 *= w1 * f;
+                        c0 = c0 * w0 * f;        // (in turn: the scales' product may leave the range)
+                        c1 = c1 * w1 * f;
                     }
                     if constexpr (WHOLE) st_policy(yt, f4_from_float2<T>(c0, c1), y_policy);
                     else if (t + e + (odd ? 1 : 0) < end && put) {
@@ -336,8 +336,8 @@ __global__ void __launch_bounds__(kPairThreads) f4_pair_kernel(const __grid_cons
                 if (ok && hdr_ok && m < p.M && n < p.N) {
                     if constexpr (BLOCK == 16) {
                         const float f = ld_dependent(a_row + m);
-                        v0 *= f * w_row[n];
-                        v1 *= f * w_row[min(n + 1, p.N - 1)];
+                        v0 = v0 * w_row[n] * f;
+                        v1 = v1 * w_row[min(n + 1, p.N - 1)] * f;
                     }
                     T *y = static_cast<T *>(p.y) + (size_t)m * p.ldy + n;
                     if (pairs_ok) *reinterpret_cast<uint32_t *>(y) = f4_from_float2<T>(v0, v1);

@@ -293,3 +293,27 @@ def test_headers_that_do_not_match_leave_the_output():
 @pytest.mark.parametrize("M,K,N", [(65, 4096, 256), (100, 2048, 1000), (129, 8256, 300), (250, 14336, 513), (600, 5152, 96), (1030, 2080, 250)])
 def test_gemm_of_few_tiles(M, K, N, block):
     test_gemm(M, K, N, block, "bf16")
+
+
+@pytest.mark.parametrize("M,K,N", [(20, 512, 264), (300, 512, 520), (300, 4096, 264), (201, 4096, 131)])
+def test_row_scales_whose_product_leaves_the_range(M, K, N):
+    """Row scales of 2^36 and about 2^93: their product is no fp32 number, the sums times both are.  Odd channels have one weight, 2^-10 x 2^36, even
+    ones none: exact products, so that only the type's half step is left, and zeros stay zeros."""
+    rng = np.random.default_rng(M + N)
+    codes = np.zeros((N, K), np.uint8)
+    codes[1::2, 0] = 1                                # 0.5
+    scales = np.ones((N, K // 16), np.uint8)          # e4m3 2^-9
+    packed = pack_on_device(codes, scales, np.full(N, 2.0 ** 36, np.float32), 16)
+    x = rng.uniform(0.5, 1.0, (M, K)) * 2.0 ** 104
+    x[:, :16] *= 2.0 ** -8
+    dev, held = to_device(x, K, torch.bfloat16)
+    a = H.alloc_f4(M, K, 16)
+    B.tman_quantize_rows_f4(dev, K, B.DTYPE_BF16, M, K, 16, a)
+    ws, y = H.alloc_workspace_f4(B.OP_GEMM, M, K, N, 16), H.alloc_matrix(M, N, torch.bfloat16)
+    B.tman_mpgemm_f4(packed, a, y, N, B.DTYPE_BF16, M, K, N, 16, ws)
+    assert B.tman_read_status(ws) == 0
+    ref = np.zeros((M, N))
+    ref[:, 1::2] = fo.values(*fo.quantize(held, 16), 16)[:, :1] * 2.0 ** 26
+    got = f64(y)
+    assert np.all(got[:, ::2] == 0)
+    assert np.all(np.abs(got - ref) <= HALF_STEP["bf16"] * np.abs(ref))
