@@ -161,7 +161,7 @@ tman_status launch_f4_unpack(const void *packed, int rows, int K, int block, uin
                              cudaStream_t s);
 tman_status launch_f4_quantize(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, cudaStream_t s);
 tman_status launch_f4_dequant(const void *packed, int rows, int K, int block, void *x, int ldx, int dtype, uint32_t *status, cudaStream_t s);
-// Whether the last quantization on stream s wrote `packed`; asked once by a launch that reads it as weights.
+// Whether a quantization ahead of the next launch on s may still be writing `packed`; asked once by a launch that reads it as weights.
 bool        f4_write_pending(cudaStream_t s, const void *packed);
 size_t      f4_workspace_bytes(int op, int M, int K, int N, int block);
 tman_status launch_f4_gemv(const void *packed, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N, int block, void *ws, cudaStream_t s);

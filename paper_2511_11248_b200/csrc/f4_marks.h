@@ -1,4 +1,4 @@
-// Which packed buffer the last quantization of each stream wrote.  A stream is a handle on a device: the default stream's handle is the same on every
+// Which packed buffer the last eager quantization of each stream wrote.  A stream is a handle on a device: the default stream's handle is the same on every
 // device, and the per-thread one's in every thread.
 #pragma once
 

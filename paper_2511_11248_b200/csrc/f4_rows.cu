@@ -1,7 +1,7 @@
 // Microscaled 4-bit floating point: packing and unpacking of a checkpoint's matrix, quantization of rows, dequantization.
 // Memory-bound: every value is read and written once.
 #include "f4.cuh"
-#include "f4_marks.h"
+#include "f4_order.h"
 #include "sm100_ptx.cuh"
 
 #include <type_traits>
@@ -85,29 +85,8 @@ tman_status launch_f4_unpack(const void *packed, int rows, int K, int block, uin
 
 // ---- quantization of rows ----------------------------------------------------------------------
 // The kernels let their successor start once their predecessor has ended, so that a product behind them fetches its weights meanwhile; what they
-// write is read only behind the successor's wait.  Unless it is the successor's weights: a product on the stream whose weights are the last
-// thing quantized there is launched in plain stream order.  (An earlier quantization has ended when a later one has let anything start.)
-static F4Marks g_f4_marks;
-
-static tman_status note_f4_write(cudaStream_t s, const void *packed)
-{
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return TMAN_ERR_CUDA;
-    g_f4_marks.note(dev, reinterpret_cast<uintptr_t>(s), packed);
-    return TMAN_OK;
-}
-
-// (Another stream's quantization is ordered before the product by an event, a full dependency.  While a graph is captured the launch's attribute
-// could loosen the edges to all that is ahead of it: plain order there too.)
-bool f4_write_pending(cudaStream_t s, const void *packed)
-{
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return true;
-    const F4Marks::Found found = g_f4_marks.take(dev, reinterpret_cast<uintptr_t>(s), packed);
-    if (found != F4Marks::kElsewhere) return found == F4Marks::kHere;
-    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
-    return cudaStreamIsCapturing(s, &st) != cudaSuccess || st != cudaStreamCaptureStatusNone;
-}
+// write is read only behind the successor's wait.  Unless it is the successor's weights: such a product is launched in plain stream order
+// (f4_write_pending).  (An earlier quantization has ended when a later one has let anything start.)
 
 // One block's scale byte and the codes of eight of its values.  top: the largest magnitude of the block; fine: all its values are finite;
 // inv_row: 1 / r, a power of two.
@@ -192,7 +171,7 @@ template <int BLOCK, typename T, int V>
 __global__ void __launch_bounds__(32 * kRowsWarps) f4_quantize_kernel(const T *x, int ldx, int rows, int K, uint8_t *packed, const __grid_constant__ F4Layout L, int parts)
 {
     grid_wait();
-    grid_launch_next();                  // (see note_f4_write)
+    grid_launch_next();                  // (see f4_write_pending)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q = lane & 3;
     const int part = blockIdx.x % parts, g = blockIdx.x / parts, row = g * 8 + r;
     if (blockIdx.x == 0 && threadIdx.x < 64) reinterpret_cast<uint32_t *>(packed)[threadIdx.x] = f4_header_word(threadIdx.x, rows, K, BLOCK, L);
@@ -256,7 +235,7 @@ __global__ void __launch_bounds__(THREADS) f4_quantize16_kernel(const T *x, int 
     constexpr int WARPS = THREADS / 32;
     __shared__ uint32_t tops[WARPS];
     grid_wait();
-    grid_launch_next();                  // (see note_f4_write)
+    grid_launch_next();                  // (see f4_write_pending)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
     if (blockIdx.x == 0 && threadIdx.x < 64) reinterpret_cast<uint32_t *>(packed)[threadIdx.x] = f4_header_word(threadIdx.x, rows, K, 16, L);
     const uint4 *src = reinterpret_cast<const uint4 *>(x + (size_t)row * ldx) + threadIdx.x;
@@ -322,7 +301,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) f4_row_scales_kernel(const T 
 {
     __shared__ uint32_t tops[kRowsWarps];
     grid_wait();
-    grid_launch_next();                  // (see note_f4_write)
+    grid_launch_next();                  // (see f4_write_pending)
     const uint4 *src = reinterpret_cast<const uint4 *>(x + (size_t)blockIdx.x * ldx);
     uint32_t top = 0u;
     for (int i = threadIdx.x; i < K / 8; i += 32 * kRowsWarps) top = max(top, finite_top<T>(ld_dependent(src + i)));
@@ -385,10 +364,30 @@ static tman_status launch_quantize_as(const void *xv, int ldx, int rows, int K, 
     }
 }
 
+// All kernels that write a packed matrix and let their successor start: argument `at` is the matrix.
+struct F4Quantizer { const void *kernel; int at; };
+template <typename T> static bool quantizer_writes(const cudaKernelNodeParams &node, const void *packed)
+{
+    static const F4Quantizer all[] = {
+        {(const void *)f4_quantize_kernel<32, T, 4>, 4},     {(const void *)f4_quantize_kernel<32, T, 8>, 4},     {(const void *)f4_quantize_kernel<16, T, 8>, 4},
+        {(const void *)f4_quantize16_kernel<T, 1, 1024>, 4}, {(const void *)f4_quantize16_kernel<T, 3, 1024>, 4}, {(const void *)f4_quantize16_kernel<T, 1, 256>, 4},
+        {(const void *)f4_quantize16_kernel<T, 2, 256>, 4},  {(const void *)f4_quantize16_kernel<T, 4, 256>, 4},  {(const void *)f4_quantize16_kernel<T, 7, 256>, 4},
+        {(const void *)f4_quantize16_kernel<T, 10, 256>, 4}, {(const void *)f4_quantize16_kernel<T, 16, 256>, 4}, {(const void *)f4_row_scales_kernel<T>, 3}};
+    for (const F4Quantizer &q : all)
+        if (node.func == q.kernel) return *static_cast<const void *const *>(node.kernelParams[q.at]) == packed;
+    return false;
+}
+
+static F4Order g_f4_order;
+
+bool f4_write_pending(cudaStream_t s, const void *packed)
+{
+    return g_f4_order.pending(s, packed, [](const cudaKernelNodeParams &node, const void *w) { return quantizer_writes<__half>(node, w) || quantizer_writes<__nv_bfloat16>(node, w); });
+}
+
 tman_status launch_f4_quantize(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, cudaStream_t s)
 {
-    const tman_status noted = note_f4_write(s, packed);
-    if (noted != TMAN_OK) return noted;
+    if (!g_f4_order.note(s, packed)) return TMAN_ERR_CUDA;
     if (dtype == kF4TypeHalf) return block == 32 ? launch_quantize_as<32, __half>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __half>(x, ldx, rows, K, packed, s);
     return block == 32 ? launch_quantize_as<32, __nv_bfloat16>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __nv_bfloat16>(x, ldx, rows, K, packed, s);
 }
@@ -400,7 +399,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) f4_dequant_kernel(const uint8
                                                                      uint32_t *status)
 {
     grid_wait();
-    grid_launch_next();                  // (see note_f4_write)
+    grid_launch_next();                  // (see f4_write_pending)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q = lane & 3;
     const int part = blockIdx.x % parts, g = blockIdx.x / parts, row = g * 8 + r, u = part * kRowsWarps + warp;      // unit
     const int chunks = min(8, L.halves * 4 - u * 8);
