@@ -17,6 +17,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "f4_order.h"
 
 #include <cuda_bf16.h>
 
@@ -161,8 +162,9 @@ tman_status launch_f4_unpack(const void *packed, int rows, int K, int block, uin
                              cudaStream_t s);
 tman_status launch_f4_quantize(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, cudaStream_t s);
 tman_status launch_f4_dequant(const void *packed, int rows, int K, int block, void *x, int ldx, int dtype, uint32_t *status, cudaStream_t s);
-// Whether a quantization ahead of the next launch on s may still be writing `packed`; asked once by a launch that reads it as weights.
-bool        f4_write_pending(cudaStream_t s, const void *packed);
+// A launch that reads `packed` as weights: whether a quantization ahead of it on s may still be writing them (call.pending), and that it was launched.
+F4Order::Call f4_read_ahead(cudaStream_t s, const void *packed);
+void          f4_read_behind(const F4Order::Call &call, bool launched);
 size_t      f4_workspace_bytes(int op, int M, int K, int N, int block);
 tman_status launch_f4_gemv(const void *packed, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N, int block, void *ws, cudaStream_t s);
 tman_status launch_f4_gemm(const void *packed, const void *a, void *y, int ldy, int dtype, int M, int K, int N, int block, void *ws, cudaStream_t s);

@@ -11,27 +11,42 @@ namespace tman {
 
 class F4Marks {
 public:
+    // A quantization: begin, its launch, then note, or drop if the launch failed.  Threads that share a stream may have several of them between
+    // begin and note, and the order of their launches is not that of these calls: then whichever is asked for may be the last one, until one
+    // alone has gone through.
     // handle: the cudaStream_t's bits; 1 is the legacy default stream by name, 2 the calling thread's
+    void begin(int device, uintptr_t handle)
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        Mark &m = at(key(device, handle));
+        m.mixed = m.writing++ > 0;
+    }
     void note(int device, uintptr_t handle, const void *packed)
     {
-        const Key k = key(device, handle);
         std::lock_guard<std::mutex> lock(mutex_);
-        for (Mark &m : marks_)
-            if (m.key == k) { m.packed = packed; return; }
-        marks_.push_back({k, packed});
+        Mark &m = at(key(device, handle));
+        if (m.writing > 0) --m.writing;
+        m.packed = packed;
     }
-    enum Found { kNone, kElsewhere, kHere };      // kHere: on this stream, and forgotten now
-    Found take(int device, uintptr_t handle, const void *packed)
+    void drop(int device, uintptr_t handle)
     {
-        const Key k = key(device, handle);
-        Found found = kNone;
         std::lock_guard<std::mutex> lock(mutex_);
-        for (Mark &m : marks_) {
-            if (m.packed != packed) continue;
-            if (m.key == k) { m.packed = nullptr; return kHere; }
-            if (m.key.device == device) found = kElsewhere;
-        }
-        return found;
+        Mark &m = at(key(device, handle));
+        if (m.writing > 0) --m.writing;
+        m.mixed = true;                           // (what was launched before may be the last one still)
+    }
+    // A product: find, its launch, then take.  (A mark taken ahead of the launch would let another thread's product of the same weights go first,
+    // early.)
+    enum Found { kNone, kElsewhere, kHere };      // kHere: on this stream
+    Found find(int device, uintptr_t handle, const void *packed)
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        return look(key(device, handle), packed, false);
+    }
+    Found take(int device, uintptr_t handle, const void *packed)      // and forgotten
+    {
+        std::lock_guard<std::mutex> lock(mutex_);
+        return look(key(device, handle), packed, true);
     }
 
 private:
@@ -46,7 +61,32 @@ private:
         if (handle == 1) handle = 0;
         return {device, handle, handle == 2 ? std::this_thread::get_id() : std::thread::id()};
     }
-    struct Mark { Key key; const void *packed; };
+    struct Mark {
+        Key key;
+        const void *packed;
+        int writing;                              // quantizations between begin and note
+        bool mixed;                               // some of them were there together
+    };
+    Mark &at(const Key &k)
+    {
+        for (Mark &m : marks_)
+            if (m.key == k) return m;
+        marks_.push_back({k, nullptr, 0, false});
+        return marks_.back();
+    }
+    Found look(const Key &k, const void *packed, bool forget)
+    {
+        Found found = kNone;
+        for (Mark &m : marks_) {
+            if (m.key == k) {
+                const bool unsure = m.writing > 0 || m.mixed, here = m.packed == packed;
+                if (here && forget) m.packed = nullptr;
+                if (here || unsure) return kHere;
+            } else if (m.packed == packed && m.key.device == k.device)
+                found = kElsewhere;
+        }
+        return found;
+    }
     std::mutex mutex_;
     std::vector<Mark> marks_;
 };

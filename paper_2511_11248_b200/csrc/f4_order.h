@@ -18,26 +18,40 @@ public:
     // Whether the kernel of a graph node is a quantization that writes `packed`.
     using Writes = bool (*)(const cudaKernelNodeParams &node, const void *packed);
 
-    // A quantization of `packed` is about to be launched on s.  False: a CUDA call failed.
-    bool note(cudaStream_t s, const void *packed)
+    struct Call {
+        const void *packed;
+        int device;
+        uintptr_t handle;
+        bool captured, pending;                  // pending (of a product): it has to wait for all of what is ahead
+    };
+
+    // A quantization of `packed` on s: begin, the launch, end.  False: a CUDA call failed, nothing to launch or to end.
+    bool begin(cudaStream_t s, const void *packed, Call &c)
     {
         noted_.store(true, std::memory_order_release);
-        int dev = 0;
-        bool capturing = false;
-        if (!state(s, dev, capturing)) return false;
-        if (!capturing) marks_.note(dev, reinterpret_cast<uintptr_t>(s), packed);
+        if (!state(s, packed, c)) return false;
+        if (!c.captured) marks_.begin(c.device, c.handle);
         return true;
     }
-    // Whether a product of `packed` on s has to wait for all of what is ahead; asked once a launch.
-    bool pending(cudaStream_t s, const void *packed, Writes writes)
+    void end(const Call &c, bool launched)
     {
-        if (!noted_.load(std::memory_order_acquire)) return false;      // nothing quantized in this process: no lock
-        int dev = 0;
-        bool capturing = false;
-        if (!state(s, dev, capturing)) return true;
-        if (capturing) return captured_behind(s, packed, writes);
+        if (c.captured) return;
+        if (launched) marks_.note(c.device, c.handle, c.packed);
+        else marks_.drop(c.device, c.handle);
+    }
+    // A product of `packed` on s: ahead, the launch, behind.
+    Call ahead(cudaStream_t s, const void *packed, Writes writes)
+    {
+        Call c = {};
+        if (!noted_.load(std::memory_order_acquire)) return c;      // nothing quantized in this process: no lock
+        if (!state(s, packed, c)) { c.captured = c.pending = true; return c; }
         // (Another stream's quantization is ordered before the product by an event, a replayed one by the end of its graph: full dependencies.)
-        return marks_.take(dev, reinterpret_cast<uintptr_t>(s), packed) == F4Marks::kHere;
+        c.pending = c.captured ? captured_behind(s, packed, writes) : marks_.find(c.device, c.handle, packed) == F4Marks::kHere;
+        return c;
+    }
+    void behind(const Call &c, bool launched)
+    {
+        if (launched && c.pending && !c.captured) (void)marks_.take(c.device, c.handle, c.packed);
     }
 
 private:
@@ -46,11 +60,12 @@ private:
         if (e != cudaSuccess) (void)cudaGetLastError();
         return e == cudaSuccess;
     }
-    static bool state(cudaStream_t s, int &dev, bool &capturing)
+    static bool state(cudaStream_t s, const void *packed, Call &c)
     {
         cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
-        if (!ok(cudaGetDevice(&dev)) || !ok(cudaStreamIsCapturing(s, &st))) return false;
-        capturing = st != cudaStreamCaptureStatusNone;
+        c = {packed, 0, reinterpret_cast<uintptr_t>(s), false, false};
+        if (!ok(cudaGetDevice(&c.device)) || !ok(cudaStreamIsCapturing(s, &st))) return false;
+        c.captured = st != cudaStreamCaptureStatusNone;
         return true;
     }
     // Only a kernel can let its successor start early; one that this library does not know by its function is no quantization.

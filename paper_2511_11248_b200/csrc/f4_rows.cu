@@ -1,7 +1,6 @@
 // Microscaled 4-bit floating point: packing and unpacking of a checkpoint's matrix, quantization of rows, dequantization.
 // Memory-bound: every value is read and written once.
 #include "f4.cuh"
-#include "f4_order.h"
 #include "sm100_ptx.cuh"
 
 #include <type_traits>
@@ -86,7 +85,7 @@ tman_status launch_f4_unpack(const void *packed, int rows, int K, int block, uin
 // ---- quantization of rows ----------------------------------------------------------------------
 // The kernels let their successor start once their predecessor has ended, so that a product behind them fetches its weights meanwhile; what they
 // write is read only behind the successor's wait.  Unless it is the successor's weights: such a product is launched in plain stream order
-// (f4_write_pending).  (An earlier quantization has ended when a later one has let anything start.)
+// (f4_read_ahead).  (An earlier quantization has ended when a later one has let anything start.)
 
 // One block's scale byte and the codes of eight of its values.  top: the largest magnitude of the block; fine: all its values are finite;
 // inv_row: 1 / r, a power of two.
@@ -171,7 +170,7 @@ template <int BLOCK, typename T, int V>
 __global__ void __launch_bounds__(32 * kRowsWarps) f4_quantize_kernel(const T *x, int ldx, int rows, int K, uint8_t *packed, const __grid_constant__ F4Layout L, int parts)
 {
     grid_wait();
-    grid_launch_next();                  // (see f4_write_pending)
+    grid_launch_next();                  // (see f4_read_ahead)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q = lane & 3;
     const int part = blockIdx.x % parts, g = blockIdx.x / parts, row = g * 8 + r;
     if (blockIdx.x == 0 && threadIdx.x < 64) reinterpret_cast<uint32_t *>(packed)[threadIdx.x] = f4_header_word(threadIdx.x, rows, K, BLOCK, L);
@@ -235,7 +234,7 @@ __global__ void __launch_bounds__(THREADS) f4_quantize16_kernel(const T *x, int 
     constexpr int WARPS = THREADS / 32;
     __shared__ uint32_t tops[WARPS];
     grid_wait();
-    grid_launch_next();                  // (see f4_write_pending)
+    grid_launch_next();                  // (see f4_read_ahead)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
     if (blockIdx.x == 0 && threadIdx.x < 64) reinterpret_cast<uint32_t *>(packed)[threadIdx.x] = f4_header_word(threadIdx.x, rows, K, 16, L);
     const uint4 *src = reinterpret_cast<const uint4 *>(x + (size_t)row * ldx) + threadIdx.x;
@@ -301,7 +300,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) f4_row_scales_kernel(const T 
 {
     __shared__ uint32_t tops[kRowsWarps];
     grid_wait();
-    grid_launch_next();                  // (see f4_write_pending)
+    grid_launch_next();                  // (see f4_read_ahead)
     const uint4 *src = reinterpret_cast<const uint4 *>(x + (size_t)blockIdx.x * ldx);
     uint32_t top = 0u;
     for (int i = threadIdx.x; i < K / 8; i += 32 * kRowsWarps) top = max(top, finite_top<T>(ld_dependent(src + i)));
@@ -380,16 +379,21 @@ template <typename T> static bool quantizer_writes(const cudaKernelNodeParams &n
 
 static F4Order g_f4_order;
 
-bool f4_write_pending(cudaStream_t s, const void *packed)
+F4Order::Call f4_read_ahead(cudaStream_t s, const void *packed)
 {
-    return g_f4_order.pending(s, packed, [](const cudaKernelNodeParams &node, const void *w) { return quantizer_writes<__half>(node, w) || quantizer_writes<__nv_bfloat16>(node, w); });
+    return g_f4_order.ahead(s, packed, [](const cudaKernelNodeParams &node, const void *w) { return quantizer_writes<__half>(node, w) || quantizer_writes<__nv_bfloat16>(node, w); });
 }
+void f4_read_behind(const F4Order::Call &call, bool launched) { g_f4_order.behind(call, launched); }
 
 tman_status launch_f4_quantize(const void *x, int ldx, int dtype, int rows, int K, int block, void *packed, cudaStream_t s)
 {
-    if (!g_f4_order.note(s, packed)) return TMAN_ERR_CUDA;
-    if (dtype == kF4TypeHalf) return block == 32 ? launch_quantize_as<32, __half>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __half>(x, ldx, rows, K, packed, s);
-    return block == 32 ? launch_quantize_as<32, __nv_bfloat16>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __nv_bfloat16>(x, ldx, rows, K, packed, s);
+    F4Order::Call call;
+    if (!g_f4_order.begin(s, packed, call)) return TMAN_ERR_CUDA;
+    tman_status st;
+    if (dtype == kF4TypeHalf) st = block == 32 ? launch_quantize_as<32, __half>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __half>(x, ldx, rows, K, packed, s);
+    else st = block == 32 ? launch_quantize_as<32, __nv_bfloat16>(x, ldx, rows, K, packed, s) : launch_quantize_as<16, __nv_bfloat16>(x, ldx, rows, K, packed, s);
+    g_f4_order.end(call, st == TMAN_OK);
+    return st;
 }
 
 // ---- dequantization -----------------------------------------------------------------------------
@@ -399,7 +403,7 @@ __global__ void __launch_bounds__(32 * kRowsWarps) f4_dequant_kernel(const uint8
                                                                      uint32_t *status)
 {
     grid_wait();
-    grid_launch_next();                  // (see f4_write_pending)
+    grid_launch_next();                  // (see f4_read_ahead)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q = lane & 3;
     const int part = blockIdx.x % parts, g = blockIdx.x / parts, row = g * 8 + r, u = part * kRowsWarps + warp;      // unit
     const int chunks = min(8, L.halves * 4 - u * 8);

@@ -457,8 +457,11 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     // (also a cluster of one: without the attribute the next call's CTAs do not spread over the SMs, 1 x 3584 x 18944 7.1 -> 8.9 us)
     cfg.attrs = attr;
-    cfg.numAttrs = packed_write_pending(s, /*clear=*/true) || f4_write_pending(s, p.w) ? 1 : 2;
-    return launch_with_smem(kern, kStreamAllSm, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
+    const F4Order::Call call = f4_read_ahead(s, p.w);
+    cfg.numAttrs = packed_write_pending(s, /*clear=*/true) || call.pending ? 1 : 2;
+    const tman_status st = launch_with_smem(kern, kStreamAllSm, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
+    f4_read_behind(call, st == TMAN_OK);
+    return st;
 }
 
 }  // namespace

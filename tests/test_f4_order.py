@@ -34,6 +34,10 @@ using namespace tman;
 static int quantizer, w, a, v;
 static bool writes(const cudaKernelNodeParams &n, const void *packed) { return n.func == &quantizer && *(void **)n.kernelParams[4] == packed; }
 static cudaStream_t stream(size_t h) { return (cudaStream_t)h; }
+struct Order : F4Order {                                     // calls whose launches succeed, by one thread
+    bool note(cudaStream_t s, const void *packed) { Call c; if (!begin(s, packed, c)) return false; end(c, true); return true; }
+    bool pending(cudaStream_t s, const void *packed, Writes writes) { const Call c = ahead(s, packed, writes); behind(c, true); return c.pending; }
+};
 """
 
 
@@ -53,7 +57,7 @@ def run(tmp_path):
 
 def test_a_captured_product_leaves_the_mark_of_an_eager_quantization(run):
     run("""
-F4Order o;
+Order o;
 REQUIRE(!o.pending(stream(64), &w, writes));
 REQUIRE(o.note(stream(64), &w));                         // eager quantization of w
 g_capturing = true;
@@ -65,7 +69,7 @@ REQUIRE(!o.pending(stream(64), &w, writes));""")
 
 def test_a_captured_quantization_does_not_replace_the_mark_of_an_eager_one(run):
     run("""
-F4Order o;
+Order o;
 REQUIRE(o.note(stream(64), &w));
 g_capturing = true;
 REQUIRE(o.note(stream(64), &a));
@@ -75,7 +79,7 @@ REQUIRE(!o.pending(stream(64), &a, writes) && o.pending(stream(64), &w, writes))
 
 def test_a_captured_product_asks_the_nodes_ahead_of_it(run):
     run("""
-F4Order o;
+Order o;
 void *pw = &w, *pa = &a;
 Node qw = {cudaGraphNodeTypeKernel, cudaSuccess, &quantizer, {0, 0, 0, 0, &pw}}, qa = {cudaGraphNodeTypeKernel, cudaSuccess, &quantizer, {0, 0, 0, 0, &pa}},
      other = {cudaGraphNodeTypeKernel, cudaSuccess, &v, {0, 0, 0, 0, &pw}}, foreign = {cudaGraphNodeTypeKernel, cudaErrorInvalidDeviceFunction, nullptr, {}},
@@ -91,7 +95,44 @@ REQUIRE(ahead({&odd}));                                  // not known: plain ord
 
 def test_a_runtime_that_fails_means_plain_order(run):
     run("""
-F4Order o;
+Order o;
 REQUIRE(o.note(stream(64), &a));
 g_error = cudaErrorOther;
 REQUIRE(!o.note(stream(64), &w) && o.pending(stream(64), &v, writes));""")
+
+
+def test_quantizations_of_two_threads_on_one_stream(run):
+    """Begun in one order and launched in the other: the product of either waits, until a quantization has gone through alone."""
+    run("""
+Order o;
+F4Order::Call cw, ca;
+REQUIRE(o.begin(stream(64), &w, cw) && o.begin(stream(64), &a, ca));
+REQUIRE(o.pending(stream(64), &w, writes));               // under way
+o.end(cw, true); o.end(ca, true);                         // (launched the other way around)
+REQUIRE(o.pending(stream(64), &w, writes) && o.pending(stream(64), &a, writes) && o.pending(stream(64), &w, writes));
+REQUIRE(!o.pending(stream(128), &w, writes));
+REQUIRE(o.note(stream(64), &a));
+REQUIRE(!o.pending(stream(64), &w, writes) && o.pending(stream(64), &a, writes) && !o.pending(stream(64), &a, writes));""")
+
+
+def test_a_mark_is_taken_when_its_product_has_been_launched(run):
+    """Two threads' products of the same weights behind one quantization: whichever is launched first waits for it."""
+    run("""
+Order o;
+REQUIRE(o.note(stream(64), &w));
+const F4Order::Call one = o.ahead(stream(64), &w, writes), two = o.ahead(stream(64), &w, writes);
+REQUIRE(one.pending && two.pending);
+o.behind(two, false);                                     // its launch failed
+REQUIRE(o.ahead(stream(64), &w, writes).pending);
+o.behind(one, true);
+REQUIRE(!o.ahead(stream(64), &w, writes).pending);""")
+
+
+def test_a_quantization_whose_launch_failed_hides_no_other(run):
+    run("""
+Order o;
+F4Order::Call c;
+REQUIRE(o.note(stream(64), &w));
+REQUIRE(o.begin(stream(64), &a, c));
+o.end(c, false);
+REQUIRE(o.pending(stream(64), &w, writes));""")
