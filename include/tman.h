@@ -5,8 +5,10 @@
  *
  * Conventions for every call
  *   - All data pointers are DEVICE pointers owned by the caller unless a parameter says "host".
- *   - Nothing is allocated, nothing is kept between calls, the device is never synchronised
- *     (except tman_read_status), all work is enqueued on `stream`.
+ *   - Nothing is allocated on the device, no data is kept between calls, the device is never synchronised
+ *     (except tman_read_status), all work is enqueued on `stream`.  What the host keeps in the process is which
+ *     streams a packing or a quantization to 4 bits has lately been enqueued on, for the order of the calls
+ *     behind them.
  *   - The return value is a tman_status.  Argument errors are reported before anything is
  *     enqueued.  Errors only the device can see (a packed buffer whose header does not match
  *     the arguments, a bounded wait that ran out) are written to the first 32-bit word of the

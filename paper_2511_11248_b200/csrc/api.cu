@@ -1,5 +1,6 @@
-// C ABI: argument validation and dispatch.  No allocation, no global state, no device sync
-// (except tman_read_status, whose job is to wait).
+// C ABI: argument validation and dispatch.  No allocation, no device sync (except tman_read_status, whose job is
+// to wait); the only state beside cached device properties is which streams were lately packed or quantized on
+// (pack.cu, f4_marks.h).
 #include "common.cuh"
 #include "f4.cuh"
 

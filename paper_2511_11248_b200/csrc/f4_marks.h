@@ -1,11 +1,11 @@
 // Which packed buffer the last eager quantization of each stream wrote.  A stream is a handle on a device: the default stream's handle is the same on every
-// device, and the per-thread one's in every thread.
+// device, and the per-thread one's in every thread.  The table has a fixed size and allocates nothing: the stream that was not used for longest makes
+// room for a new one, and from then on a stream that is not there counts as one whose last quantization is not known.
 #pragma once
 
 #include <cstdint>
 #include <mutex>
 #include <thread>
-#include <vector>
 
 namespace tman {
 
@@ -46,7 +46,10 @@ public:
     Found take(int device, uintptr_t handle, const void *packed)      // and forgotten
     {
         std::lock_guard<std::mutex> lock(mutex_);
-        return look(key(device, handle), packed, true);
+        const Key k = key(device, handle);
+        const Found found = look(k, packed, true);
+        if (lost_ && !slot(k)) at(k).mixed = false;      // (behind a product in plain order nothing is under way)
+        return found;
     }
 
 private:
@@ -65,30 +68,47 @@ private:
         Key key;
         const void *packed;
         int writing;                              // quantizations between begin and note
-        bool mixed;                               // some of them were there together
+        bool mixed;                               // some of them were there together, or what was there is not known
+        uint64_t used;                            // 0: free
     };
-    Mark &at(const Key &k)
+    Mark *slot(const Key &k)
     {
         for (Mark &m : marks_)
-            if (m.key == k) return m;
-        marks_.push_back({k, nullptr, 0, false});
-        return marks_.back();
+            if (m.used && m.key == k) {
+                m.used = ++clock_;
+                return &m;
+            }
+        return nullptr;
+    }
+    Mark &at(const Key &k)
+    {
+        if (Mark *m = slot(k)) return *m;
+        Mark *to = nullptr;
+        for (Mark &m : marks_)
+            if (m.writing == 0 && (!to || m.used < to->used)) to = &m;
+        const bool unknown = lost_;
+        if (!to) to = &spare_;                    // (every stream of the table is between begin and note: this one is not kept)
+        if (to == &spare_ || to->packed || to->mixed) lost_ = true;
+        *to = {k, nullptr, 0, unknown, ++clock_};
+        return *to;
     }
     Found look(const Key &k, const void *packed, bool forget)
     {
-        Found found = kNone;
-        for (Mark &m : marks_) {
-            if (m.key == k) {
-                const bool unsure = m.writing > 0 || m.mixed, here = m.packed == packed;
-                if (here && forget) m.packed = nullptr;
-                if (here || unsure) return kHere;
-            } else if (m.packed == packed && m.key.device == k.device)
-                found = kElsewhere;
-        }
-        return found;
+        if (Mark *m = slot(k)) {
+            const bool here = m->packed == packed;
+            if (here && forget) m->packed = nullptr;
+            if (here || m->writing > 0 || m->mixed) return kHere;
+        } else if (lost_)
+            return kHere;
+        for (const Mark &m : marks_)
+            if (m.used && m.packed == packed && m.key.device == k.device) return kElsewhere;
+        return kNone;
     }
+    static constexpr int kStreams = 64;
     std::mutex mutex_;
-    std::vector<Mark> marks_;
+    Mark marks_[kStreams] = {}, spare_ = {};
+    uint64_t clock_ = 0;
+    bool lost_ = false;                           // a stream with a mark has made room
 };
 
 }  // namespace tman

@@ -27,7 +27,9 @@ inline cudaError_t cudaGraphKernelNodeGetParams(cudaGraphNode_t n, cudaKernelNod
 
 PRELUDE = """
 #include "f4_order.h"
+#include <initializer_list>
 #include <thread>
+#include <type_traits>
 #define REQUIRE(c) do { if (!(c)) return __LINE__; } while (0)
 int g_device = 0; bool g_capturing = false; cudaError_t g_error = cudaSuccess; cudaGraphNode_t g_ahead[4]; size_t g_n = 0;
 using namespace tman;
@@ -136,3 +138,28 @@ REQUIRE(o.note(stream(64), &w));
 REQUIRE(o.begin(stream(64), &a, c));
 o.end(c, false);
 REQUIRE(o.pending(stream(64), &w, writes));""")
+
+
+def test_more_streams_than_the_table_holds(run):
+    """Nothing is allocated, and a stream that had to make room is one whose products wait: once, then they know that nothing is under way."""
+    run("""
+static_assert(std::is_trivially_destructible<F4Marks>::value, "no memory of its own");
+Order o;
+for (size_t s = 1; s <= 64; ++s) REQUIRE(o.note(stream(64 * s), &w));
+REQUIRE(!o.pending(stream(64 * 100), &a, writes));        // a stream without quantizations
+REQUIRE(o.note(stream(64 * 65), &w));                     // the first one made room
+REQUIRE(o.ahead(stream(64), &w, writes).pending && o.pending(stream(64), &a, writes));
+REQUIRE(!o.pending(stream(64), &a, writes) && !o.pending(stream(64), &w, writes));
+for (size_t s = 66; s <= 400; ++s) REQUIRE(o.note(stream(64 * s), &w) && o.ahead(stream(64 * s), &w, writes).pending);
+for (size_t s = 1; s <= 400; ++s) REQUIRE(o.pending(stream(64 * s), &w, writes) && !o.pending(stream(64 * s), &w, writes));""")
+
+
+def test_more_threads_in_a_quantization_than_the_table_holds(run):
+    run("""
+Order o;
+F4Order::Call c[80];
+for (size_t s = 0; s < 80; ++s) REQUIRE(o.begin(stream(64 * (s + 1)), &w, c[s]));
+for (size_t s = 0; s < 80; ++s) REQUIRE(o.ahead(stream(64 * (s + 1)), &w, writes).pending);
+for (size_t s = 0; s < 80; ++s) { o.end(c[s], true); REQUIRE(o.ahead(stream(64 * (s + 1)), &w, writes).pending); }
+for (size_t s = 0; s < 80; ++s) REQUIRE(o.ahead(stream(64 * (s + 1)), &w, writes).pending);
+for (size_t s = 0; s < 80; ++s) REQUIRE(o.note(stream(64 * (s + 1)), &a) && !o.ahead(stream(64 * (s + 1)), &w, writes).pending);""")
