@@ -128,15 +128,8 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
         bad_header = 0u;
     }
     if (threadIdx.x < 8) row_top[threadIdx.x] = 0u;
-    if (warp == 1) {
-        tcgen05_alloc(smem_u32(&tmem_slot), tmem_cols);
-        tcgen05_relinquish();
-    }
-    tcgen05_fence_before();
     __syncthreads();
     cluster_arrive();                    // (waited for before the sums are sent)
-    tcgen05_fence_after();
-    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
 
     // (Warps 0 and 1 walk as one, one lane issues: addresses and descriptors in uniform registers.)
     if (warp == 0) {
@@ -178,6 +171,14 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
             if (++s == p.stages) { s = 0; ph ^= 1u; }
         }
     } else if (warp == 1) {
+        // Tensor memory is taken behind the wait for the kernel ahead, which may be one that signals before it takes its own (each would wait for
+        // the other), and before the signal to the next.
+        grid_wait();
+        tcgen05_alloc(smem_u32(&tmem_slot), tmem_cols);
+        tcgen05_relinquish();
+        grid_launch_next();
+        __syncwarp();
+        const uint32_t tmem = __shfl_sync(0xffffffffu, *const_cast<volatile uint32_t *>(&tmem_slot), 0);
         const bool lead = elect_one();
         const uint32_t id0 = f4_idesc(BLOCK, 128, p.cols, 0), id1 = f4_idesc(BLOCK, 128, p.cols, BLOCK == 32 ? 2 : 0);
         const uint64_t sf0 = make_kmajor_desc(ring, 128, 128);                     // (+ 1: 16 bytes)
@@ -231,7 +232,6 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
         }
         if (BLOCK == 16 && pt < 128 && tile * 128 + pt < p.N) row_scale = __ldcg(reinterpret_cast<const float *>(p.w + p.w_rows) + tile * 128 + pt);
         grid_wait();
-        grid_launch_next();
         if constexpr (!DIGITS) {
             if (pt == 32 && !f4_header_matches(p.a, p.M, p.K, BLOCK)) bad_header = 1u;
             if (BLOCK == 16 && pt < p.M) a_row[pt] = ld_dependent(reinterpret_cast<const float *>(p.a + p.a_rows) + pt);
@@ -337,8 +337,11 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     }
 
     // ---- epilogue: warps 2..5, a channel a lane -------------------------------------------------
+    tcgen05_fence_before();
     __syncthreads();                     // row scales and the rest in shared memory are there; roles are done
     cluster_wait();
+    tcgen05_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     const bool hdr_ok = bad_header == 0u;
     if (!hdr_ok && threadIdx.x == 64 && blockIdx.x == 0) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_BAD_PACKED);
     T *y = static_cast<T *>(p.y);

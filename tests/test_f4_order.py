@@ -163,3 +163,21 @@ for (size_t s = 0; s < 80; ++s) REQUIRE(o.ahead(stream(64 * (s + 1)), &w, writes
 for (size_t s = 0; s < 80; ++s) { o.end(c[s], true); REQUIRE(o.ahead(stream(64 * (s + 1)), &w, writes).pending); }
 for (size_t s = 0; s < 80; ++s) REQUIRE(o.ahead(stream(64 * (s + 1)), &w, writes).pending);
 for (size_t s = 0; s < 80; ++s) REQUIRE(o.note(stream(64 * (s + 1)), &a) && !o.ahead(stream(64 * (s + 1)), &w, writes).pending);""")
+
+
+@pytest.mark.parametrize("name,alloc", [("f4_stream.cuh", "tcgen05_alloc("), ("f4_pair.cuh", "tcgen05_alloc2(")])
+def test_tensor_memory_is_taken_behind_the_wait_and_ahead_of_the_signal(name, alloc):
+    """A kernel ahead may signal before it takes its own tensor memory: with this kernel's taken ahead of the wait, each would wait for the other.
+    Read from the source, since a run that shows it would hang."""
+    import os
+    import re
+    from paper_2511_11248_b200 import build
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(build.CSRC, name)).read())
+    body = re.search(r"__global__ void[^;{]*?_kernel\s*\([^)]*\)\s*\{(.*?)\n\}", text, re.S)[1]
+    assert body.count(alloc) == 1 and body.count("grid_launch_next();") == 1
+    at = body.index(alloc)
+    # the last thing that this warp does before it is the wait: in its own branch, or in front of all branches
+    before = body[:at]
+    wait, branch = before.rindex("grid_wait();"), max(before.rfind("} else if (warp == 1) {"), before.rfind("    if (warp == 1) {"))
+    assert wait > branch or "if (" not in before[wait:branch].replace("if (warp == 1) {", "")
+    assert at < body.index("grid_launch_next();")
