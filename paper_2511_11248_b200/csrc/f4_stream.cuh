@@ -96,6 +96,24 @@ __device__ __forceinline__ void digit_codes(const uint32_t (&y)[8], uint32_t (&o
     bytes(hi, out + 4);
 }
 
+// Row scales of weights as a power of two times what is left of them: 1 to 2, or all of what is not an ordinary number.
+__device__ __forceinline__ int scale_exponent(float s)
+{
+    const int e = (int)(__float_as_uint(s) >> 23 & 255u);
+    return e == 0 || e == 255 ? 0 : e - 127;
+}
+__device__ __forceinline__ float scale_rest(float s)
+{
+    const uint32_t u = __float_as_uint(s), e = u >> 23 & 255u;
+    return e == 0u || e == 255u ? s : __uint_as_float((u & 0x807FFFFFu) | 0x3F800000u);
+}
+// v 2^e, e from -252 to 254: exact where the result is an ordinary number.
+__device__ __forceinline__ float times_power(float v, int e)
+{
+    const int h = e >> 1;
+    return v * __uint_as_float((uint32_t)(h + 127) << 23) * __uint_as_float((uint32_t)(e - h + 127) << 23);
+}
+
 template <int BLOCK, typename T, bool DIGITS>
 __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_stream_kernel(const __grid_constant__ F4StreamParams p)
 {
@@ -353,11 +371,14 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
         const uint32_t acc = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const bool put = ok && hdr_ok && n < p.N;
         const float wr = BLOCK == 16 ? w_row[ch] : 1.f;
+        // (Digits' sums are of x over a power of two of the row.  That, and the power of two in the weights' row scale, come back in one step: in turn
+        // they may leave the range where their product does not.  Powers of two change no rounding.)
+        [[maybe_unused]] const int w_exp = scale_exponent(wr);
         const int to = ch / per;
         const uint32_t to_sums = mapa_u32(smem_u32(sums), (uint32_t)to) + (uint32_t)((rank * p.M) * per + ch - to * per) * 4u, to_bar = mapa_u32(smem_u32(&sums_bar), (uint32_t)to);
         auto give = [&](int m, float v) {
             if (push) store_cluster(to_sums + (uint32_t)(m * per) * 4u, v, to_bar);
-            else if (put) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * wr * (DIGITS ? 1.f : a_row[m]) : v);
+            else if (put) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? (DIGITS ? v * scale_rest(wr) : v * wr * a_row[m]) : v);
         };
         if constexpr (DIGITS) {
 #pragma unroll 1
@@ -368,8 +389,9 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                 float v = __uint_as_float(r[0]);
 #pragma unroll
                 for (int e = 1; e < 8; ++e) v = fmaf(v, 0.125f, __uint_as_float(r[e]));
-                if constexpr (BLOCK == 16) v *= __uint_as_float((uint32_t)max((int)(__float_as_uint(f4_to_float2<T>(row_top[m]).x) >> 23) - 8, 16) << 23);
-                give(m, v * 4.f);
+                if constexpr (BLOCK == 16) v = times_power(v, max((int)(__float_as_uint(f4_to_float2<T>(row_top[m]).x) >> 23) - 8, 16) - 127 + 2 + w_exp);
+                else v *= 4.f;
+                give(m, v);
             }
         } else {
 #pragma unroll 1
@@ -393,7 +415,8 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
             const int m = i / own_n, c = i - m * own_n, n = tile * 128 + own0 + c;
             float v = 0.f;
             for (int r = 0; r < p.split; ++r) v += sums[(r * p.M + m) * per + c];
-            if (ok && hdr_ok && n < p.N) y[(size_t)m * p.ldy + n] = f4_from_float<T>(BLOCK == 16 ? v * w_row[own0 + c] * (DIGITS ? 1.f : a_row[m]) : v);
+            if constexpr (BLOCK == 16) v = DIGITS ? v * scale_rest(w_row[own0 + c]) : v * w_row[own0 + c] * a_row[m];
+            if (ok && hdr_ok && n < p.N) y[(size_t)m * p.ldy + n] = f4_from_float<T>(v);
         }
     }
     if (!ok) atomicCAS(p.status, 0u, (uint32_t)TMAN_ERR_TIMEOUT);
