@@ -8,9 +8,9 @@
 // DIGITS: x in 16 bits.  The tensor cores multiply e2m1 with e2m1, so a row of x becomes eight columns of balanced octal digits.  In a block of 16
 // or 32 values with largest magnitude in [2^E, 2^(E+1)) every x is the fixed-point number 2^(E-20) X, X = round(x 2^(20-E)) < 2^21, off by
 // at most 2^(E-21); X = sum_j n_j 8^j with eight digits n_j in [-4, 4], and n_j / 2 is an e2m1 value.  Column 8 m + j holds the digits n_j of
-// row m, the block's scale (2^E as e8m0; as e4m3 relative to a power of two of the row) is the columns' block scale, and
-// x w = 4 sum_j 8^(j-7) (column j): products of digits and weights are exact, sums are in fp32.  Sixteen
-// warps cut x up while the weights arrive.
+// row m, the block's scale (2^(E-2) as e8m0; as e4m3 2^E relative to a power of two of the row) is the columns' block scale, and
+// x w = 16 (4) sum_j 8^(j-7) (column j): products of digits and weights are exact, sums are in fp32.  (A column counts up to twice what x
+// does, -4 + 8 for 4; under 2^E the largest numbers of bf16 would leave the range there.)  Sixteen warps cut x up while the weights arrive.
 //
 // Otherwise: x is a packed 4-bit matrix, whose units are loaded as they are.
 //
@@ -304,8 +304,8 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                 uint32_t byte;                                   // the block's scale
                 int e2;                                          // E + 127
                 if constexpr (BLOCK == 32) {
-                    e2 = max((int)eb, std::is_same<T, __half>::value ? 103 : 1);
-                    byte = eb == 255u ? 255u : (uint32_t)e2;
+                    e2 = max((int)eb, std::is_same<T, __half>::value ? 103 : 3);
+                    byte = eb == 255u ? 255u : (uint32_t)e2 - 2u;
                 } else {
                     const uint32_t rt = row_top[m];
                     const int r2 = max((int)(__float_as_uint(f4_to_float2<T>(rt).x) >> 23) - 8, 16);     // the row's power of two, + 127
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
 #pragma unroll
                 for (int e = 1; e < 8; ++e) v = fmaf(v, 0.125f, __uint_as_float(r[e]));
                 if constexpr (BLOCK == 16) v = times_power(v, max((int)(__float_as_uint(f4_to_float2<T>(row_top[m]).x) >> 23) - 8, 16) - 127 + 2 + w_exp);
-                else v *= 4.f;
+                else v *= 16.f;
                 give(m, v);
             }
         } else {

@@ -59,3 +59,18 @@ def test_row_scales_that_are_no_ordinary_numbers():
     x = rng.standard_normal((M, K))
     x[0] *= 1e-4
     check(x * 1e-4, codes, scales, rs, 16, "bf16")
+
+
+@pytest.mark.parametrize("block", [32, 16])
+@pytest.mark.parametrize("M,K,N", SIZES)
+def test_the_largest_rows_times_weights_of_one(M, K, N, block):
+    """Outputs next to the largest number of bf16, each of one activation: a digit's column counts up to twice what the digits together do."""
+    rng = np.random.default_rng(N)
+    K += -K % block
+    x = rng.uniform(1.0, 1.98, (M, K)) * 2.0 ** 127 * rng.choice([-1.0, 1.0], (M, K))
+    x[:, 1::2] = rng.standard_normal((M, K // 2))
+    x[0, ::3] = 2.0 ** 127
+    codes = np.zeros((N, K), np.uint8)
+    codes[np.arange(N), rng.integers(0, K, N)] = rng.choice([2, 10, 1], N)      # 1, -1, 0.5
+    scales = np.full((N, K // block), 127 if block == 32 else 0x38, np.uint8)
+    check(x, codes, scales, np.ones(N, np.float32), block, "bf16")
