@@ -295,9 +295,11 @@ tman_status tman_dequant_rows_f4(const void *packed, size_t packed_bytes, int ro
                                  void *workspace, size_t ws_bytes, tman_stream_t stream);
 
 /* Decode: y[m][n] = sum_k x[m][k] w[n][k] for 16-bit activations, M in [1, 8]; x and y have the type `dtype`.
- * Precision: within a block of k the activations are fixed-point numbers of 22 bits (off by at most 2^-21 of the block's largest
- * magnitude; with block = 16, of 2^-17 of the largest magnitude of the row's share of k that a CTA has, where the block's own is
- * smaller), multiplied with the weights exactly; sums in fp32, in an order that does not depend on timing.  A row with an infinity or a
+ * Precision: within a block of k the activations are fixed-point numbers of 22 bits, multiplied with the weights exactly: an activation is off
+ * by at most 2^-21 of the block's largest magnitude (with block = 16, of 2^-17 of the largest magnitude of the row's share of k that a CTA has,
+ * where the block's own is smaller), or by 2^-141 where that is more (with bf16, whose smallest number is 2^-133).  So a value far below its
+ * neighbours loses bits that its type has: all of them below 2^-22 of the block's largest.  Sums in fp32, in an order that does not depend on
+ * timing; with block = 16 the row scale comes last and brings sums of any size into range.  A row with an infinity or a
  * NaN gives NaN in every channel.  Nothing is kept in the workspace but the status word. */
 tman_status tman_mpgemv_f4(const void *packed, size_t packed_bytes, const void *x, int ldx, void *y, int ldy, int dtype,
                            int M, int K, int N, int block, void *workspace, size_t ws_bytes, tman_stream_t stream);

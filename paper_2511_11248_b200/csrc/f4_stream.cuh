@@ -308,7 +308,8 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
                     byte = eb == 255u ? 255u : (uint32_t)e2 - 2u;
                 } else {
                     const uint32_t rt = row_top[m];
-                    const int r2 = max((int)(__float_as_uint(f4_to_float2<T>(rt).x) >> 23) - 8, 16);     // the row's power of two, + 127
+                    // the row's power of two, + 127 (at least 2^-111: bf16's smallest numbers are then off by 2^-141 at most, a 2^-8 of the least of them)
+                    const int r2 = max((int)(__float_as_uint(f4_to_float2<T>(rt).x) >> 23) - 8, 16);
                     e2 = min(max((int)eb, r2 - 9), r2 + 8);
                     const int d = e2 - r2;                       // -9 .. 8
                     byte = eb == 255u ? 0x7Fu : d >= -6 ? (uint32_t)(d + 7) << 3 : 1u << (d + 9);

@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 def check(x, codes, scales, rs, block, ty, floor=0.0):
     """Half a step of the type, 2^-23 of S = sum |x w| for every addition in 32 bits, the header's 2^-20 of the block's largest value times the weights'
-    magnitudes (2^-17 of the row's where that is more; `floor`: of the smallest magnitudes), and half the type's smallest value."""
+    magnitudes (of 2^-17 of the row's where that is more; `floor`: of the smallest magnitudes), and half the type's smallest value."""
     dtype, code = (torch.float16, B.DTYPE_F16) if ty == "f16" else (torch.bfloat16, B.DTYPE_BF16)
     (M, K), N = x.shape, codes.shape[0]
     packed = pack_on_device(codes, scales, rs, block)
@@ -24,10 +24,9 @@ def check(x, codes, scales, rs, block, ty, floor=0.0):
     ref, S = held @ w.T, np.abs(held) @ np.abs(w).T
     assert np.abs(ref).max() < float(torch.finfo(dtype).max)
     top = np.abs(held).reshape(M, -1, block).max(-1)
-    unit = 2.0 ** -20 * top
     if block == 16:
-        unit = np.maximum(unit, 2.0 ** -17 * top.max(1, keepdims=True))
-    unit = np.maximum(unit, floor)
+        top = np.maximum(top, 2.0 ** -17 * top.max(1, keepdims=True))
+    unit = np.maximum(2.0 ** -20 * top, floor)
     tol = (2.0 ** -8 if ty == "bf16" else 2.0 ** -11) * np.abs(ref) + (K / 64 + 32) * 2.0 ** -23 * S + unit @ np.abs(w).reshape(N, -1, block).sum(-1).T
     tol += 2.0 ** -134 if ty == "bf16" else 2.0 ** -25
     got = f64(y)
@@ -74,3 +73,17 @@ def test_the_largest_rows_times_weights_of_one(M, K, N, block):
     codes[np.arange(N), rng.integers(0, K, N)] = rng.choice([2, 10, 1], N)      # 1, -1, 0.5
     scales = np.full((N, K // block), 127 if block == 32 else 0x38, np.uint8)
     check(x, codes, scales, np.ones(N, np.float32), block, "bf16")
+
+
+@pytest.mark.parametrize("block", [32, 16])
+@pytest.mark.parametrize("M,K,N", SIZES)
+@pytest.mark.parametrize("top", [2.0 ** -100, 2.0 ** -115, 2.0 ** -124, 2.0 ** -128, 2.0 ** -133])
+def test_the_smallest_rows(M, K, N, block, top):
+    """Down to the type's smallest value a block's numbers are as exact as the header says: off by 2^-141 at most where 2^-21 of the
+    block's largest is less."""
+    rng = np.random.default_rng(N + 1)
+    K += -K % block
+    x = rng.uniform(-1.0, 1.0, (M, K)) * top
+    codes = rng.integers(0, 16, (N, K)).astype(np.uint8)
+    scales = rng.integers(150, 156, (N, K // 32)).astype(np.uint8) if block == 32 else rng.integers(0x30, 0x50, (N, K // 16)).astype(np.uint8)
+    check(x, codes, scales, np.full(N, 2.0 ** 25, np.float32), block, "bf16", floor=2.0 ** -141)
