@@ -385,6 +385,16 @@ tman_status tman_debug_gemm_plan_for(int M, int K, int N, int bits, int group, i
 tman_status tman_debug_gemv_plan(int M, int K, int N, int bits, int group, int sms, size_t ws_limit,
                                  int *out /*host*/);
 
+/* How tman_mpgemv_f4 (op 0) or tman_mpgemm_f4 (op 1) would cut a call on the current device (host-side decision, nothing is launched).
+ * out8 (host) receives: 0 if CTAs with a tile of 128 channels each stream the weights, 1 if pairs of CTAs have tiles of 256 channels; rows of x (of
+ * a tile); shares of k of a tile; tiles along the rows; tiles along the channels; CTAs (pairs) launched; stages of a ring; of pairs, bit 0 if
+ * tiles are numbered rows first, bit 1 if the output leaves L2 early. */
+tman_status tman_debug_f4_plan(int op, int M, int K, int N, int block, int *out8 /*host*/);
+
+/* The same for a device described by the caller: `sms` multiprocessors, of which clusters of four (eight) CTAs with all of an SM each can run
+ * `clusters4` (`clusters8`) at the same time.  Pure host arithmetic: needs no GPU. */
+tman_status tman_debug_f4_plan_for(int op, int M, int K, int N, int block, int sms, int clusters4, int clusters8, int *out8 /*host*/);
+
 /* Lets a bounded wait run out, safely: one warp waits, with the same routine the decode kernel's split-K
  * combine uses, for partial sums that nothing writes (the workspace must be freshly prepared), gives up
  * after `polls` polls (1 .. 2^20, a few hundred nanoseconds each) and reports TMAN_ERR_TIMEOUT in the

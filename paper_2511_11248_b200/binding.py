@@ -28,7 +28,7 @@ EXPORTS = [
     "tman_mpgemv", "tman_mpgemm", "tman_debug_indices", "tman_debug_luts", "tman_debug_gemm_plan", "tman_mpgemv_static", "tman_mpgemv_grouped",
     "tman_debug_microbench", "tman_debug_cluster_capacity", "tman_debug_gemm_plan_for", "tman_debug_gemv_plan", "tman_debug_wait_timeout", "tman_debug_mpgemm_variant", "tman_quantize_rows", "tman_mpgemv_ternary", "tman_dequant_ternary_int8", "tman_debug_role_stamps", "tman_quantize_rows_i8", "tman_mpgemm_ternary_i8",
     "tman_packed_bytes_f4", "tman_workspace_bytes_f4", "tman_pack_f4", "tman_unpack_f4", "tman_quantize_rows_f4", "tman_dequant_rows_f4",
-    "tman_mpgemv_f4", "tman_mpgemm_f4",
+    "tman_mpgemv_f4", "tman_mpgemm_f4", "tman_debug_f4_plan", "tman_debug_f4_plan_for",
 ]
 
 _lib = None
@@ -86,6 +86,8 @@ def lib() -> C.CDLL:
         L.tman_dequant_rows_f4.argtypes = [vp, sz, i, i, i, vp, i, i, vp, sz, vp]
         L.tman_mpgemv_f4.argtypes = [vp, sz, vp, i, vp, i, i, i, i, i, i, vp, sz, vp]
         L.tman_mpgemm_f4.argtypes = [vp, sz, vp, sz, vp, i, i, i, i, i, i, vp, sz, vp]
+        L.tman_debug_f4_plan.argtypes = [i, i, i, i, i, C.POINTER(C.c_int)]
+        L.tman_debug_f4_plan_for.argtypes = [i, i, i, i, i, i, i, i, C.POINTER(C.c_int)]
         L.tman_debug_mpgemm_variant.argtypes = [i, vp, sz, vp, vp, i, i, i, i, i, vp, vp, sz, vp]
         for name in EXPORTS[2:]:
             getattr(L, name).restype = C.c_int
@@ -309,6 +311,21 @@ def tman_mpgemm_f4(packed, a, y, ldy, dtype, M, K, N, block, workspace, stream=N
     st = _hot().mpgemm_f4(packed, a, y, ldy, dtype, M, K, N, block, workspace, _stream(stream))
     if st:
         raise TmanError(st, "tman_mpgemm_f4")
+
+
+F4_PLAN_KEYS = ("pair", "rows", "shares", "tiles_m", "tiles_n", "workers", "stages", "flags")
+
+
+def tman_debug_f4_plan(op, M, K, N, block) -> dict:
+    out = (C.c_int * 8)()
+    _check(lib().tman_debug_f4_plan(op, M, K, N, block, out), "tman_debug_f4_plan")
+    return dict(zip(F4_PLAN_KEYS, list(out)))
+
+
+def tman_debug_f4_plan_for(op, M, K, N, block, sms, clusters4, clusters8) -> dict:
+    out = (C.c_int * 8)()
+    _check(lib().tman_debug_f4_plan_for(op, M, K, N, block, sms, clusters4, clusters8, out), "tman_debug_f4_plan_for")
+    return dict(zip(F4_PLAN_KEYS, list(out)))
 
 
 GEMM_VARIANTS = {"product": 0, "convert_dq": 1, "load_full": 2, "sequential": 3}

@@ -414,6 +414,29 @@ tman_status tman_debug_gemm_plan_for(int M, int K, int N, int bits, int group, i
     return mpgemm_plan_for(M, K, N, bits, sms, resident, out8);
 }
 
+static tman_status check_f4_plan(int op, int M, int K, int N, int block, const int *out8)
+{
+    if (!out8) return TMAN_ERR_NULL;
+    TMAN_F4_CHECK(f4_check(N, K, block));
+    TMAN_F4_CHECK(f4_check(M, K, block));
+    if (op < 0 || op > 1) return TMAN_ERR_UNSUPPORTED;
+    return op == 0 && M > 8 ? TMAN_ERR_SHAPE : TMAN_OK;
+}
+
+tman_status tman_debug_f4_plan(int op, int M, int K, int N, int block, int *out8)
+{
+    TMAN_F4_CHECK(check_f4_plan(op, M, K, N, block, out8));
+    return f4_plan(op, M, K, N, block, out8);
+}
+
+tman_status tman_debug_f4_plan_for(int op, int M, int K, int N, int block, int sms, int clusters4, int clusters8, int *out8)
+{
+    TMAN_F4_CHECK(check_f4_plan(op, M, K, N, block, out8));
+    if (sms < 2 || clusters4 < 0 || clusters8 < 0) return TMAN_ERR_SHAPE;
+    const int clusters[2] = {clusters4, clusters8};
+    return f4_plan_for(op, M, K, N, block, sms, clusters, out8);
+}
+
 tman_status tman_debug_gemv_plan(int M, int K, int N, int bits, int group, int sms, size_t ws_limit, int *out)
 {
     if (!out) return TMAN_ERR_NULL;

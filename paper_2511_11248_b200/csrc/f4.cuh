@@ -166,6 +166,8 @@ tman_status launch_f4_dequant(const void *packed, int rows, int K, int block, vo
 F4Order::Call f4_read_ahead(cudaStream_t s, const void *packed);
 void          f4_read_behind(const F4Order::Call &call, bool launched);
 size_t      f4_workspace_bytes(int op, int M, int K, int N, int block);
+tman_status f4_plan(int op, int M, int K, int N, int block, int *out8);
+tman_status f4_plan_for(int op, int M, int K, int N, int block, int sms, const int (&clusters)[2], int *out8);
 tman_status launch_f4_gemv(const void *packed, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N, int block, void *ws, cudaStream_t s);
 tman_status launch_f4_gemm(const void *packed, const void *a, void *y, int ldy, int dtype, int M, int K, int N, int block, void *ws, cudaStream_t s);
 

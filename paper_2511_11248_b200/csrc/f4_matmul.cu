@@ -52,4 +52,34 @@ tman_status launch_f4_gemm(const void *packed, const void *a, void *y, int ldy, 
     return block == 32 ? gemm_as<32, __nv_bfloat16>(packed, a, y, ldy, M, K, N, ws, s) : gemm_as<16, __nv_bfloat16>(packed, a, y, ldy, M, K, N, ws, s);
 }
 
+// How a call is cut; see tman_debug_f4_plan.
+tman_status f4_plan_for(int op, int M, int K, int N, int block, int sms, const int (&clusters)[2], int *out8)
+{
+    if (op == 0 || stream_wins(M, N)) {
+        const StreamPlan t = stream_plan(M, K, N, block, op == 0, sms);
+        const int out[8] = {0, M, t.split, 1, t.tiles, t.tiles * t.split, t.stages, 0};
+        for (int i = 0; i < 8; ++i) out8[i] = out[i];
+        return TMAN_OK;
+    }
+    F4PairParams p = {};
+    p.M = M;
+    p.N = N;
+    p.halves = f4_layout(N, K, block).halves;
+    const long long tiles = pair_shape(p, sms / 2, clusters), pairs = tiles < sms / 2 ? tiles : sms / 2;
+    if (tiles > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
+    const int out[8] = {1, p.nt, 1 << p.split_sh, p.tiles_m, p.tiles_n, (int)pairs << p.split_sh, block == 32 ? pair_stages<32>() : pair_stages<16>(),
+                        p.rows_fastest | p.stream_y << 1};
+    for (int i = 0; i < 8; ++i) out8[i] = out[i];
+    return TMAN_OK;
+}
+tman_status f4_plan(int op, int M, int K, int N, int block, int *out8)
+{
+    int dev = 0, clusters[2];
+    const DeviceInfo *info = device_info(&dev);
+    if (!info) return TMAN_ERR_CUDA;
+    if (block == 32) pair_capacity<32, __half>(dev, clusters);
+    else pair_capacity<16, __half>(dev, clusters);
+    return f4_plan_for(op, M, K, N, block, info->sms.load(std::memory_order_relaxed), clusters, out8);
+}
+
 }  // namespace tman

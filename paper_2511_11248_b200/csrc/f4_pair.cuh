@@ -41,6 +41,12 @@ template <int BLOCK> struct PairStage {
     static constexpr uint32_t kB = kF4Tile * 128, kSfa = kB + kPairCols / 2 * 128, kSfb = kSfa + 2 * SB, kBytes = kSfb + 2 * 2 * SB;
 };
 
+template <int BLOCK> constexpr int pair_stages()
+{
+    constexpr int n = kPairSmem / (int)PairStage<BLOCK>::kBytes;
+    return n < kPairStages ? n : kPairStages;
+}
+
 template <int BLOCK, typename T>
 __global__ void __launch_bounds__(kPairThreads) f4_pair_kernel(const __grid_constant__ F4PairParams p)
 {
@@ -403,29 +409,15 @@ template <typename Kernel> inline int pair_clusters(Kernel kern, int ctas)
     return n;
 }
 
-template <int BLOCK, typename T>
-tman_status launch_pair(F4PairParams p, cudaStream_t s)
+// A call's tiles: fills in what the kernel is told of them (p.M, N, halves are set), returns how many there are.
+inline long long pair_shape(F4PairParams &p, int workers, const int (&clusters)[2])
 {
-    auto kern = f4_pair_kernel<BLOCK, T>;
-    static std::atomic<bool> raised[kMaxDevices];
-    int dev = 0;
-    const DeviceInfo *info = device_info(&dev);
-    if (!info) return TMAN_ERR_CUDA;
-    const int workers = info->sms.load(std::memory_order_relaxed) / 2;
     p.tiles_n = (p.N + 255) / 256;
-    static std::atomic<int> held[kMaxDevices][2];                // + 1 (0: not asked yet)
-    int clusters[2];
-    for (int i = 0; i < 2; ++i) {
-        int n = held[dev][i].load(std::memory_order_relaxed);
-        if (n == 0) held[dev][i].store(n = pair_clusters(kern, 4 << i) + 1, std::memory_order_relaxed);
-        clusters[i] = n - 1;
-    }
     const PairPlan plan = pair_plan(p.M, (p.halves + 1) / 2, p.tiles_n, workers, clusters);
     p.nt = plan.nt;
     p.split_sh = plan.split >> 1;        // 0, 1, 2
     p.tiles_m = (p.M + p.nt - 1) / p.nt;
     const long long tiles = (long long)p.tiles_m * p.tiles_n;
-    if (tiles > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
     // Tiles are numbered so that a round of them touches the fewest bytes: rows first, it takes all of a and few channels, or the other way
     // around (2048 x 3584 x 18944 rows first 52.5 us, channels first 54.3; 8192 x 18944 x 3584 215 and 195).
     const long long round = tiles < workers ? tiles : workers;
@@ -436,8 +428,34 @@ tman_status launch_pair(F4PairParams p, cudaStream_t s)
     p.tile_mul = inner > 1 && tiles < 65536 ? 0xFFFFFFFFu / inner + 1u : 0u;
     // An output that does not fit L2 beside the operands leaves it early (8192 x 4096 x 14336 184 -> 172 us; 4096 x 14336 x 4096 would go 97 -> 105).
     p.stream_y = (size_t)p.M * p.N * 2 > kPairStreamBytes ? 1 : 0;
-    p.stages = kPairSmem / (int)PairStage<BLOCK>::kBytes;
-    if (p.stages > kPairStages) p.stages = kPairStages;
+    return tiles;
+}
+
+// Clusters of two and of four pairs of the kernel that device dev, the current one, holds at once.
+template <int BLOCK, typename T> inline void pair_capacity(int dev, int (&clusters)[2])
+{
+    static std::atomic<int> held[kMaxDevices][2];                // + 1 (0: not asked yet)
+    for (int i = 0; i < 2; ++i) {
+        int n = held[dev][i].load(std::memory_order_relaxed);
+        if (n == 0) held[dev][i].store(n = pair_clusters(f4_pair_kernel<BLOCK, T>, 4 << i) + 1, std::memory_order_relaxed);
+        clusters[i] = n - 1;
+    }
+}
+
+template <int BLOCK, typename T>
+tman_status launch_pair(F4PairParams p, cudaStream_t s)
+{
+    auto kern = f4_pair_kernel<BLOCK, T>;
+    static std::atomic<bool> raised[kMaxDevices];
+    int dev = 0;
+    const DeviceInfo *info = device_info(&dev);
+    if (!info) return TMAN_ERR_CUDA;
+    int clusters[2];
+    pair_capacity<BLOCK, T>(dev, clusters);
+    const int workers = info->sms.load(std::memory_order_relaxed) / 2;
+    const long long tiles = pair_shape(p, workers, clusters);
+    if (tiles > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
+    p.stages = pair_stages<BLOCK>();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((2 << p.split_sh) * (tiles < workers ? tiles : workers)));
     cfg.blockDim = dim3(kPairThreads);

@@ -445,6 +445,30 @@ inline int stream_split(int tiles, int units, int sms)      // units of 256
 //   M = 96          11.9 / 8.7                 17.2 / 18.8                    10.2 / 7.3                 24.9 / 14.4
 inline bool stream_wins(int M, int N) { return M <= 48 || (M <= kStreamMaxRows && (N + kF4Tile - 1) / kF4Tile <= 74); }
 
+struct StreamPlan { int tiles, cols, split, stages, stage_bytes, smem; };
+inline StreamPlan stream_plan(int M, int K, int N, int block, bool digits, int sms)
+{
+    StreamPlan t;
+    const int halves = (K + kF4Half - 1) / kF4Half, steps = (halves + 1) / 2;
+    t.tiles = (N + kF4Tile - 1) / kF4Tile;
+    t.cols = digits ? (M + 1) / 2 * 16 : (M + 15) / 16 * 16;
+    t.split = stream_split(t.tiles, steps, sms);
+    const int b_bytes = digits ? stream_b_bytes<true>(M, t.cols) : stream_b_bytes<false>(M, t.cols);
+    t.stage_bytes = (kF4Tile * 128 + 2 * f4_scale_bytes(block) + stream_sfb_bytes(block, digits) + b_bytes + 127) / 128 * 128;
+    // Half an SM's shared memory, so that the next call's CTAs fill their rings beside this one's; all of it where half holds few stages.
+    const int budget = t.stage_bytes * (digits ? 3 : 4) <= kStreamHalfSm ? kStreamHalfSm : kStreamAllSm;
+    const int sums = t.split > 1 ? (128 + 8) * M * 4 : 0;
+    t.stages = (budget - sums) / t.stage_bytes;
+    if (t.stages > kStreamMaxStages) t.stages = kStreamMaxStages;
+    const int share = (steps + t.split - 1) / t.split;
+    if (t.stages > share) t.stages = share;
+    // (at least a quarter of an SM's, so that no more CTAs share an SM than its tensor memory has room for: CTAs of a cluster wait for one another,
+    // which one that waits for tensor memory must not hold up)
+    t.smem = t.stages * t.stage_bytes + sums;
+    if (t.smem < kStreamLeastSmem) t.smem = kStreamLeastSmem;
+    return t;
+}
+
 template <int BLOCK, typename T, bool DIGITS>
 tman_status launch_stream(F4StreamParams p, cudaStream_t s)
 {
@@ -453,27 +477,16 @@ tman_status launch_stream(F4StreamParams p, cudaStream_t s)
     int dev = 0;
     const DeviceInfo *info = device_info(&dev);
     if (!info) return TMAN_ERR_CUDA;
-    const int tiles = (p.N + kF4Tile - 1) / kF4Tile;
-    p.cols = DIGITS ? (p.M + 1) / 2 * 16 : (p.M + 15) / 16 * 16;
-    const int steps = (p.halves + 1) / 2;
-    p.split = stream_split(tiles, steps, info->sms.load(std::memory_order_relaxed));
-    p.stage_bytes = (kF4Tile * 128 + 2 * f4_scale_bytes(BLOCK) + stream_sfb_bytes(BLOCK, DIGITS) + stream_b_bytes<DIGITS>(p.M, p.cols) + 127) / 128 * 128;
-    // Half an SM's shared memory, so that the next call's CTAs fill their rings beside this one's; all of it where half holds few stages.
-    const int budget = p.stage_bytes * (DIGITS ? 3 : 4) <= kStreamHalfSm ? kStreamHalfSm : kStreamAllSm;
-    const int sums = p.split > 1 ? (128 + 8) * p.M * 4 : 0;
-    p.stages = (budget - sums) / p.stage_bytes;
-    if (p.stages > kStreamMaxStages) p.stages = kStreamMaxStages;
-    const int share = (steps + p.split - 1) / p.split;
-    if (p.stages > share) p.stages = share;
-    // (at least a quarter of an SM's, so that no more CTAs share an SM than its tensor memory has room for: CTAs of a cluster wait for one another,
-    // which one that waits for tensor memory must not hold up)
-    int bytes = p.stages * p.stage_bytes + sums;
-    if (bytes < kStreamLeastSmem) bytes = kStreamLeastSmem;
-    if ((long long)tiles * p.split > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
+    const StreamPlan plan = stream_plan(p.M, p.K, p.N, BLOCK, DIGITS, info->sms.load(std::memory_order_relaxed));
+    p.cols = plan.cols;
+    p.split = plan.split;
+    p.stages = plan.stages;
+    p.stage_bytes = plan.stage_bytes;
+    if ((long long)plan.tiles * p.split > 0x7FFFFFFF) return TMAN_ERR_SHAPE;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * p.split));
+    cfg.gridDim = dim3((unsigned)(plan.tiles * p.split));
     cfg.blockDim = dim3((unsigned)stream_threads(DIGITS));
-    cfg.dynamicSmemBytes = (size_t)bytes;
+    cfg.dynamicSmemBytes = (size_t)plan.smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
