@@ -22,10 +22,28 @@ static F4StreamParams stream_params(const void *packed, const void *a, const voi
     p.height8 = L.height8;
     return p;
 }
+// Whether a packed x of M rows goes to CTAs that stream the weights rather than to pairs of CTAs with a tile each: by the two modelled times, and
+// beyond 48 rows not with more tiles than pairs (the stream's stages are then few or its second round long).  Over the 23 shapes that the models are
+// fitted to, both blocks, 16 to 64 rows, the kernel chosen takes 0.1 % more than the faster one in the mean and 6 % at most, over 11 others 7 % at
+// most.  One call in a graph of them, us, weights rotated over 300 MB, 32-value blocks, stream / pairs:
+//   K x N   4096 x 1024   4096 x 4096   2048 x 8192   3584 x 4608   14336 x 4096   18944 x 3584   8192 x 8192   4096 x 14336   4096 x 28672
+//   M = 32  4.3 / 6.2     5.7 / 8.1     7.6 / 5.8     7.6 / 7.5     10.0 / 14.4    12.9 / 12.8    13.0 / 12.7   8.3 / 9.7      13.7 / 14.5
+//   M = 48  5.3 / 6.2     7.6 / 8.7     10.5 / 6.5    9.5 / 8.2     12.5 / 14.4    15.0 / 13.0    16.3 / 12.8   9.7 / 10.4     14.6 / 15.1
+//   M = 64  6.3 / 6.3     9.3 / 8.3     13.1 / 6.1    11.4 / 7.8    15.5 / 14.5    18.5 / 13.0    20.6 / 12.8   10.4 / 10.0    15.4 / 14.8
+static bool stream_wins(int M, int K, int N, int sms, const int (&clusters)[2])
+{
+    const int tiles = (N + kF4Tile - 1) / kF4Tile, units = (K + 2 * kF4Half - 1) / (2 * kF4Half);
+    if (M > kStreamMaxRows || (M > 48 && tiles > sms / 2)) return false;
+    return stream_us(M, units, tiles, sms, clusters) <= 3.5 + 0.88 * pair_plan(M, units, (N + 255) / 256, sms / 2, clusters).us;
+}
 template <int BLOCK, typename T>
 static tman_status gemm_as(const void *packed, const void *a, void *y, int ldy, int M, int K, int N, void *ws, cudaStream_t s)
 {
-    if (stream_wins(M, N)) return launch_stream<BLOCK, T, false>(stream_params(packed, a, nullptr, 0, y, ldy, M, K, N, BLOCK, ws), s);
+    int dev = 0, clusters[2];
+    const DeviceInfo *info = device_info(&dev);
+    if (!info) return TMAN_ERR_CUDA;
+    pair_capacity<BLOCK, T>(dev, clusters);
+    if (stream_wins(M, K, N, info->sms.load(std::memory_order_relaxed), clusters)) return launch_stream<BLOCK, T, false>(stream_params(packed, a, nullptr, 0, y, ldy, M, K, N, BLOCK, ws), s);
     const F4Layout L = f4_layout(N, K, BLOCK), A = f4_layout(M, K, BLOCK);
     F4PairParams p = {};
     p.w = static_cast<const uint8_t *>(packed);
@@ -55,7 +73,7 @@ tman_status launch_f4_gemm(const void *packed, const void *a, void *y, int ldy, 
 // How a call is cut; see tman_debug_f4_plan.
 tman_status f4_plan_for(int op, int M, int K, int N, int block, int sms, const int (&clusters)[2], int *out8)
 {
-    if (op == 0 || stream_wins(M, N)) {
+    if (op == 0 || stream_wins(M, K, N, sms, clusters)) {
         const StreamPlan t = stream_plan(M, K, N, block, op == 0, sms);
         const int out[8] = {0, M, t.split, 1, t.tiles, t.tiles * t.split, t.stages, 0};
         for (int i = 0; i < 8; ++i) out8[i] = out[i];

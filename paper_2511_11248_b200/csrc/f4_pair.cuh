@@ -369,18 +369,17 @@ __global__ void __launch_bounds__(kPairThreads) f4_pair_kernel(const __grid_cons
 // bound a unit, so that it takes 0.28 us with 128 rows and 0.33 with 256 (32-value blocks; 2048 x 3584 x 18944 with 128 / 192 / 256 rows a
 // tile: 79.7 / 61.8 / 53.2 us, 8192 x 18944 x 3584: 282 / 213 / 183).  Whole tiles go round the pairs; shares are for few tiles, one a
 // cluster of pairs.
-struct PairPlan { int nt, split; };
+struct PairPlan { int nt, split; double us; };
 inline PairPlan pair_plan(int M, int steps, int tiles_n, int workers, const int (&clusters)[2])      // clusters of two and of four pairs held at once
 {
-    PairPlan best = {64, 1};
-    double least = 1e300;
+    PairPlan best = {64, 1, 1e300};
     for (int nt = 64; nt <= kPairCols; nt += 64) {
         const long long tiles = (long long)((M + nt - 1) / nt) * tiles_n, rounds = (tiles + workers - 1) / workers;
         const double unit = 0.245 + 0.00032 * nt, tile = 0.1 + 0.0075 * nt;
         for (int split = 1; split <= 4; split *= 2) {
             if (split > 1 && (tiles > clusters[split >> 2] || steps < 2 * split)) continue;
             const double us = split == 1 ? (double)rounds * (steps * unit + tile) : (steps + split - 1) / split * unit + tile + kPairSharesUs + 0.004 * nt;
-            if (us < least - 1e-9) { least = us; best = {nt, split}; }
+            if (us < best.us - 1e-9) best = {nt, split, us};
         }
     }
     return best;

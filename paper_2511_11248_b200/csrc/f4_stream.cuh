@@ -437,13 +437,16 @@ inline int stream_split(int tiles, int units, int sms)      // units of 256
     return s;
 }
 
-// Whether a packed x of M rows goes here rather than to pairs of CTAs with a tile each (32-value blocks, us, here / there):
-//   K x N           4096 x 14336               14336 x 4096                   4096 x 1024                4096 x 28672
-//   M = 16          6.4 / 8.1                  6.6 / 18.4                     3.2 / 7.2                  11.3 / 13.8
-//   M = 48          8.2 / 8.2                  9.4 / 18.6                     4.9 / 7.3                  13.8 / 14.1
-//   M = 64          9.2 / 8.3                  11.5 / 18.7                    5.8 / 7.3                  14.8 / 14.1
-//   M = 96          11.9 / 8.7                 17.2 / 18.8                    10.2 / 7.3                 24.9 / 14.4
-inline bool stream_wins(int M, int N) { return M <= 48 || (M <= kStreamMaxRows && (N + kF4Tile - 1) / kF4Tile <= 74); }
+// Modelled time of a packed x of M rows here, beside what the weights' bytes cost either kernel; `clusters`: of four and of eight CTAs that the device
+// holds at once with an SM each.  A row costs its stores, a unit its loads, and in shares the sums of the own channels are added up row by row.
+// Clusters beyond what fits with an SM for each CTA put CTAs on one SM while others idle.
+inline double stream_us(int M, int units, int tiles, int sms, const int (&clusters)[2])
+{
+    const int split = stream_split(tiles, units, sms), share = (units + split - 1) / split, rounds = (tiles * split + sms - 1) / sms;
+    const int fit = split == 1 ? tiles : split == 2 ? sms / 2 : split < 7 ? clusters[0] * 4 / split : clusters[1];
+    const double us = 1.5 + 0.045 * M + 0.225 * share * rounds + (split > 1 ? 0.23 * M / split : 0.0);
+    return tiles > fit ? us + 2.0 + 0.0017 * share * M : us;
+}
 
 struct StreamPlan { int tiles, cols, split, stages, stage_bytes, smem; };
 inline StreamPlan stream_plan(int M, int K, int N, int block, bool digits, int sms)

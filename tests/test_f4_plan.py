@@ -63,3 +63,14 @@ def test_refusals(B):
             B.tman_debug_f4_plan_for(*a.values())
         assert e.value.status == status, over
     assert B.lib().tman_debug_f4_plan_for(1, 100, 256, 512, 32, 148, 33, 15, None) == 1 and B.lib().tman_debug_f4_plan(1, 100, 256, 512, 32, None) == 1
+
+
+# K, N, rows from which pairs of CTAs were measured to be faster by a tenth and more, rows up to which streams of weights were; of either block
+@pytest.mark.parametrize("block", [32, 16])
+@pytest.mark.parametrize("K,N,pairs,streams", [(4096, 1024, 0, 48), (4096, 4096, 64, 48), (2048, 2048, 48, 24), (2048, 8192, 32, 16), (3584, 4608, 48, 24), (14336, 4096, 0, 56),
+                                               (18944, 3584, 40, 16), (18944, 512, 0, 64), (8192, 8192, 48, 24), (28672, 8192, 40, 16), (8192, 3584, 40, 16), (4096, 14336, 0, 32),
+                                               (28672, 1024, 0, 64), (512, 512, 44, 16), (7168, 7168, 60, 16)])
+def test_few_rows_go_to_the_faster_kernel(B, K, N, pairs, streams, block):
+    for M in range(1, 66):
+        p = B.tman_debug_f4_plan_for(1, M, K, N, block, 148, 33, 15)["pair"]
+        assert not (p and M <= streams) and not (pairs and M >= pairs and not p), M
