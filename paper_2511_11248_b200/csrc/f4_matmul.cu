@@ -29,7 +29,7 @@ static F4StreamParams stream_params(const void *packed, const void *a, const voi
 //   K x N   4096 x 1024   4096 x 4096   2048 x 8192   3584 x 4608   14336 x 4096   18944 x 3584   8192 x 8192   4096 x 14336   4096 x 28672
 //   M = 32  4.3 / 6.2     5.7 / 8.1     7.6 / 5.8     7.6 / 7.5     10.0 / 14.4    12.9 / 12.8    13.0 / 12.7   8.3 / 9.7      13.7 / 14.5
 //   M = 48  5.3 / 6.2     7.6 / 8.7     10.5 / 6.5    9.5 / 8.2     12.5 / 14.4    15.0 / 13.0    16.3 / 12.8   9.7 / 10.4     14.6 / 15.1
-//   M = 64  6.3 / 6.3     9.3 / 8.3     13.1 / 6.1    11.4 / 7.8    15.5 / 14.5    18.5 / 13.0    20.6 / 12.8   10.4 / 10.0    15.4 / 14.8
+//   M = 64  6.3 / 6.3     9.4 / 8.3     13.1 / 6.1    17.2 / 7.8    12.7 / 14.5    23.9 / 13.0    17.1 / 12.8   10.4 / 10.0    15.4 / 14.8
 static bool stream_wins(int M, int K, int N, int sms, const int (&clusters)[2])
 {
     const int tiles = (N + kF4Tile - 1) / kF4Tile, units = (K + 2 * kF4Half - 1) / (2 * kF4Half);

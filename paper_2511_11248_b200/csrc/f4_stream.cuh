@@ -458,9 +458,11 @@ inline StreamPlan stream_plan(int M, int K, int N, int block, bool digits, int s
     t.split = stream_split(t.tiles, steps, sms);
     const int b_bytes = digits ? stream_b_bytes<true>(M, t.cols) : stream_b_bytes<false>(M, t.cols);
     t.stage_bytes = (kF4Tile * 128 + 2 * f4_scale_bytes(block) + stream_sfb_bytes(block, digits) + b_bytes + 127) / 128 * 128;
-    // Half an SM's shared memory, so that the next call's CTAs fill their rings beside this one's; all of it where half holds few stages.
-    const int budget = t.stage_bytes * (digits ? 3 : 4) <= kStreamHalfSm ? kStreamHalfSm : kStreamAllSm;
+    // Half an SM's shared memory, so that the next call's CTAs fill their rings beside this one's; all of it where half holds fewer than three stages
+    // beside the sums (64 rows of 32-value blocks: 14336 x 4096 15.5 us with two stages, 12.7 with seven; 28672 x 4096 23.6 and 17.4), or, of a packed
+    // x, fewer than four without them.
     const int sums = t.split > 1 ? (128 + 8) * M * 4 : 0;
+    const int budget = t.stage_bytes * 3 + sums <= kStreamHalfSm && (digits || t.stage_bytes * 4 <= kStreamHalfSm) ? kStreamHalfSm : kStreamAllSm;
     t.stages = (budget - sums) / t.stage_bytes;
     if (t.stages > kStreamMaxStages) t.stages = kStreamMaxStages;
     const int share = (steps + t.split - 1) / t.split;

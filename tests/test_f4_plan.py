@@ -74,3 +74,16 @@ def test_few_rows_go_to_the_faster_kernel(B, K, N, pairs, streams, block):
     for M in range(1, 66):
         p = B.tman_debug_f4_plan_for(1, M, K, N, block, 148, 33, 15)["pair"]
         assert not (p and M <= streams) and not (pairs and M >= pairs and not p), M
+
+
+@pytest.mark.parametrize("block", [32, 16])
+def test_a_ring_has_three_stages_or_all_that_its_share_takes(B, block):
+    """Also where the sums of the shares, which lie behind it, take a third of half an SM's memory."""
+    for M in range(1, 65):
+        for K, N in ((14336, 4096), (4096, 4096), (28672, 4096), (18944, 512), (4096, 14336), (2048, 512), (96, 40)):
+            for op in (0, 1):
+                if op == 0 and M > 8:
+                    continue
+                p = B.tman_debug_f4_plan_for(op, M, K, N, block, 148, 33, 15)
+                if not p["pair"]:
+                    assert p["stages"] >= min(3, -(-K // 256 // p["shares"])), (op, M, K, N, p)
