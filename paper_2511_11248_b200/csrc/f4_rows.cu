@@ -315,25 +315,19 @@ __global__ void __launch_bounds__(32 * kRowsWarps) f4_row_scales_kernel(const T 
 
 // A launch that may start while the kernel ahead drains (the kernels wait for it before they read or write).
 template <typename... P, typename... A>
-static cudaError_t try_rows(void (*kern)(P...), long long grid, int threads, size_t smem, cudaStream_t s, A... args)
+static tman_status launch_rows(void (*kern)(P...), long long grid, int threads, cudaStream_t s, A... args)
 {
+    if (grid > 0x7FFFFFFFll) return TMAN_ERR_SHAPE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
-}
-template <typename... P, typename... A>
-static tman_status launch_rows(void (*kern)(P...), long long grid, int threads, cudaStream_t s, A... args)
-{
-    if (grid > 0x7FFFFFFFll) return TMAN_ERR_SHAPE;
-    return try_rows(kern, grid, threads, 0, s, args...) == cudaSuccess ? TMAN_OK : TMAN_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...) == cudaSuccess ? TMAN_OK : TMAN_ERR_CUDA;
 }
 
 template <int BLOCK, typename T>
@@ -342,12 +336,14 @@ static tman_status launch_quantize_as(const void *xv, int ldx, int rows, int K, 
     const F4Layout L = f4_layout(rows, K, BLOCK);
     const T *x = static_cast<const T *>(xv);
     uint8_t *packed = static_cast<uint8_t *>(pv);
-    const long long groups = L.height8 / 8;
+    const int sms = sm_count();
+    if (sms == 0) return TMAN_ERR_CUDA;
+    const long long groups = L.height8 / 8, few = 2 * sms;       // (below two CTAs an SM, more and smaller ones)
     const auto parts = [&](int v) { return (L.halves * 4 + kRowsWarps * v - 1) / (kRowsWarps * v); };      // CTAs along K
     if constexpr (BLOCK == 16) {
         const int units = (L.halves + 1) / 2;                    // (few rows: more warps a row)
-        if (rows < 296 && units <= 32) return launch_rows(f4_quantize16_kernel<T, 1, 1024>, rows, 1024, s, x, ldx, rows, K, packed, L);
-        if (rows < 296 && units <= 96) return launch_rows(f4_quantize16_kernel<T, 3, 1024>, rows, 1024, s, x, ldx, rows, K, packed, L);
+        if (rows < few && units <= 32) return launch_rows(f4_quantize16_kernel<T, 1, 1024>, rows, 1024, s, x, ldx, rows, K, packed, L);
+        if (rows < few && units <= 96) return launch_rows(f4_quantize16_kernel<T, 3, 1024>, rows, 1024, s, x, ldx, rows, K, packed, L);
         if (units <= 8) return launch_rows(f4_quantize16_kernel<T, 1, 256>, rows, 256, s, x, ldx, rows, K, packed, L);
         if (units <= 16) return launch_rows(f4_quantize16_kernel<T, 2, 256>, rows, 256, s, x, ldx, rows, K, packed, L);
         if (units <= 32) return launch_rows(f4_quantize16_kernel<T, 4, 256>, rows, 256, s, x, ldx, rows, K, packed, L);
@@ -358,7 +354,7 @@ static tman_status launch_quantize_as(const void *xv, int ldx, int rows, int K, 
         if (st != TMAN_OK) return st;
         return launch_rows(f4_quantize_kernel<BLOCK, T, 8>, groups * parts(8), 32 * kRowsWarps, s, x, ldx, rows, K, packed, L, parts(8));
     } else {
-        if (groups * parts(8) >= 296) return launch_rows(f4_quantize_kernel<BLOCK, T, 8>, groups * parts(8), 32 * kRowsWarps, s, x, ldx, rows, K, packed, L, parts(8));
+        if (groups * parts(8) >= few) return launch_rows(f4_quantize_kernel<BLOCK, T, 8>, groups * parts(8), 32 * kRowsWarps, s, x, ldx, rows, K, packed, L, parts(8));
         return launch_rows(f4_quantize_kernel<BLOCK, T, 4>, groups * parts(4), 32 * kRowsWarps, s, x, ldx, rows, K, packed, L, parts(4));
     }
 }
