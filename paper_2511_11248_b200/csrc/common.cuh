@@ -78,6 +78,13 @@ inline tman_status launch_status()
 {
     return cudaGetLastError() == cudaSuccess ? TMAN_OK : TMAN_ERR_CUDA;
 }
+// Of a call that returns its error: reported here, and not by the next call that asks for the last one.
+inline tman_status call_status(cudaError_t e)
+{
+    if (e == cudaSuccess) return TMAN_OK;
+    (void)cudaGetLastError();
+    return TMAN_ERR_CUDA;
+}
 
 // Properties of the current device that launches are planned from.  They never change, so they are asked once per
 // device (two attribute queries a call otherwise).
@@ -112,14 +119,13 @@ template <typename Kernel, typename Launch>
 inline tman_status launch_with_smem(Kernel kern, int bytes, int dev, std::atomic<bool> *raised, const Launch &launch)
 {
     if (raised[dev].load(std::memory_order_relaxed)) {
-        if (launch() == cudaSuccess) return TMAN_OK;
-        (void)cudaGetLastError();
+        if (call_status(launch()) == TMAN_OK) return TMAN_OK;
         raised[dev].store(false, std::memory_order_relaxed);
     }
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return TMAN_ERR_CUDA;
-    if (launch() != cudaSuccess) return TMAN_ERR_CUDA;
-    raised[dev].store(true, std::memory_order_relaxed);
-    return TMAN_OK;
+    tman_status st = call_status(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    if (st == TMAN_OK) st = call_status(launch());
+    if (st == TMAN_OK) raised[dev].store(true, std::memory_order_relaxed);
+    return st;
 }
 
 // ---- loads behind a wait (device) ----------------------------------------------------------

@@ -327,7 +327,7 @@ static tman_status launch_rows(void (*kern)(P...), long long grid, int threads, 
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...) == cudaSuccess ? TMAN_OK : TMAN_ERR_CUDA;
+    return call_status(cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...));
 }
 
 template <int BLOCK, typename T>

@@ -1410,7 +1410,7 @@ static tman_status launch_quantize(const void *x, int M, int K, int qmax, OUT *a
             preferred[few][dev].store(true, std::memory_order_relaxed);
         }
     }
-    return cudaLaunchKernelEx(&cfg, kern, xh, nvec, qmax, a, s_a) == cudaSuccess ? TMAN_OK : TMAN_ERR_CUDA;
+    return call_status(cudaLaunchKernelEx(&cfg, kern, xh, nvec, qmax, a, s_a));
 }
 
 tman_status launch_quantize_rows(const void *x, int M, int K, int qmax, int16_t *a, float *s_a, cudaStream_t s)

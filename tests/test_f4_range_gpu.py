@@ -87,3 +87,28 @@ def test_the_smallest_rows(M, K, N, block, top):
     codes = rng.integers(0, 16, (N, K)).astype(np.uint8)
     scales = rng.integers(150, 156, (N, K // 32)).astype(np.uint8) if block == 32 else rng.integers(0x30, 0x50, (N, K // 16)).astype(np.uint8)
     check(x, codes, scales, np.full(N, 2.0 ** 25, np.float32), block, "bf16", floor=2.0 ** -141)
+
+
+@pytest.mark.parametrize("M,K,N", SIZES)
+@pytest.mark.parametrize("low", [True, False])
+def test_the_smallest_and_largest_block_scales(M, K, N, low):
+    """Weights under the scales 2^-127 to 2^-125, or 2^125 to 2^127, and activations that bring the outputs to ordinary sizes: by the decode product, and
+    with both operands in 4 bits (quantized activations are exact operands, so that only sums and the type's half step remain)."""
+    rng = np.random.default_rng(N + low)
+    K += -K % 32
+    codes = rng.integers(0, 16, (N, K)).astype(np.uint8)
+    scales = rng.integers(0, 3, (N, K // 32)).astype(np.uint8) if low else rng.integers(252, 255, (N, K // 32)).astype(np.uint8)
+    x = rng.standard_normal((M, K)) * (2.0 ** 110 if low else 2.0 ** -120)
+    check(x, codes, scales, np.ones(N, np.float32), 32, "bf16", floor=2.0 ** -141)
+    packed = pack_on_device(codes, scales, np.ones(N, np.float32), 32)
+    for rows in (M, 70):
+        many = np.tile(x, (-(-rows // M), 1))[:rows]
+        dev, held = to_device(many, K, torch.bfloat16)
+        a, ws, y = H.alloc_f4(rows, K, 32), H.alloc_workspace_f4(B.OP_GEMM, rows, K, N, 32), H.alloc_matrix(rows, N, torch.bfloat16)
+        B.tman_quantize_rows_f4(dev, K, B.DTYPE_BF16, rows, K, 32, a)
+        B.tman_mpgemm_f4(packed, a, y, N, B.DTYPE_BF16, rows, K, N, 32, ws)
+        assert B.tman_read_status(ws) == 0
+        v, w = fo.values(*fo.quantize(held, 32), 32), fo.values(codes, scales, np.ones(N), 32)
+        ref, S = v @ w.T, np.abs(v) @ np.abs(w).T
+        bad = int((~(np.abs(f64(y) - ref) <= 2.0 ** -8 * np.abs(ref) + (K / 64 + 32) * 2.0 ** -23 * S)).sum())
+        assert bad == 0, f"{bad} of {ref.size}"
