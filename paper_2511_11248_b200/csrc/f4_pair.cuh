@@ -1,4 +1,4 @@
-// Products of many rows, both operands in 4 bits: y[m][n] = a_row[m] w_row[n] sum_k a[m][k] w[n][k], bound by the tensor cores.
+// Products of many rows, both operands in 4 bits: y[m][n] = a_row[m] w_row[n] sum_k a[m][k] w[n][k].
 //
 // A pair of CTAs (cta_group::2) has a tile of 256 channels (the rows of the tensor-core tile, 128 a CTA) x up to 256 rows of a (its columns).
 // The packed layout is the operands' layout: units of 256 values of k reach shared memory by four linear bulk copies a CTA, its own
@@ -365,10 +365,10 @@ __global__ void __launch_bounds__(kPairThreads) f4_pair_kernel(const __grid_cons
     }
 }
 
-// Rows of a in a tile, a multiple of 64, and shares of k of a tile: what has the least modelled time.  The loads, about 57 bytes a clock and SM,
-// bound a unit, so that it takes 0.28 us with 128 rows and 0.33 with 256 (32-value blocks; 2048 x 3584 x 18944 with 128 / 192 / 256 rows a
-// tile: 79.7 / 61.8 / 53.2 us, 8192 x 18944 x 3584: 282 / 213 / 183).  Whole tiles go round the pairs; shares are for few tiles, one a
-// cluster of pairs.
+// Rows of a in a tile, a multiple of 64, and shares of k of a tile: what has the least modelled time.  A unit takes 0.28 us with 128 rows and 0.33
+// with 256 (32-value blocks; 2048 x 3584 x 18944 with 128 / 192 / 256 rows a tile: 79.7 / 61.8 / 53.2 us, 8192 x 18944 x 3584: 282 / 213 / 183).  What
+// holds it there is not the products alone: in 2048 x 3584 x 18944 the tensor pipe is active 61 % of the cycles, L2 is at 39 % and sends an SM 48
+// bytes a clock, DRAM is at 14 %.  Whole tiles go round the pairs; shares are for few tiles, one a cluster of pairs.
 struct PairPlan { int nt, split; double us; };
 inline PairPlan pair_plan(int M, int steps, int tiles_n, int workers, const int (&clusters)[2])      // clusters of two and of four pairs held at once
 {
