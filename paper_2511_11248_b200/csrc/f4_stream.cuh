@@ -432,33 +432,37 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     }
 }
 
-// Shares of k: as many as give every SM a CTA at most (4096 x 4096, one row: four shares 3.9 us, eight, two CTAs an SM, 5.6).
-inline int stream_split(int tiles, int units, int sms)      // units of 256
+// Clusters of `split` CTAs that the device holds at once with an SM for each CTA; `clusters`: of four and of eight.
+inline int stream_fit(int split, int sms, const int (&clusters)[2])
 {
-    int s = 1;
-    while (s < kStreamMaxSplit && tiles * (s + 1) <= sms && units >= s + 1) ++s;
-    return s;
+    return split <= 2 ? sms / split : split < 7 ? clusters[0] * 4 / split : clusters[1];
+}
+// Shares of k: as many as give every SM a CTA at most (4096 x 4096, one row: four shares 3.9 us, eight, two CTAs an SM, 5.6), in clusters that fit so: a CTA
+// that shares its SM starts late (see above).
+inline int stream_split(int tiles, int units, int sms, const int (&clusters)[2])      // units of 256
+{
+    int best = 1;
+    for (int s = 2; s <= kStreamMaxSplit && units >= s; ++s)
+        if (tiles <= stream_fit(s, sms, clusters)) best = s;
+    return best;
 }
 
-// Modelled time of a packed x of M rows here, beside what the weights' bytes cost either kernel; `clusters`: of four and of eight CTAs that the device
-// holds at once with an SM each.  A row costs its stores, a unit its loads, and in shares the sums of the own channels are added up row by row.
-// Clusters beyond what fits with an SM for each CTA put CTAs on one SM while others idle.
+// Modelled time of a packed x of M rows here, beside what the weights' bytes cost either kernel.  A row costs its stores, a unit its loads, and in
+// shares the sums of the own channels are added up row by row.
 inline double stream_us(int M, int units, int tiles, int sms, const int (&clusters)[2])
 {
-    const int split = stream_split(tiles, units, sms), share = (units + split - 1) / split, rounds = (tiles * split + sms - 1) / sms;
-    const int fit = split == 1 ? tiles : split == 2 ? sms / 2 : split < 7 ? clusters[0] * 4 / split : clusters[1];
-    const double us = 1.5 + 0.045 * M + 0.225 * share * rounds + (split > 1 ? 0.23 * M / split : 0.0);
-    return tiles > fit ? us + 2.0 + 0.0017 * share * M : us;
+    const int split = stream_split(tiles, units, sms, clusters), share = (units + split - 1) / split, rounds = (tiles * split + sms - 1) / sms;
+    return 1.5 + 0.045 * M + 0.225 * share * rounds + (split > 1 ? 0.23 * M / split : 0.0);
 }
 
 struct StreamPlan { int tiles, cols, split, stages, stage_bytes, smem; };
-inline StreamPlan stream_plan(int M, int K, int N, int block, bool digits, int sms)
+inline StreamPlan stream_plan(int M, int K, int N, int block, bool digits, int sms, const int (&clusters)[2])
 {
     StreamPlan t;
     const int halves = (K + kF4Half - 1) / kF4Half, steps = (halves + 1) / 2;
     t.tiles = (N + kF4Tile - 1) / kF4Tile;
     t.cols = digits ? (M + 1) / 2 * 16 : (M + 15) / 16 * 16;
-    t.split = stream_split(t.tiles, steps, sms);
+    t.split = stream_split(t.tiles, steps, sms, clusters);
     const int b_bytes = digits ? stream_b_bytes<true>(M, t.cols) : stream_b_bytes<false>(M, t.cols);
     t.stage_bytes = (kF4Tile * 128 + 2 * f4_scale_bytes(block) + stream_sfb_bytes(block, digits) + b_bytes + 127) / 128 * 128;
     // Half an SM's shared memory, so that the next call's CTAs fill their rings beside this one's; all of it where half holds fewer than three stages
@@ -478,14 +482,14 @@ inline StreamPlan stream_plan(int M, int K, int N, int block, bool digits, int s
 }
 
 template <int BLOCK, typename T, bool DIGITS>
-tman_status launch_stream(F4StreamParams p, cudaStream_t s)
+tman_status launch_stream(F4StreamParams p, const int (&clusters)[2], cudaStream_t s)
 {
     auto kern = f4_stream_kernel<BLOCK, T, DIGITS>;
     static std::atomic<bool> raised[kMaxDevices];
     int dev = 0;
     const DeviceInfo *info = device_info(&dev);
     if (!info) return TMAN_ERR_CUDA;
-    const StreamPlan plan = stream_plan(p.M, p.K, p.N, BLOCK, DIGITS, info->sms.load(std::memory_order_relaxed));
+    const StreamPlan plan = stream_plan(p.M, p.K, p.N, BLOCK, DIGITS, info->sms.load(std::memory_order_relaxed), clusters);
     p.cols = plan.cols;
     p.split = plan.split;
     p.stages = plan.stages;

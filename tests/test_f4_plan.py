@@ -53,6 +53,7 @@ def test_no_more_clusters_than_the_device_holds(B):
             assert -(-K // 256) >= 2 * p["shares"]
         elif not p["pair"]:
             assert p["shares"] <= 8 and p["tiles_n"] * p["shares"] <= max(148, p["tiles_n"]) and p["stages"] >= 1
+            assert p["shares"] < 3 or p["tiles_n"] <= (held[0] * 4 // p["shares"] if p["shares"] < 7 else held[1])
 
 
 def test_refusals(B):
@@ -65,11 +66,11 @@ def test_refusals(B):
     assert B.lib().tman_debug_f4_plan_for(1, 100, 256, 512, 32, 148, 33, 15, None) == 1 and B.lib().tman_debug_f4_plan(1, 100, 256, 512, 32, None) == 1
 
 
-# K, N, rows from which pairs of CTAs were measured to be faster by a tenth and more, rows up to which streams of weights were; of either block
+# K, N, rows from which pairs of CTAs were measured to be faster by a twentieth and more, rows up to which streams of weights were; of either block
 @pytest.mark.parametrize("block", [32, 16])
 @pytest.mark.parametrize("K,N,pairs,streams", [(4096, 1024, 0, 48), (4096, 4096, 64, 48), (2048, 2048, 48, 24), (2048, 8192, 32, 16), (3584, 4608, 48, 24), (14336, 4096, 0, 56),
-                                               (18944, 3584, 40, 16), (18944, 512, 0, 64), (8192, 8192, 48, 24), (28672, 8192, 40, 16), (8192, 3584, 40, 16), (4096, 14336, 0, 32),
-                                               (28672, 1024, 0, 64), (512, 512, 44, 16), (7168, 7168, 60, 16)])
+                                               (18944, 3584, 48, 24), (18944, 512, 0, 64), (8192, 8192, 40, 24), (28672, 8192, 40, 16), (8192, 3584, 56, 40), (4096, 14336, 0, 32),
+                                               (28672, 1024, 0, 64), (512, 512, 44, 16), (7168, 7168, 40, 24)])
 def test_few_rows_go_to_the_faster_kernel(B, K, N, pairs, streams, block):
     for M in range(1, 66):
         p = B.tman_debug_f4_plan_for(1, M, K, N, block, 148, 33, 15)["pair"]
