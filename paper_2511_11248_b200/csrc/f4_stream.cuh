@@ -23,8 +23,8 @@
 // 4096 x 14336 and 9.1 / 7.2 / 8.6 for 14336 x 4096; with all of an SM's memory the next call cannot fetch its weights beside this one).  More rows
 // leave a ring fewer stages: two, four and eight take 7.9, 8.4 and 10.1 us, in 16-value blocks of 14336 x 4096 8.7, 10.8 and 12.7.
 // More tiles than SMs: a second CTA starts on an SM when the first has given up its right to tensor memory, which it takes behind the wait (see
-// there).  So these calls cannot start early with all of their CTAs: 4096 x 20480 12.1 us, 4096 x 28672 13.2 (9.5 and 11.6 with the tensor
-// memory taken ahead of the wait; behind a kernel that does not signal early, 13.2 and 14.7 of 12.7 and 14.6).
+// there).  So these calls cannot start early with all of their CTAs: 4096 x 20480 10.6 us, 4096 x 28672 12.4 (9.5 and 11.6 with the tensor
+// memory taken ahead of the wait; behind a kernel that does not signal early the two orders are within 4 %).
 // Tried and slower, on earlier builds: the weights' later units prefetched into L2 before the wait (8.6 -> 9.0), separate rings for weights and x,
 // also with two tiles a CTA (7.5 -> 8.4, eight rows 9.7 -> 12.2: a second wait and commit a unit), two CTAs an SM (4096 x 4096 3.9 -> 5.6), sums
 // fetched from the other CTAs between two cluster barriers instead of sent (4096 x 4096 5.2, sent and with the headers checked early 3.9).
@@ -57,7 +57,7 @@ struct F4StreamParams {
     void *y;
     uint32_t *status;
     size_t w_codes, w_scales, w_rows, a_codes, a_scales, a_rows;
-    int M, K, N, ldx, ldy, halves, height8, split, stages, stage_bytes, cols;
+    int M, K, N, ldx, ldy, halves, height8, split, stages, stage_bytes, cols, sms;
 };
 
 template <bool DIGITS>
@@ -150,7 +150,11 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     }
     if (threadIdx.x < 8) row_top[threadIdx.x] = 0u;
     __syncthreads();
-    cluster_arrive();                    // (waited for before the sums are sent)
+    // (Waited for before the sums are sent.)  The arrival takes 2 to 3.5 us of a CTA beside a busy one.  That holds the first loads of an early CTA back
+    // until the kernel ahead needs the bandwidth less (without it 1 x 14336 x 4096 takes 8.7 us instead of 7.5), but a CTA that shares its SM with another of its
+    // own grid starts late and does without, as it has no peers (1 x 4096 x 20480 12.1 -> 10.6 us).
+    const bool arrive = push || (int)blockIdx.x < p.sms;
+    if (arrive) cluster_arrive();
 
     // (Warps 0 and 1 walk as one, one lane issues: addresses and descriptors in uniform registers.)
     if (warp == 0) {
@@ -361,7 +365,7 @@ __global__ void __launch_bounds__(stream_threads(DIGITS), DIGITS ? 2 : 1) f4_str
     // ---- epilogue: warps 2..5, a channel a lane -------------------------------------------------
     tcgen05_fence_before();
     __syncthreads();                     // row scales and the rest in shared memory are there; roles are done
-    cluster_wait();
+    if (arrive) cluster_wait();
     tcgen05_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
     const bool hdr_ok = bad_header == 0u;
@@ -489,7 +493,8 @@ tman_status launch_stream(F4StreamParams p, const int (&clusters)[2], cudaStream
     int dev = 0;
     const DeviceInfo *info = device_info(&dev);
     if (!info) return TMAN_ERR_CUDA;
-    const StreamPlan plan = stream_plan(p.M, p.K, p.N, BLOCK, DIGITS, info->sms.load(std::memory_order_relaxed), clusters);
+    p.sms = info->sms.load(std::memory_order_relaxed);
+    const StreamPlan plan = stream_plan(p.M, p.K, p.N, BLOCK, DIGITS, p.sms, clusters);
     p.cols = plan.cols;
     p.split = plan.split;
     p.stages = plan.stages;
