@@ -19,13 +19,13 @@
 // What bounds it, one row in a graph of calls, each after the one before, weights rotated over 300 MB (32-value blocks; the weights' bytes alone take
 // 4.8 us): 4096 x 14336 7.7 us, 14336 x 4096 7.5, 4096 x 4096 4.0 of 1.4, 4096 x 1024 3.0 of 0.3; with weights in L2 6.5, 6.5, 4.2 and 3.5.
 // About 3 us a call pass between the wait for the kernel ahead and the first product (x from L2, its digits) and between the last one and the
-// end of the kernel; in between the weights' bytes in flight bound it (an earlier build: rings of 74 / 111 / 220 KB a CTA 8.9 / 7.6 / 7.3 us for
+// end of the kernel; in between the weights' bytes in flight bound it (an earlier version of the kernel: rings of 74 / 111 / 220 KB a CTA 8.9 / 7.6 / 7.3 us for
 // 4096 x 14336 and 9.1 / 7.2 / 8.6 for 14336 x 4096; with all of an SM's memory the next call cannot fetch its weights beside this one).  More rows
 // leave a ring fewer stages: two, four and eight take 7.9, 8.4 and 10.1 us, in 16-value blocks of 14336 x 4096 8.7, 10.8 and 12.7.
 // More tiles than SMs: a second CTA starts on an SM when the first has given up its right to tensor memory, which it takes behind the wait (see
 // there).  So these calls cannot start early with all of their CTAs: 4096 x 20480 10.6 us, 4096 x 28672 12.4 (9.5 and 11.6 with the tensor
 // memory taken ahead of the wait; behind a kernel that does not signal early the two orders are within 4 %).
-// Tried and slower, on earlier builds: the weights' later units prefetched into L2 before the wait (8.6 -> 9.0), separate rings for weights and x,
+// Tried and slower, on earlier versions: the weights' later units prefetched into L2 before the wait (8.6 -> 9.0), separate rings for weights and x,
 // also with two tiles a CTA (7.5 -> 8.4, eight rows 9.7 -> 12.2: a second wait and commit a unit), two CTAs an SM (4096 x 4096 3.9 -> 5.6), sums
 // fetched from the other CTAs between two cluster barriers instead of sent (4096 x 4096 5.2, sent and with the headers checked early 3.9).
 #pragma once
