@@ -29,8 +29,9 @@ public:
     bool begin(cudaStream_t s, const void *packed, Call &c)
     {
         noted_.store(true, std::memory_order_release);
-        if (!state(s, packed, c)) return false;
-        if (!c.captured) marks_.begin(c.device, c.handle);
+        if (!place(s, packed, c) || !state(s, c)) return false;
+        if (c.captured) captured_.store(true, std::memory_order_release);
+        else marks_.begin(c.device, c.handle);
         return true;
     }
     void end(const Call &c, bool launched)
@@ -44,9 +45,12 @@ public:
     {
         Call c = {};
         if (!noted_.load(std::memory_order_acquire)) return c;      // nothing quantized in this process: no lock
-        if (!state(s, packed, c)) { c.captured = c.pending = true; return c; }
+        if (!place(s, packed, c)) return unknown(c);
         // (Another stream's quantization is ordered before the product by an event, a replayed one by the end of its graph: full dependencies.)
-        c.pending = c.captured ? captured_behind(s, packed, writes) : marks_.find(c.device, c.handle, packed) == F4Marks::kHere;
+        c.pending = marks_.find(c.device, c.handle, packed) == F4Marks::kHere;
+        if (!c.pending && !captured_.load(std::memory_order_acquire)) return c;      // whether it is captured makes no difference
+        if (!state(s, c)) return unknown(c);
+        if (c.captured) c.pending = captured_behind(s, packed, writes);
         return c;
     }
     void behind(const Call &c, bool launched)
@@ -60,13 +64,22 @@ private:
         if (e != cudaSuccess) (void)cudaGetLastError();
         return e == cudaSuccess;
     }
-    static bool state(cudaStream_t s, const void *packed, Call &c)
+    static bool place(cudaStream_t s, const void *packed, Call &c)
+    {
+        c = {packed, 0, reinterpret_cast<uintptr_t>(s), false, false};
+        return ok(cudaGetDevice(&c.device));
+    }
+    static bool state(cudaStream_t s, Call &c)
     {
         cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
-        c = {packed, 0, reinterpret_cast<uintptr_t>(s), false, false};
-        if (!ok(cudaGetDevice(&c.device)) || !ok(cudaStreamIsCapturing(s, &st))) return false;
+        if (!ok(cudaStreamIsCapturing(s, &st))) return false;
         c.captured = st != cudaStreamCaptureStatusNone;
         return true;
+    }
+    static Call unknown(Call c)                  // plain order, and no mark is taken
+    {
+        c.captured = c.pending = true;
+        return c;
     }
     // Only a kernel can let its successor start early; one that this library does not know by its function is no quantization.
     static bool captured_behind(cudaStream_t s, const void *packed, Writes writes)
@@ -90,7 +103,7 @@ private:
     }
 
     F4Marks marks_;
-    std::atomic<bool> noted_{false};
+    std::atomic<bool> noted_{false}, captured_{false};      // quantizations there were, captured ones
 };
 
 }  // namespace tman
