@@ -45,7 +45,8 @@ typedef enum {
     TMAN_ERR_BAD_PACKED = 5,       /* (device-side) header does not match the arguments */
     TMAN_ERR_CUDA = 6,             /* a CUDA runtime/driver call or a launch failed */
     TMAN_ERR_TIMEOUT = 7,          /* (device-side) a bounded wait ran out */
-    TMAN_ERR_LAYOUT = 8            /* (device-side) shared memory does not start where the kernel was built to expect */
+    TMAN_ERR_LAYOUT = 8,           /* (device-side) shared memory does not start where the kernel was built to expect */
+    TMAN_ERR_INDEX = 9             /* (device-side) a row, length or page of a sequence lies outside of what the call was given */
 } tman_status;
 
 /* Human-readable name of a status code (host pointer to a static string). */
@@ -309,6 +310,78 @@ tman_status tman_mpgemv_f4(const void *packed, size_t packed_bytes, const void *
  * row NaN.  With block = 16 the sum is multiplied with the weights' row scale and then with a's, both in fp32.  Nothing is kept in the workspace but the status word. */
 tman_status tman_mpgemm_f4(const void *packed, size_t packed_bytes, const void *a_packed, size_t a_bytes, void *y, int ldy, int dtype,
                            int M, int K, int N, int block, void *workspace, size_t ws_bytes, tman_stream_t stream);
+
+/* ---- 8-bit integers: products with scales per token and channel ------------------------------------
+ * (No counterpart in the paper, whose integer path has one scale for all weights.)  y[m][n] = a_scale[m] w_scale[n] sum_k a[m][k] w[n][k].
+ *   - w: int8 [N][K], one row per output channel, rows ldw bytes apart (ldw >= K, a multiple of 16; 16-byte aligned), w_scale fp32 [N]; as a
+ *     checkpoint holds them, or as tman_quantize_tokens_i8 makes them of 16-bit weights.
+ *   - K a multiple of 16, at most 131056; any N.  dtype, ldx, ldy, x and y as for 4-bit floating point.  Codes are 16-byte aligned.
+ *   - Sums are exact 32-bit integers; the product with the two scales is right to 2^-22 before y's rounding, whatever the scales' sizes.
+ *   - Everything is read behind the kernels ahead on the stream: no rule about what they write. */
+
+/* Rows of 16 bits as codes and scales: row_scale[m] = max_k |x[m][k]| / 127 (1 for a row of zeros), a[m][k] = round(x[m][k] / row_scale[m]),
+ * division in single precision, rounding to nearest even: tman_quantize_rows_i8 for both types and any distance of rows.  A row that holds an
+ * infinity or a NaN gets codes 0 and the scale NaN, so that its products are NaN.  a: int8 [M][K]. */
+tman_status tman_quantize_tokens_i8(const void *x, int ldx, int dtype, int M, int K, int8_t *a, float *row_scale, tman_stream_t stream);
+
+/* Bytes of scratch, op as for tman_workspace_bytes: 0 = tman_mpgemv_i8, 1 = tman_mpgemm_i8. */
+tman_status tman_workspace_bytes_i8(int op, int M, int K, int N, size_t *out_bytes /*host*/);
+
+/* Decode, M in [1, 8]: quantizes the rows of x in the call; the same result, bit for bit, as tman_quantize_tokens_i8 and tman_mpgemm_i8. */
+tman_status tman_mpgemv_i8(const int8_t *w, int ldw, const float *w_scale, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N,
+                           void *workspace, size_t ws_bytes, tman_stream_t stream);
+
+/* Any M >= 1, activations quantized (a: int8 [M][K], a_scale fp32 [M]). */
+tman_status tman_mpgemm_i8(const int8_t *w, int ldw, const float *w_scale, const int8_t *a, const float *a_scale, void *y, int ldy, int dtype, int M,
+                           int K, int N, void *workspace, size_t ws_bytes, tman_stream_t stream);
+
+/* ---- query and key heads: norm and rotation -----------------------------------------------------------
+ * (No counterpart in the paper.)  A row of x holds q_heads query heads and behind them k_heads key heads of `width` values each (what follows in
+ * the row, values say, is left alone); y the same.  For each head, in 32 bits and rounded once:
+ *   z = x / sqrt(mean(x^2) + eps) * weight            (q_weight, k_weight: `width` values of type dtype; NULL: z = x)
+ *   each pair of the first `rot` values of z is turned by positions[t] * inv_freq[i], i < rot / 2: the pair (i, i + rot / 2), or with
+ *   `adjacent` (2i, 2i + 1); (a, b) -> (a cos - b sin, b cos + a sin).  Angles are right at any position.
+ * width a multiple of 8, at most 256; rot a multiple of 16, at most width, or 0 (no rotation: positions and inv_freq may be NULL); positions
+ * int32 [T], inv_freq fp32 [rot / 2].  x, y and weights 16-byte aligned, ldx and ldy multiples of 8; y may be x (with ldy = ldx). */
+tman_status tman_norm_rotate(const void *x, int ldx, void *y, int ldy, int dtype, int T, int q_heads, int k_heads, int width, int rot, int adjacent,
+                             const void *q_weight, const void *k_weight, float eps, const int32_t *positions, const float *inv_freq,
+                             tman_stream_t stream);
+
+/* ---- a cache of keys and values in 8 bits, and attention over it ----------------------------------------
+ * (No counterpart in the paper.)  The cache has `pages` pages; a page holds `page` consecutive tokens of one sequence (16, 32, 64 or 128), for
+ * `kv_heads` heads of `width` values (64, 128, 192 or 256).  Keys of a page and head have one scale, values another; what is held is code x scale,
+ * codes in [-127, 127] (layout: csrc/cache_i8.cuh).  The buffer needs no preparation; its size counts what pages may be named.
+ * Sequences, S of them: lens[s] tokens, the newest included; table[s * ld_table + i] (int32) is the page of tokens i * page ..; a call's rows of sequence s,
+ * starts[s] .. starts[s + 1] - 1 (int32 [S + 1], T rows in all), are its last tokens; starts NULL: one row each (T = S).  All are device
+ * memory.  Rows behind the last sequence's are left alone.
+ * What only the device can see is reported in the status word as TMAN_ERR_INDEX, and skipped: sequences whose rows lie outside of [0, T) or
+ * that have more tokens than ld_table pages (their rows stay as they were), pages that the cache does not have (their tokens count as masked).
+ * 16-bit matrices: 16-byte aligned, distances of rows multiples of 8.  workspace: tman_workspace_bytes_attend, or 256 bytes for append and read. */
+tman_status tman_cache_bytes_i8(int pages, int page, int kv_heads, int width, size_t *out_bytes /*host*/);
+tman_status tman_workspace_bytes_attend(int width, size_t *out_bytes /*host*/);
+
+/* Rows of k and v ([T][kv_heads * width]) into the cache, each as a token at its position.  A page's scale becomes max(what it was, max|new| / 127)
+ * (a page whose first token is among the new ones begins with 0); codes that are there already become round(code * (old scale / new scale)), new ones
+ * round(x / scale), all in single precision, to nearest even.  A page that gets an infinity or a NaN has the scale NaN and stands for NaN until its
+ * first token is appended again.  More rows than tokens are TMAN_ERR_INDEX.  No page may be appended to by two sequences of a call. */
+tman_status tman_append_i8(void *cache, size_t cache_bytes, int pages, int page, int kv_heads, int width, const void *k, int ldk, const void *v, int ldv,
+                           int dtype, const int32_t *table, int ld_table, const int32_t *lens, const int32_t *starts, int S, int T, void *workspace,
+                           size_t ws_bytes, tman_stream_t stream);
+
+/* Tokens of the cache back in 16 bits, into rows of k and v. */
+tman_status tman_read_cache_i8(const void *cache, size_t cache_bytes, int pages, int page, int kv_heads, int width, const int32_t *table, int ld_table,
+                               const int32_t *lens, const int32_t *starts, int S, int T, void *k, int ldk, void *v, int ldv, int dtype, void *workspace,
+                               size_t ws_bytes, tman_stream_t stream);
+
+/* Attention of each row's query heads (q, y: [T][heads * width]; heads a multiple of kv_heads, query head h has the key head h / (heads / kv_heads)) over
+ * the tokens up to the row's own, the last `window` of them if window > 0:  y = sum_j softmax_j(scale q . key_j) value_j.
+ * The cache holds the row's own token already (tman_append_i8).  A row that sees no token (of a sequence of length 0, or of more rows
+ * than tokens) is 0.
+ * Precision: queries as they are (bf16: exact down to 2^-38 of the row's largest), scores, maxima and sums in 32 bits, probabilities times the value page's
+ * scale rounded to 11 bits.  The result does not depend on timing. */
+tman_status tman_attend_i8(const void *q, int ldq, void *y, int ldy, int dtype, int heads, const void *cache, size_t cache_bytes, int pages, int page,
+                           int kv_heads, int width, const int32_t *table, int ld_table, const int32_t *lens, const int32_t *starts, int S, int T,
+                           float scale, int window, void *workspace, size_t ws_bytes, tman_stream_t stream);
 
 /* ---- test-only extractors of the integer / table intermediates -------------------------- */
 

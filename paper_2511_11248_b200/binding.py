@@ -18,6 +18,7 @@ TMAN_OK = 0
 STATUS_NAMES = {
     0: "TMAN_OK", 1: "TMAN_ERR_NULL", 2: "TMAN_ERR_SHAPE", 3: "TMAN_ERR_UNSUPPORTED",
     4: "TMAN_ERR_BUFFER_TOO_SMALL", 5: "TMAN_ERR_BAD_PACKED", 6: "TMAN_ERR_CUDA", 7: "TMAN_ERR_TIMEOUT",
+    8: "TMAN_ERR_LAYOUT", 9: "TMAN_ERR_INDEX",
 }
 OP_GEMV, OP_GEMM, OP_AUX, OP_TERNARY = 0, 1, 2, 3
 DTYPE_F16, DTYPE_BF16 = 0, 1            # of the 16-bit matrices beside 4-bit floating-point ones
@@ -29,6 +30,8 @@ EXPORTS = [
     "tman_debug_microbench", "tman_debug_cluster_capacity", "tman_debug_gemm_plan_for", "tman_debug_gemv_plan", "tman_debug_wait_timeout", "tman_debug_mpgemm_variant", "tman_quantize_rows", "tman_mpgemv_ternary", "tman_dequant_ternary_int8", "tman_debug_role_stamps", "tman_quantize_rows_i8", "tman_mpgemm_ternary_i8",
     "tman_packed_bytes_f4", "tman_workspace_bytes_f4", "tman_pack_f4", "tman_unpack_f4", "tman_quantize_rows_f4", "tman_dequant_rows_f4",
     "tman_mpgemv_f4", "tman_mpgemm_f4", "tman_debug_f4_plan", "tman_debug_f4_plan_for",
+    "tman_quantize_tokens_i8", "tman_workspace_bytes_i8", "tman_mpgemv_i8", "tman_mpgemm_i8", "tman_norm_rotate",
+    "tman_cache_bytes_i8", "tman_workspace_bytes_attend", "tman_append_i8", "tman_read_cache_i8", "tman_attend_i8",
 ]
 
 _lib = None
@@ -89,6 +92,17 @@ def lib() -> C.CDLL:
         L.tman_debug_f4_plan.argtypes = [i, i, i, i, i, C.POINTER(C.c_int)]
         L.tman_debug_f4_plan_for.argtypes = [i, i, i, i, i, i, i, i, C.POINTER(C.c_int)]
         L.tman_debug_mpgemm_variant.argtypes = [i, vp, sz, vp, vp, i, i, i, i, i, vp, vp, sz, vp]
+        f = C.c_float
+        L.tman_quantize_tokens_i8.argtypes = [vp, i, i, i, i, vp, vp, vp]
+        L.tman_workspace_bytes_i8.argtypes = [i, i, i, i, C.POINTER(sz)]
+        L.tman_mpgemv_i8.argtypes = [vp, i, vp, vp, i, vp, i, i, i, i, i, vp, sz, vp]
+        L.tman_mpgemm_i8.argtypes = [vp, i, vp, vp, vp, vp, i, i, i, i, i, vp, sz, vp]
+        L.tman_norm_rotate.argtypes = [vp, i, vp, i, i, i, i, i, i, i, i, vp, vp, f, vp, vp, vp]
+        L.tman_cache_bytes_i8.argtypes = [i, i, i, i, C.POINTER(sz)]
+        L.tman_workspace_bytes_attend.argtypes = [i, C.POINTER(sz)]
+        L.tman_append_i8.argtypes = [vp, sz, i, i, i, i, vp, i, vp, i, i, vp, i, vp, vp, i, i, vp, sz, vp]
+        L.tman_read_cache_i8.argtypes = [vp, sz, i, i, i, i, vp, i, vp, vp, i, i, vp, i, vp, i, i, vp, sz, vp]
+        L.tman_attend_i8.argtypes = [vp, i, vp, i, i, i, vp, sz, i, i, i, i, vp, i, vp, vp, i, i, f, i, vp, sz, vp]
         for name in EXPORTS[2:]:
             getattr(L, name).restype = C.c_int
         try:
@@ -99,7 +113,8 @@ def lib() -> C.CDLL:
         _marshal.bind(*[C.cast(getattr(L, name), vp).value for name in (
             "tman_mpgemv", "tman_mpgemv_grouped", "tman_mpgemm", "tman_quantize_rows", "tman_quantize_rows_i8",
             "tman_mpgemv_ternary", "tman_mpgemm_ternary_i8", "tman_pack_weights", "tman_quantize_rows_f4", "tman_dequant_rows_f4",
-            "tman_mpgemv_f4", "tman_mpgemm_f4")])
+            "tman_mpgemv_f4", "tman_mpgemm_f4", "tman_quantize_tokens_i8", "tman_mpgemv_i8", "tman_mpgemm_i8", "tman_norm_rotate",
+            "tman_append_i8", "tman_read_cache_i8", "tman_attend_i8")])
         _fast = _marshal
         _lib = L
     return _lib
@@ -326,6 +341,74 @@ def tman_debug_f4_plan_for(op, M, K, N, block, sms, clusters4, clusters8) -> dic
     out = (C.c_int * 8)()
     _check(lib().tman_debug_f4_plan_for(op, M, K, N, block, sms, clusters4, clusters8, out), "tman_debug_f4_plan_for")
     return dict(zip(F4_PLAN_KEYS, list(out)))
+
+
+# ---- 8-bit integers: products, query and key heads, the cache and attention over it ----
+
+def tman_quantize_tokens_i8(x, ldx, dtype, M, K, a, row_scale, stream=None) -> None:
+    st = _hot().quantize_tokens_i8(x, ldx, dtype, M, K, a, row_scale, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_quantize_tokens_i8")
+
+
+def tman_workspace_bytes_i8(op: int, M: int, K: int, N: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().tman_workspace_bytes_i8(op, M, K, N, C.byref(out)), "tman_workspace_bytes_i8")
+    return int(out.value)
+
+
+def tman_mpgemv_i8(w, ldw, w_scale, x, ldx, y, ldy, dtype, M, K, N, workspace, stream=None) -> None:
+    st = _hot().mpgemv_i8(w, ldw, w_scale, x, ldx, y, ldy, dtype, M, K, N, workspace, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_mpgemv_i8")
+
+
+def tman_mpgemm_i8(w, ldw, w_scale, a, a_scale, y, ldy, dtype, M, K, N, workspace, stream=None) -> None:
+    st = _hot().mpgemm_i8(w, ldw, w_scale, a, a_scale, y, ldy, dtype, M, K, N, workspace, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_mpgemm_i8")
+
+
+def tman_norm_rotate(x, ldx, y, ldy, dtype, T, q_heads, k_heads, width, rot, adjacent, q_weight, k_weight, eps, positions, inv_freq, stream=None) -> None:
+    """Norm (weights not None) and rotation (rot > 0) of query and key heads; y may be x."""
+    st = _hot().norm_rotate(x, ldx, y, ldy, dtype, T, q_heads, k_heads, width, rot, adjacent, q_weight, k_weight, eps, positions, inv_freq, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_norm_rotate")
+
+
+def tman_cache_bytes_i8(pages: int, page: int, kv_heads: int, width: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().tman_cache_bytes_i8(pages, page, kv_heads, width, C.byref(out)), "tman_cache_bytes_i8")
+    return int(out.value)
+
+
+def tman_workspace_bytes_attend(width: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().tman_workspace_bytes_attend(width, C.byref(out)), "tman_workspace_bytes_attend")
+    return int(out.value)
+
+
+def tman_append_i8(cache, pages, page, kv_heads, width, k, ldk, v, ldv, dtype, table, ld_table, lens, starts, S, T, workspace, stream=None) -> None:
+    """Each sequence's last tokens into the cache; starts None: one token a sequence."""
+    st = _hot().append_i8(cache, pages, page, kv_heads, width, k, ldk, v, ldv, dtype, table, ld_table, lens, starts, S, T, workspace, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_append_i8")
+
+
+def tman_read_cache_i8(cache, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T, k, ldk, v, ldv, dtype, workspace, stream=None) -> None:
+    """Each sequence's last tokens back in 16 bits."""
+    st = _hot().read_cache_i8(cache, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T, k, ldk, v, ldv, dtype, workspace, _stream(stream))
+    if st:
+        raise TmanError(st, "tman_read_cache_i8")
+
+
+def tman_attend_i8(q, ldq, y, ldy, dtype, heads, cache, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T, scale, window, workspace,
+                   stream=None) -> None:
+    """Attention of each sequence's last tokens over the cache; window 0: all tokens up to their own."""
+    st = _hot().attend_i8(q, ldq, y, ldy, dtype, heads, cache, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T, scale, window, workspace,
+                          _stream(stream))
+    if st:
+        raise TmanError(st, "tman_attend_i8")
 
 
 GEMM_VARIANTS = {"product": 0, "convert_dq": 1, "load_full": 2, "sequential": 3}

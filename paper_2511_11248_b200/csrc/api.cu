@@ -3,6 +3,7 @@
 // (pack.cu, f4_marks.h).
 #include "common.cuh"
 #include "f4.cuh"
+#include "cache_i8.cuh"
 
 using namespace tman;
 
@@ -49,6 +50,7 @@ const char *tman_status_string(int status)
         case TMAN_ERR_CUDA: return "TMAN_ERR_CUDA";
         case TMAN_ERR_TIMEOUT: return "TMAN_ERR_TIMEOUT";
         case TMAN_ERR_LAYOUT: return "TMAN_ERR_LAYOUT";
+        case TMAN_ERR_INDEX: return "TMAN_ERR_INDEX";
         default: return "TMAN_ERR_UNKNOWN";
     }
 }
@@ -373,6 +375,154 @@ tman_status tman_mpgemm_f4(const void *packed, size_t packed_bytes, const void *
     TMAN_F4_CHECK(check_f4_output(y, ldy, dtype, N));
     TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, f4_workspace_bytes(1, M, K, N, block)));
     return launch_f4_gemm(packed, a_packed, y, ldy, dtype, M, K, N, block, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+// ---- 8-bit integers ----
+static tman_status check_i8_weights(const int8_t *w, int ldw, const float *w_scale, int K, int N)
+{
+    if (!w || !w_scale) return TMAN_ERR_NULL;
+    if (K < 16 || K % 16 != 0 || K > kI8MaxK || N < 1 || ldw < K || ldw % 16 != 0) return TMAN_ERR_SHAPE;
+    return aligned_to(w, 16) && aligned_to(w_scale, 4) ? TMAN_OK : TMAN_ERR_SHAPE;
+}
+static tman_status check_i8_tokens(const int8_t *a, const float *a_scale, int M, int K)
+{
+    if (!a || !a_scale) return TMAN_ERR_NULL;
+    if (M < 1 || K < 16 || K % 16 != 0 || K > kI8MaxK) return TMAN_ERR_SHAPE;
+    return aligned_to(a, 16) && aligned_to(a_scale, 4) ? TMAN_OK : TMAN_ERR_SHAPE;
+}
+
+tman_status tman_quantize_tokens_i8(const void *x, int ldx, int dtype, int M, int K, int8_t *a, float *row_scale, tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_i8_tokens(a, row_scale, M, K));
+    TMAN_F4_CHECK(check_f4_rows(x, ldx, dtype, K));
+    return launch_i8_quantize(x, ldx, dtype, M, K, a, row_scale, reinterpret_cast<cudaStream_t>(stream));
+}
+
+tman_status tman_workspace_bytes_i8(int op, int M, int K, int N, size_t *out_bytes)
+{
+    if (!out_bytes) return TMAN_ERR_NULL;
+    if (op < 0 || op > 1) return TMAN_ERR_UNSUPPORTED;
+    if (M < 1 || (op == 0 && M > 8) || K < 16 || K % 16 != 0 || K > kI8MaxK || N < 1) return TMAN_ERR_SHAPE;
+    *out_bytes = i8_workspace_bytes(op, M, K);
+    return TMAN_OK;
+}
+
+tman_status tman_mpgemv_i8(const int8_t *w, int ldw, const float *w_scale, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N,
+                           void *workspace, size_t ws_bytes, tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_i8_weights(w, ldw, w_scale, K, N));
+    if (M < 1 || M > 8) return TMAN_ERR_SHAPE;
+    TMAN_F4_CHECK(check_f4_rows(x, ldx, dtype, K));
+    TMAN_F4_CHECK(check_f4_output(y, ldy, dtype, N));
+    TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, i8_workspace_bytes(0, M, K)));
+    return launch_i8_gemv(w, ldw, w_scale, x, ldx, y, ldy, dtype, M, K, N, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+tman_status tman_mpgemm_i8(const int8_t *w, int ldw, const float *w_scale, const int8_t *a, const float *a_scale, void *y, int ldy, int dtype, int M,
+                           int K, int N, void *workspace, size_t ws_bytes, tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_i8_weights(w, ldw, w_scale, K, N));
+    TMAN_F4_CHECK(check_i8_tokens(a, a_scale, M, K));
+    TMAN_F4_CHECK(check_f4_output(y, ldy, dtype, N));
+    TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, i8_workspace_bytes(1, M, K)));
+    return launch_i8_gemm(w, ldw, w_scale, a, a_scale, y, ldy, dtype, M, K, N, workspace, reinterpret_cast<cudaStream_t>(stream));
+}
+
+// ---- query and key heads ----
+tman_status tman_norm_rotate(const void *x, int ldx, void *y, int ldy, int dtype, int T, int q_heads, int k_heads, int width, int rot, int adjacent,
+                             const void *q_weight, const void *k_weight, float eps, const int32_t *positions, const float *inv_freq,
+                             tman_stream_t stream)
+{
+    if (!x || !y || (rot != 0 && (!positions || !inv_freq))) return TMAN_ERR_NULL;
+    if (dtype != kF4TypeHalf && dtype != kF4TypeBf16) return TMAN_ERR_UNSUPPORTED;
+    if (T < 1 || q_heads < 0 || k_heads < 0 || width < 8 || width > 256 || width % 8 != 0 || rot < 0 || rot > width || rot % 16 != 0) return TMAN_ERR_SHAPE;
+    const long long row = ((long long)q_heads + k_heads) * width;
+    if (row == 0 || ldx < row || ldy < row || ldx % 8 != 0 || ldy % 8 != 0 || !matrices_aligned(x, y) || (x == y && ldx != ldy)) return TMAN_ERR_SHAPE;
+    if (!aligned_to(q_weight, 16) || !aligned_to(k_weight, 16) || !aligned_to(positions, 4) || !aligned_to(inv_freq, 4)) return TMAN_ERR_SHAPE;
+    return launch_norm_rotate(x, ldx, y, ldy, dtype, T, q_heads, k_heads, width, rot, adjacent, q_weight, k_weight, eps, positions, inv_freq,
+                              reinterpret_cast<cudaStream_t>(stream));
+}
+
+// ---- the 8-bit cache ----
+static tman_status check_cache_format(int pages, int page, int kv_heads, int width)
+{
+    if (pages < 1 || kv_heads < 1 || kv_heads > 65535) return TMAN_ERR_SHAPE;
+    if ((page != 16 && page != 32 && page != 64 && page != 128) || (width != 64 && width != 128 && width != 192 && width != 256)) return TMAN_ERR_UNSUPPORTED;
+    return TMAN_OK;
+}
+static tman_status check_cache(const void *cache, size_t bytes, int pages, int page, int kv_heads, int width, const int32_t *table, int ld_table,
+                               const int32_t *lens, const int32_t *starts, int S, int T)
+{
+    if (!cache || !table || !lens) return TMAN_ERR_NULL;
+    TMAN_F4_CHECK(check_cache_format(pages, page, kv_heads, width));
+    if (bytes < cache_bytes(pages, page, kv_heads, width)) return TMAN_ERR_BUFFER_TOO_SMALL;
+    if (!aligned_to(cache, 256) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_to(starts, 4)) return TMAN_ERR_SHAPE;
+    return ld_table < 1 || S < 1 || T < 1 || (!starts && T != S) ? TMAN_ERR_SHAPE : TMAN_OK;
+}
+static tman_status check_cache_rows(const void *x, int ld, int dtype, long long row, int T)
+{
+    if (!x) return TMAN_ERR_NULL;
+    if (dtype != kF4TypeHalf && dtype != kF4TypeBf16) return TMAN_ERR_UNSUPPORTED;
+    return row > INT32_MAX || ld < row || ld % 8 != 0 || !aligned_to(x, 16) || (long long)T * row / 16 > INT32_MAX ? TMAN_ERR_SHAPE : TMAN_OK;
+}
+static CacheSeqs cache_seqs(const void *cache, int pages, int page, int kv_heads, int width, const int32_t *table, int ld_table, const int32_t *lens,
+                            const int32_t *starts, int S, int T, void *ws)
+{
+    return {static_cast<uint8_t *>(const_cast<void *>(cache)), table, lens, starts, static_cast<uint32_t *>(ws), cache_scales_off(pages, page, kv_heads, width),
+            pages, page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7, kv_heads, width, ld_table, S, T};
+}
+
+tman_status tman_cache_bytes_i8(int pages, int page, int kv_heads, int width, size_t *out_bytes)
+{
+    if (!out_bytes) return TMAN_ERR_NULL;
+    TMAN_F4_CHECK(check_cache_format(pages, page, kv_heads, width));
+    *out_bytes = cache_bytes(pages, page, kv_heads, width);
+    return TMAN_OK;
+}
+
+tman_status tman_workspace_bytes_attend(int width, size_t *out_bytes)
+{
+    if (!out_bytes) return TMAN_ERR_NULL;
+    TMAN_F4_CHECK(check_cache_format(1, 16, 1, width));
+    *out_bytes = attend_workspace_bytes(width);
+    return TMAN_OK;
+}
+
+tman_status tman_append_i8(void *cache, size_t cache_bytes, int pages, int page, int kv_heads, int width, const void *k, int ldk, const void *v, int ldv,
+                           int dtype, const int32_t *table, int ld_table, const int32_t *lens, const int32_t *starts, int S, int T, void *workspace,
+                           size_t ws_bytes, tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_cache(cache, cache_bytes, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T));
+    TMAN_F4_CHECK(check_cache_rows(k, ldk, dtype, (long long)kv_heads * width, T));
+    TMAN_F4_CHECK(check_cache_rows(v, ldv, dtype, (long long)kv_heads * width, T));
+    TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, kWsStatusBytes));
+    return launch_append_i8(cache_seqs(cache, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T, workspace), k, ldk, v, ldv, dtype,
+                            reinterpret_cast<cudaStream_t>(stream));
+}
+
+tman_status tman_read_cache_i8(const void *cache, size_t cache_bytes, int pages, int page, int kv_heads, int width, const int32_t *table, int ld_table,
+                               const int32_t *lens, const int32_t *starts, int S, int T, void *k, int ldk, void *v, int ldv, int dtype, void *workspace,
+                               size_t ws_bytes, tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_cache(cache, cache_bytes, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T));
+    TMAN_F4_CHECK(check_cache_rows(k, ldk, dtype, (long long)kv_heads * width, T));
+    TMAN_F4_CHECK(check_cache_rows(v, ldv, dtype, (long long)kv_heads * width, T));
+    TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, kWsStatusBytes));
+    return launch_read_cache_i8(cache_seqs(cache, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T, workspace), k, ldk, v, ldv, dtype,
+                                reinterpret_cast<cudaStream_t>(stream));
+}
+
+tman_status tman_attend_i8(const void *q, int ldq, void *y, int ldy, int dtype, int heads, const void *cache, size_t cache_bytes, int pages, int page,
+                           int kv_heads, int width, const int32_t *table, int ld_table, const int32_t *lens, const int32_t *starts, int S, int T,
+                           float scale, int window, void *workspace, size_t ws_bytes, tman_stream_t stream)
+{
+    TMAN_F4_CHECK(check_cache(cache, cache_bytes, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T));
+    if (heads < 1 || heads % kv_heads != 0 || window < 0) return TMAN_ERR_SHAPE;
+    TMAN_F4_CHECK(check_cache_rows(q, ldq, dtype, (long long)heads * width, T));
+    TMAN_F4_CHECK(check_cache_rows(y, ldy, dtype, (long long)heads * width, T));
+    TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, attend_workspace_bytes(width)));
+    return launch_attend_i8(cache_seqs(cache, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T, workspace), q, ldq, y, ldy, dtype, heads, scale,
+                            window, workspace, reinterpret_cast<cudaStream_t>(stream));
 }
 
 tman_status tman_debug_indices(const void *packed, int K, int N, int bits, int group,

@@ -1,0 +1,68 @@
+// 8-bit integers: what the token quantization, the products and the cache share.
+#pragma once
+
+#include "common.cuh"
+#include "f4.cuh"                        // conversions of the two 16-bit types
+#include "sm100_ptx.cuh"
+
+namespace tman {
+
+constexpr int kI8MaxK = 131056;          // products of two bytes, 2^14 at most, in 32-bit sums
+
+// entry points implemented per file
+tman_status launch_i8_quantize(const void *x, int ldx, int dtype, int M, int K, int8_t *a, float *row_scale, cudaStream_t s);
+tman_status launch_i8_gemv(const int8_t *w, int ldw, const float *w_scale, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N,
+                           void *ws, cudaStream_t s);
+tman_status launch_i8_gemm(const int8_t *w, int ldw, const float *w_scale, const int8_t *a, const float *a_scale, void *y, int ldy, int dtype, int M,
+                           int K, int N, void *ws, cudaStream_t s);
+size_t      i8_workspace_bytes(int op, int M, int K);
+
+#ifdef __CUDACC__
+// Magnitudes of two 16-bit floating-point numbers as integers, which are ordered like them; an infinity is above every number, a NaN above that.
+__device__ __forceinline__ uint32_t i8_magnitudes(uint32_t pair) { return pair & 0x7FFF7FFFu; }
+__device__ __forceinline__ uint32_t i8_larger(uint32_t a, uint32_t b) { return __vmaxu2(a, b); }
+template <typename T> __device__ __forceinline__ uint32_t i8_infinity();
+template <> __device__ __forceinline__ uint32_t i8_infinity<__half>() { return 0x7C00u; }
+template <> __device__ __forceinline__ uint32_t i8_infinity<__nv_bfloat16>() { return 0x7F80u; }
+template <typename T> __device__ __forceinline__ float i8_value(uint32_t bits) { return f4_to_float2<T>(bits).x; }
+
+// The divisor of a row or page whose largest magnitude is `top` (bits): top / 127; NaN where top is none.
+template <typename T> __device__ __forceinline__ float i8_scale(uint32_t top)
+{
+    return top >= i8_infinity<T>() ? __uint_as_float(0x7FFFFFFFu) : __fdiv_rn(i8_value<T>(top), 127.f);
+}
+
+// round(x / scale) of the quotient rounded to 32 bits.  The product with the reciprocal is off by 127 x 2^-23 at most, so that only a quotient
+// next to a half needs the division; so do scales whose reciprocal is none (a scale of 0 stands for zeros).
+struct I8Divisor {
+    float scale, inv;
+    __device__ __forceinline__ explicit I8Divisor(float s) : scale(s), inv(s >= 1e-30f ? 1.f / s : 0.f) {}
+    __device__ __forceinline__ int code(float x) const
+    {
+        const float q = x * inv;
+        float r = rintf(q);
+        if (fabsf(q - r) > 0.4999f || inv == 0.f) r = scale > 0.f ? rintf(__fdiv_rn(x, scale)) : 0.f;       // (scale NaN: 0)
+        return (int)fminf(fmaxf(r, -127.f), 127.f);
+    }
+};
+__device__ __forceinline__ uint32_t i8_pack(int a, int b, int c, int d)
+{
+    return __byte_perm(__byte_perm((uint32_t)a, (uint32_t)b, 0x0040), __byte_perm((uint32_t)c, (uint32_t)d, 0x0040), 0x5410);
+}
+// Eight codes of eight 16-bit values.
+template <typename T> __device__ __forceinline__ uint2 i8_codes(const I8Divisor &d, const uint4 &v)
+{
+    const float2 a = f4_to_float2<T>(v.x), b = f4_to_float2<T>(v.y), c = f4_to_float2<T>(v.z), e = f4_to_float2<T>(v.w);
+    return make_uint2(i8_pack(d.code(a.x), d.code(a.y), d.code(b.x), d.code(b.y)), i8_pack(d.code(c.x), d.code(c.y), d.code(e.x), d.code(e.y)));
+}
+
+// sum x (token's scale x channel's scale).  The scales' product in 32 bits where it and what it multiplies stay in range, else in 64.
+__device__ __forceinline__ float i8_scaled(int sum, float a_scale, float w_scale)
+{
+    const float s = a_scale * w_scale;
+    if (fabsf(s) >= 1e-30f && fabsf(s) <= 1e28f) return (float)sum * s;
+    return (float)((double)sum * (double)a_scale * (double)w_scale);
+}
+#endif
+
+}  // namespace tman

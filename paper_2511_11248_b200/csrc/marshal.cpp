@@ -15,7 +15,8 @@
 
 namespace {
 
-enum { F_GEMV, F_GROUPED, F_GEMM, F_QUANT, F_QUANT_I8, F_TERNARY, F_TERNARY_I8, F_PACK, F_QUANT_F4, F_DEQUANT_F4, F_GEMV_F4, F_GEMM_F4, F_COUNT };
+enum { F_GEMV, F_GROUPED, F_GEMM, F_QUANT, F_QUANT_I8, F_TERNARY, F_TERNARY_I8, F_PACK, F_QUANT_F4, F_DEQUANT_F4, F_GEMV_F4, F_GEMM_F4,
+       F_QUANT_TOKENS, F_GEMV_I8, F_GEMM_I8, F_HEADS, F_APPEND, F_READ_CACHE, F_ATTEND, F_COUNT };
 void *g_fn[F_COUNT];
 PyObject *g_data_ptr, *g_nbytes, *g_numel, *g_element_size;                // interned attribute names
 
@@ -286,6 +287,134 @@ PyObject *py_gemm_f4(PyObject *, PyObject *const *args, Py_ssize_t n)
     TMAN_ISSUE(tman_mpgemm_f4, (pk, pb, a, ab, y, ldy, dtype, M, K, N, block, ws, wb, s));
 }
 
+PyObject *py_quant_tokens(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_QUANT_TOKENS;
+    if (!arity(n, 8)) return nullptr;
+    Reader r(args);
+    void *x = r.ptr();
+    const int ldx = r.num(), dtype = r.num(), M = r.num(), K = r.num();
+    void *a = r.ptr(), *sc = r.ptr();
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_quantize_tokens_i8, (x, ldx, dtype, M, K, (int8_t *)a, (float *)sc, s));
+}
+
+PyObject *py_gemv_i8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_GEMV_I8;
+    if (!arity(n, 13)) return nullptr;
+    Reader r(args);
+    size_t wb = 0;
+    void *w = r.ptr();
+    const int ldw = r.num();
+    void *sc = r.ptr(), *x = r.ptr();
+    const int ldx = r.num();
+    void *y = r.ptr();
+    const int ldy = r.num(), dtype = r.num(), M = r.num(), K = r.num(), N = r.num();
+    void *ws = r.buf(&wb);
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_mpgemv_i8, ((const int8_t *)w, ldw, (const float *)sc, x, ldx, y, ldy, dtype, M, K, N, ws, wb, s));
+}
+
+PyObject *py_gemm_i8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_GEMM_I8;
+    if (!arity(n, 13)) return nullptr;
+    Reader r(args);
+    size_t wb = 0;
+    void *w = r.ptr();
+    const int ldw = r.num();
+    void *sc = r.ptr(), *a = r.ptr(), *as = r.ptr(), *y = r.ptr();
+    const int ldy = r.num(), dtype = r.num(), M = r.num(), K = r.num(), N = r.num();
+    void *ws = r.buf(&wb);
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_mpgemm_i8, ((const int8_t *)w, ldw, (const float *)sc, (const int8_t *)a, (const float *)as, y, ldy, dtype, M, K, N, ws, wb, s));
+}
+
+PyObject *py_heads(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_HEADS;
+    if (!arity(n, 17)) return nullptr;
+    Reader r(args);
+    void *x = r.ptr();
+    const int ldx = r.num();
+    void *y = r.ptr();
+    const int ldy = r.num(), dtype = r.num(), T = r.num(), qh = r.num(), kh = r.num(), width = r.num(), rot = r.num(), adjacent = r.num();
+    void *qw = r.ptr(), *kw = r.ptr();
+    const float eps = r.real();
+    void *pos = r.ptr(), *freq = r.ptr();
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_norm_rotate, (x, ldx, y, ldy, dtype, T, qh, kh, width, rot, adjacent, qw, kw, eps, (const int32_t *)pos, (const float *)freq, s));
+}
+
+PyObject *py_append(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_APPEND;
+    if (!arity(n, 18)) return nullptr;
+    Reader r(args);
+    size_t cb = 0, wb = 0;
+    void *cache = r.buf(&cb);
+    const int pages = r.num(), page = r.num(), heads = r.num(), width = r.num();
+    void *k = r.ptr();
+    const int ldk = r.num();
+    void *v = r.ptr();
+    const int ldv = r.num(), dtype = r.num();
+    void *table = r.ptr();
+    const int ldt = r.num();
+    void *lens = r.ptr(), *starts = r.ptr();
+    const int S = r.num(), T = r.num();
+    void *ws = r.buf(&wb);
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_append_i8, (cache, cb, pages, page, heads, width, k, ldk, v, ldv, dtype, (const int32_t *)table, ldt, (const int32_t *)lens,
+                                (const int32_t *)starts, S, T, ws, wb, s));
+}
+
+PyObject *py_read_cache(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_READ_CACHE;
+    if (!arity(n, 18)) return nullptr;
+    Reader r(args);
+    size_t cb = 0, wb = 0;
+    void *cache = r.buf(&cb);
+    const int pages = r.num(), page = r.num(), heads = r.num(), width = r.num();
+    void *table = r.ptr();
+    const int ldt = r.num();
+    void *lens = r.ptr(), *starts = r.ptr();
+    const int S = r.num(), T = r.num();
+    void *k = r.ptr();
+    const int ldk = r.num();
+    void *v = r.ptr();
+    const int ldv = r.num(), dtype = r.num();
+    void *ws = r.buf(&wb);
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_read_cache_i8, (cache, cb, pages, page, heads, width, (const int32_t *)table, ldt, (const int32_t *)lens, (const int32_t *)starts, S, T,
+                                    k, ldk, v, ldv, dtype, ws, wb, s));
+}
+
+PyObject *py_attend(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    constexpr int f = F_ATTEND;
+    if (!arity(n, 21)) return nullptr;
+    Reader r(args);
+    size_t cb = 0, wb = 0;
+    void *q = r.ptr();
+    const int ldq = r.num();
+    void *y = r.ptr();
+    const int ldy = r.num(), dtype = r.num(), heads = r.num();
+    void *cache = r.buf(&cb);
+    const int pages = r.num(), page = r.num(), kv = r.num(), width = r.num();
+    void *table = r.ptr();
+    const int ldt = r.num();
+    void *lens = r.ptr(), *starts = r.ptr();
+    const int S = r.num(), T = r.num();
+    const float scale = r.real();
+    const int window = r.num();
+    void *ws = r.buf(&wb);
+    tman_stream_t s = r.stream();
+    TMAN_ISSUE(tman_attend_i8, (q, ldq, y, ldy, dtype, heads, cache, cb, pages, page, kv, width, (const int32_t *)table, ldt, (const int32_t *)lens,
+                                (const int32_t *)starts, S, T, scale, window, ws, wb, s));
+}
+
 // bind(addresses): the loaded library's entry points, in the order of the enumeration above
 PyObject *py_bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -306,7 +435,10 @@ PyMethodDef methods[] = {
     TMAN_METHOD("mpgemm", py_gemm), TMAN_METHOD("quantize_rows", py_quant), TMAN_METHOD("quantize_rows_i8", py_quant_i8),
     TMAN_METHOD("mpgemv_ternary", py_ternary), TMAN_METHOD("mpgemm_ternary_i8", py_ternary_i8),
     TMAN_METHOD("pack_weights", py_pack), TMAN_METHOD("quantize_rows_f4", py_quant_f4), TMAN_METHOD("dequant_rows_f4", py_dequant_f4),
-    TMAN_METHOD("mpgemv_f4", py_gemv_f4), TMAN_METHOD("mpgemm_f4", py_gemm_f4), {nullptr, nullptr, 0, nullptr}};
+    TMAN_METHOD("mpgemv_f4", py_gemv_f4), TMAN_METHOD("mpgemm_f4", py_gemm_f4),
+    TMAN_METHOD("quantize_tokens_i8", py_quant_tokens), TMAN_METHOD("mpgemv_i8", py_gemv_i8), TMAN_METHOD("mpgemm_i8", py_gemm_i8),
+    TMAN_METHOD("norm_rotate", py_heads), TMAN_METHOD("append_i8", py_append), TMAN_METHOD("read_cache_i8", py_read_cache),
+    TMAN_METHOD("attend_i8", py_attend), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
