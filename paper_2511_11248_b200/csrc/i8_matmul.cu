@@ -1,4 +1,5 @@
 // 8-bit integer products: token quantization and the choice of the kernel.
+#include "i8_pair.cuh"
 #include "i8_stream.cuh"
 
 namespace tman {
@@ -60,14 +61,22 @@ tman_status launch_i8_gemv(const int8_t *w, int ldw, const float *w_scale, const
 }
 
 tman_status launch_i8_gemm(const int8_t *w, int ldw, const float *w_scale, const int8_t *a, const float *a_scale, void *y, int ldy, int dtype, int M,
-                           int K, int N, void *, cudaStream_t s)
+                           int K, int N, void *ws, cudaStream_t s)
 {
-    for (int m = 0; m < M; m += 8) {
-        I8StreamParams p = {w, a + (size_t)m * K, w_scale, a_scale + m, static_cast<uint16_t *>(y) + (size_t)m * ldy, ldw, K, ldy, M - m < 8 ? M - m : 8, K, N, 0};
-        const tman_status st = dtype == kF4TypeHalf ? launch_i8_stream<__half, true>(p, s) : launch_i8_stream<__nv_bfloat16, true>(p, s);
-        if (st != TMAN_OK) return st;
+    if (M <= 8) {
+        const I8StreamParams p = {w, a, w_scale, a_scale, y, ldw, K, ldy, M, K, N, 0};
+        return dtype == kF4TypeHalf ? launch_i8_stream<__half, true>(p, s) : launch_i8_stream<__nv_bfloat16, true>(p, s);
     }
-    return TMAN_OK;
+    I8PairParams p = {};
+    p.w_scale = w_scale;
+    p.a_scale = a_scale;
+    p.y = y;
+    p.status = static_cast<uint32_t *>(ws);
+    p.M = M;
+    p.K = K;
+    p.N = N;
+    p.ldy = ldy;
+    return dtype == kF4TypeHalf ? launch_i8_pair<__half>(w, ldw, a, p, s) : launch_i8_pair<__nv_bfloat16>(w, ldw, a, p, s);
 }
 
 }  // namespace tman
