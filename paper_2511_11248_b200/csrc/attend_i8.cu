@@ -10,15 +10,12 @@
 // Scores are products of 16-bit queries and codes, 32-bit sums, times the key page's scale.  Probabilities meet the values as fp16 numbers
 // p x (scale of the value page), relative to the largest of those so far: each off by 2^-12 of itself, or 2^-25 of that largest one.  Sums and maxima are
 // held in 32 bits.  A bf16 query row is brought into fp16 by a power of two, exact down to 2^-38 of its largest value.
-#include "cache_i8.cuh"
-
-#include <climits>
-#include <type_traits>
+#include "attend_prompt.cuh"
 
 namespace tman {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kPromptRows = 64;          // rows of a sequence from which the kernel for prompts takes it
 constexpr int kShortSteps = 48;          // heads of so few steps are not cut
 constexpr uint32_t kNoneYet = 0x7FA5A5A5u;      // what tman_workspace_init writes: a counter at rest
 
@@ -34,30 +31,14 @@ struct AttendParams {
     void *y;
     float *parts;
     uint32_t *counters;
-    int ldq, ldy, group, window;         // group: query heads of a key head
+    int ldq, ldy, group, window, least;  // group: query heads of a key head; sequences of `least` rows (tokens x group) and more are done elsewhere
     float scale;
 };
 
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint4 &a, uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
-}
-// Four signed bytes as fp16: with the top bit turned they are 0..255, which in the low byte of 0x6400 is 1024 + that.
-__device__ __forceinline__ void bytes_to_half(uint32_t w, uint32_t &lo, uint32_t &hi)
-{
-    const uint32_t u = w ^ 0x80808080u;
-    const __half2 off = __half2half2(__ushort_as_half(0x6480));
-    const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
-    const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), off), y = __hsub2(*reinterpret_cast<const __half2 *>(&b), off);
-    lo = *reinterpret_cast<const uint32_t *>(&x);
-    hi = *reinterpret_cast<const uint32_t *>(&y);
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src)
 {
@@ -79,7 +60,11 @@ __device__ __forceinline__ TileKeys tile_keys(const AttendParams &p, const Cache
     k.steps = max(((k.hi + 15) >> 4) - k.step0, 1);
     return k;
 }
-__device__ __forceinline__ int tiles_of(const AttendParams &p, const CacheSeq &q) { return (q.rows * p.group + kAttendRows - 1) / kAttendRows; }
+__device__ __forceinline__ int tiles_of(const AttendParams &p, const CacheSeq &q)
+{
+    const int rows = q.rows * p.group;
+    return rows >= p.least ? 0 : (rows + kAttendRows - 1) / kAttendRows;
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(const __grid_constant__ AttendParams p)
@@ -455,13 +440,25 @@ template <typename T, int D> tman_status launch(AttendParams p, cudaStream_t s)
     return launch_with_smem(kern, AttendShape<D>::kSmem, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
 }
 
+template <typename T, int D> tman_status launch_both(AttendParams p, cudaStream_t s)
+{
+    // Sequences of many rows go to the kernel for prompts, where the call has room for one; which do is known on the device only.
+    if (p.c.starts && (long long)p.c.T * p.group >= kPromptRows) {
+        p.least = kPromptRows;
+        const PromptParams q = {p.c, p.q, p.y, p.ldq, p.ldy, p.group, p.window, kPromptRows, p.scale};
+        const tman_status st = launch_prompt<T, D>(q, s);
+        if (st != TMAN_OK) return st;
+    }
+    return launch<T, D>(p, s);
+}
+
 template <typename T> tman_status launch_width(const AttendParams &p, cudaStream_t s)
 {
     switch (p.c.width) {
-        case 64: return launch<T, 64>(p, s);
-        case 128: return launch<T, 128>(p, s);
-        case 192: return launch<T, 192>(p, s);
-        default: return launch<T, 256>(p, s);
+        case 64: return launch_both<T, 64>(p, s);
+        case 128: return launch_both<T, 128>(p, s);
+        case 192: return launch_both<T, 192>(p, s);
+        default: return launch_both<T, 256>(p, s);
     }
 }
 
@@ -472,7 +469,7 @@ tman_status launch_attend_i8(const CacheSeqs &c, const void *q, int ldq, void *y
 {
     uint8_t *w8 = static_cast<uint8_t *>(ws);
     const AttendParams p = {c, q, y, reinterpret_cast<float *>(w8 + kWsStatusBytes + kAttendCtas * 4), reinterpret_cast<uint32_t *>(w8 + kWsStatusBytes),
-                            ldq, ldy, q_heads / c.heads, window, scale};
+                            ldq, ldy, q_heads / c.heads, window, INT_MAX, scale};
     return dtype == kF4TypeHalf ? launch_width<__half>(p, s) : launch_width<__nv_bfloat16>(p, s);
 }
 

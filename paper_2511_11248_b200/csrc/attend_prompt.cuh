@@ -1,0 +1,415 @@
+// Attention over the 8-bit cache for many new tokens of a sequence.
+//
+// What bounds it is the exponential function (16 a clock and SM) and the tensor cores, which take as long.  A CTA has up to 256 rows (new tokens x
+// query heads of one key head) in two tiles of 128, and walks over the keys 128 at a time (64 where heads are wide).  Eight warps bring keys and values from
+// the cache, make fp16 of the bytes and lay them out as the tensor cores' operands; one thread issues the MMAs (scores: rows x keys; output: rows x
+// columns, both in tensor memory); four warps a tile of rows, one thread a row, do the softmax.  While one tile's scores are worked on, the
+// other's are multiplied.
+// A thread reads its row of scores twice, for the maximum and for the probabilities, which go back to tensor memory as the A operand of the second
+// product, over the scores.  A key's score is (q . code) x (key page's scale) x scale; probabilities carry the value page's scale, p' = 2^(s + log2 vs - M), so that
+// codes are what they are multiplied with, and the row's sum is that of p' / vs.  M grows, and the output so far is scaled, only when a
+// score is above it by more than 8: then p' is at most 256, and rows seldom change it after their first keys.
+#pragma once
+
+#include "attend.cuh"
+
+namespace tman {
+namespace {
+
+template <int D> struct PromptShape {
+    static constexpr int kKeys = D <= 128 ? 128 : 64, kTiles = D <= 192 ? 2 : 1, kSoft = 4 * kTiles, kLoad = 8;
+    static constexpr int kThreads = 32 * (kSoft + kLoad + 1), kRows = 128 * kTiles;
+    static constexpr int kQ = kRows * D * 2, kKv = kKeys * D * 2, kSmem = kQ + 4 * kKv + 1024;
+    static constexpr int kScore = 0, kOut = kTiles * kKeys;      // columns of tensor memory
+    static_assert(kOut + kTiles * D <= 512 && kSmem <= 227 * 1024, "it fits");
+};
+
+struct PromptParams {
+    CacheSeqs c;
+    const void *q;
+    void *y;
+    int ldq, ldy, group, window, least;  // least: rows (tokens x group) that a sequence must have to be done here
+    float scale;
+};
+
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptParams p)
+{
+    using Sh = PromptShape<D>;
+    constexpr int KT = Sh::kKeys, RT = Sh::kTiles, GROUPS = KT / 16;
+    extern __shared__ __align__(1024) uint8_t prompt_smem[];
+    __shared__ __align__(8) uint64_t q_bar, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ float4 page_consts[4][GROUPS];                    // of 16 keys: scale of the keys, log2 of the values' scale and its reciprocal
+    __shared__ int found[2], sums[Sh::kThreads / 32 + 1];
+    const CacheSeqs &c = p.c;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, page_mask = (1 << c.page_sh) - 1;
+    const uint32_t base = (smem_u32(prompt_smem) + 1023u) & ~1023u;
+    uint8_t *smem = prompt_smem + (base - smem_u32(prompt_smem));
+    const uint32_t qs = base, ks = base + Sh::kQ, vs = ks + 2 * Sh::kKv;
+    if (tid == 0) {
+        mbar_init(smem_u32(&q_bar), 4 * RT);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&k_full[i]), Sh::kLoad);
+            mbar_init(smem_u32(&v_full[i]), Sh::kLoad);
+            mbar_init(smem_u32(&k_empty[i]), 1);
+            mbar_init(smem_u32(&v_empty[i]), 1);
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&p_full[i]), 4);
+            mbar_init(smem_u32(&o_full[i]), 1);
+        }
+        found[0] = -1;
+        fence_barrier_init();
+    }
+    grid_wait();
+    // ---- blocks of rows, counted over the sequences: which one is this CTA's.  A sequence's last rows, which see the most keys, come first.
+    const int head = blockIdx.x % c.heads, index = blockIdx.x / c.heads;
+    {
+        const int per = (c.S + Sh::kThreads - 1) / Sh::kThreads, s0 = min(tid * per, c.S), s1 = min(s0 + per, c.S);
+        auto blocks_of = [&](int s) {
+            const CacheSeq q = cache_seq(c, s);
+            const int rows = q.rows * p.group;
+            return rows < p.least ? 0 : (rows + Sh::kRows - 1) / Sh::kRows;
+        };
+        int mine = 0;
+        for (int s = s0; s < s1; ++s) mine += blocks_of(s);
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += o;
+        }
+        if (lane == 31) sums[warp] = upto;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) upto += sums[w];
+        int before = upto - mine;
+        if (index >= before && index < upto)
+            for (int s = s0; s < s1; ++s) {
+                const int n = blocks_of(s);
+                if (index < before + n) {
+                    found[0] = s;
+                    found[1] = n - 1 - (index - before);
+                    break;
+                }
+                before += n;
+            }
+        __syncthreads();
+    }
+    const int seq = found[0];
+    if (seq < 0) return;                                         // (all threads; a block that exits lets the next kernel start)
+    const CacheSeq q = cache_seq(c, seq);
+    const int row0 = found[1] * Sh::kRows, rows = min(q.rows * p.group - row0, Sh::kRows), pos0 = q.len - q.rows;
+    const int first = pos0 + row0 / p.group, last = pos0 + (row0 + rows - 1) / p.group;      // positions of the first and the last row
+    const int hi = max(last + 1, 0), lo = p.window > 0 ? max(first - p.window + 1, 0) : 0;
+    const int tile0 = lo / KT, tiles = max((hi + KT - 1) / KT - tile0, 1), active = rows > 128 ? 2 : 1;       // tiles of keys, of rows
+    if (warp == Sh::kSoft + Sh::kLoad) {
+        tcgen05_alloc(smem_u32(&tmem_slot), 512);
+        tcgen05_relinquish();
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    grid_launch_next();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
+    bool ok = true;
+
+    if (warp < Sh::kSoft) {
+        // ---- softmax: a thread has a row
+        const int r = warp >> 2, local = (warp & 3) * 32 + lane, row = r * 128 + local;
+        if (r >= active) {
+            if (lane == 0) mbar_arrive(smem_u32(&q_bar));
+        } else {
+            const bool real = row < rows;
+            const int rho = row0 + min(row, rows - 1), token = rho / p.group;
+            const size_t head_at = (size_t)(head * p.group + rho % p.group) * D;
+            const T *src = static_cast<const T *>(p.q) + (size_t)(q.row + token) * p.ldq + head_at;
+            float f = 1.f;
+            if constexpr (!std::is_same<T, __half>::value) {     // a bf16 row into fp16's range by a power of two
+                uint32_t top = 0;
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint4 v = ld_dependent(reinterpret_cast<const uint4 *>(src) + i);
+                    top = i8_larger(top, i8_larger(i8_larger(i8_magnitudes(v.x), i8_magnitudes(v.y)), i8_larger(i8_magnitudes(v.z), i8_magnitudes(v.w))));
+                }
+                top = max(top & 0xFFFFu, top >> 16);
+                f = top == 0 || top >= i8_infinity<T>() ? 1.f : __uint_as_float((uint32_t)(127 + min(141 - (int)(top >> 7), 100)) << 23);
+            }
+#pragma unroll 4
+            for (int i = 0; i < D / 8; ++i) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (real) v = ld_dependent(reinterpret_cast<const uint4 *>(src) + i);
+                if constexpr (!std::is_same<T, __half>::value) {
+                    const float2 a = f4_to_float2<T>(v.x), b = f4_to_float2<T>(v.y), d = f4_to_float2<T>(v.z), e = f4_to_float2<T>(v.w);
+                    v = make_uint4(f4_from_float2<__half>(a.x * f, a.y * f), f4_from_float2<__half>(b.x * f, b.y * f), f4_from_float2<__half>(d.x * f, d.y * f),
+                                   f4_from_float2<__half>(e.x * f, e.y * f));
+                }
+                *reinterpret_cast<uint4 *>(smem + (r * (D / 64) + (i >> 3)) * 16384 + local * 128 + (((i & 7) ^ (local & 7)) << 4)) = v;
+            }
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&q_bar));
+
+            const float rf = p.scale * kLog2e / f;
+            const int limit = pos0 + token, low = p.window > 0 ? limit - p.window + 1 : INT_MIN;
+            const int least_limit = __reduce_min_sync(0xffffffffu, limit), most_low = __reduce_max_sync(0xffffffffu, low);
+            const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16), score = at + Sh::kScore + r * KT, out = at + Sh::kOut + r * D;
+            float M = -INFINITY, l = 0.f;
+            for (int j = 0; j < tiles; ++j) {
+                const int k0 = (tile0 + j) * KT;
+                const bool plain = k0 + KT - 1 <= least_limit && k0 >= most_low;
+                const int upto = limit - k0, from = low == INT_MIN ? INT_MIN : low - k0;      // columns that this row sees
+                const float4 *consts = page_consts[j & 3];
+                ok = warp_all(mbar_wait(smem_u32(&s_full[r]), j & 1)) && ok;
+                if (!ok) break;
+                tcgen05_fence_after();
+                float mx = -INFINITY;
+#pragma unroll 1
+                for (int i = 0; i < KT; i += 32) {
+                    uint32_t z[32];
+                    tcgen05_ld_32x32b_x32(score + (uint32_t)i, z);
+                    const float4 c0 = consts[i >> 4], c1 = consts[(i >> 4) + 1];
+                    const float f0 = c0.x * rf, f1 = c1.x * rf;
+                    tcgen05_wait_ld();
+                    if (plain) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) mx = fmaxf(mx, fmaf(__uint_as_float(z[e]), e < 16 ? f0 : f1, e < 16 ? c0.y : c1.y));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const float t = fmaf(__uint_as_float(z[e]), e < 16 ? f0 : f1, e < 16 ? c0.y : c1.y);
+                            mx = fmaxf(mx, i + e <= upto && i + e >= from ? t : -INFINITY);
+                        }
+                    }
+                }
+                if (__any_sync(0xffffffffu, mx > M + 8.f || (M == -INFINITY && mx != M))) {
+                    const float next = mx > M + 8.f || M == -INFINITY ? fmaxf(mx, M) : M;
+                    const float g = next == M ? 1.f : exp2_fast(M - next);
+                    M = next;
+                    l *= g;
+                    if (j > 0) {
+#pragma unroll 1
+                        for (int i = 0; i < D; i += 16) {
+                            uint32_t z[16];
+                            tcgen05_ld_32x32b_x16(out + (uint32_t)i, z);
+                            tcgen05_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(__uint_as_float(z[e]) * g);
+                            tcgen05_st_32x32b_x16(out + (uint32_t)i, z);
+                        }
+                    }
+                }
+                const float Mu = M == -INFINITY ? 0.f : M;
+#pragma unroll 1
+                for (int i = 0; i < KT; i += 32) {
+                    uint32_t z[32], h[16];
+                    tcgen05_ld_32x32b_x32(score + (uint32_t)i, z);
+                    const float4 c0 = consts[i >> 4], c1 = consts[(i >> 4) + 1];
+                    const float f0 = c0.x * rf, f1 = c1.x * rf, b0 = c0.y - Mu, b1 = c1.y - Mu;
+                    tcgen05_wait_ld();
+                    float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float a = exp2_fast(fmaf(__uint_as_float(z[e]), e < 16 ? f0 : f1, e < 16 ? b0 : b1));
+                        float b = exp2_fast(fmaf(__uint_as_float(z[e + 1]), e < 16 ? f0 : f1, e < 16 ? b0 : b1));
+                        if (!plain) {
+                            a = i + e <= upto && i + e >= from ? a : 0.f;
+                            b = i + e + 1 <= upto && i + e + 1 >= from ? b : 0.f;
+                        }
+                        if (e < 16) l0 += a + b; else l1 += a + b;
+                        h[e / 2] = f4_from_float2<__half>(a, b);
+                    }
+                    l += l0 * c0.z + l1 * c1.z;
+                    tcgen05_st_32x32b_x16(score + (uint32_t)(i / 2), h);
+                }
+                tcgen05_wait_st();
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&p_full[r]));
+            }
+            if (ok) {
+                ok = warp_all(mbar_wait(smem_u32(&o_full[r]), 0));
+                tcgen05_fence_after();
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                T *dst = static_cast<T *>(p.y) + (size_t)(q.row + token) * p.ldy + head_at;
+#pragma unroll 1
+                for (int i = 0; ok && i < D; i += 16) {
+                    uint32_t z[16];
+                    tcgen05_ld_32x32b_x16(out + (uint32_t)i, z);
+                    tcgen05_wait_ld();
+                    if (real) {
+                        uint32_t h[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) h[e] = f4_from_float2<T>(__uint_as_float(z[2 * e]) * inv, __uint_as_float(z[2 * e + 1]) * inv);
+                        *reinterpret_cast<uint4 *>(dst + i) = make_uint4(h[0], h[1], h[2], h[3]);
+                        *reinterpret_cast<uint4 *>(dst + i + 8) = make_uint4(h[4], h[5], h[6], h[7]);
+                    }
+                }
+            }
+        }
+    } else if (warp < Sh::kSoft + Sh::kLoad) {
+        // ---- keys and values: a warp has 16 tokens of a tile (with 64 keys a tile, half of their pieces)
+        constexpr int PARTS = 128 / KT, PIECES = D / 32 / PARTS;
+        const int w = warp - Sh::kSoft, step = w / PARTS, part = w % PARTS, g = lane >> 2, t = lane & 3;
+        const uint8_t *codes = c.cache + (size_t)head * 2 * D * (page_mask + 1) + lane * 16;
+        const size_t page_bytes = (size_t)c.heads * 2 * D * (page_mask + 1);
+        const float *scales = reinterpret_cast<const float *>(c.cache + c.scales_off) + head * 2;
+        // Lane i looks up 16 keys' page and scales for group i of the tile.
+        int id = -1;
+        float key_scale = 0.f, value_scale = 0.f, seen = 0.f;
+        auto look = [&](int j) {
+            const int token = (tile0 + j) * KT + 16 * (lane & (GROUPS - 1));
+            id = -1;
+            key_scale = value_scale = 0.f;
+            if (j < tiles && lane < GROUPS && token < hi) {
+                id = cache_page(c, seq, token >> c.page_sh);
+                if (id >= 0) {
+                    key_scale = ld_dependent(scales + (size_t)id * c.heads * 2);
+                    value_scale = ld_dependent(scales + (size_t)id * c.heads * 2 + 1);
+                }
+            }
+        };
+        uint4 kr[PIECES], vr[PIECES];
+        auto fetch = [&](int j) {
+            const int mine = __shfl_sync(0xffffffffu, id, step), token = (tile0 + j) * KT + 16 * step;
+            const uint8_t *k = codes + (mine < 0 ? 0 : mine) * page_bytes + (size_t)(token & page_mask) * D + part * PIECES * 512, *v = k + (size_t)D * (page_mask + 1);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) kr[i] = mine >= 0 ? ld_dependent(reinterpret_cast<const uint4 *>(k + i * 512)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) vr[i] = mine >= 0 ? ld_dependent(reinterpret_cast<const uint4 *>(v + i * 512)) : make_uint4(0, 0, 0, 0);
+        };
+        look(0);
+        fetch(0);
+        for (int j = 0; j < tiles; ++j) {
+            const int s = j & 1;
+            const uint32_t ph = ((uint32_t)(j >> 1) & 1u) ^ 1u;
+            if (j > 1 && !warp_all(mbar_wait(smem_u32(&k_empty[s]), ph))) { ok = false; break; }
+            // Pages of zero values have no say in how large the others count, so they pass for what is around them.
+            float most = lane < GROUPS && id >= 0 && value_scale == value_scale ? value_scale : 0.f;
+            most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+            if (most > 0.f) seen = most;
+            if (w == 0 && lane < GROUPS) {
+                const float u = value_scale == 0.f ? (seen > 0.f ? seen : 1.f) : value_scale, v = u < 0x1p-120f ? 0x1p-120f : u;
+                page_consts[j & 3][lane] = id < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f) : make_float4(key_scale, __log2f(v), 1.f / v, 0.f);
+            }
+            uint8_t *kt = smem + Sh::kQ + s * Sh::kKv, *vt = smem + Sh::kQ + (2 + s) * Sh::kKv;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {                   // piece 2 p + h: token 8 h + g, columns 64 p + 16 t ..
+                const int piece = part * PIECES + i, row = step * 16 + (piece & 1) * 8 + g;
+                uint32_t h[8];
+                bytes_to_half(kr[i].x, h[0], h[1]);
+                bytes_to_half(kr[i].y, h[2], h[3]);
+                bytes_to_half(kr[i].z, h[4], h[5]);
+                bytes_to_half(kr[i].w, h[6], h[7]);
+                uint8_t *at = kt + (piece >> 1) * (KT * 128) + row * 128;
+                *reinterpret_cast<uint4 *>(at + (((2 * t) ^ g) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint4 *>(at + (((2 * t + 1) ^ g) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+            }
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&k_full[s]));
+            if (j > 1 && !warp_all(mbar_wait(smem_u32(&v_empty[s]), ph))) { ok = false; break; }
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {                   // bytes 4 e ..: column 8 (4 piece + e) + g, tokens 2t, 2t + 1, 2t + 8, 2t + 9
+                const int piece = part * PIECES + i;
+                uint8_t *atom = vt + (step >> 2) * (D * 128);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t h0, h1;
+                    bytes_to_half(e == 0 ? vr[i].x : e == 1 ? vr[i].y : e == 2 ? vr[i].z : vr[i].w, h0, h1);
+                    uint8_t *at = atom + ((4 * piece + e) * 8 + g) * 128 + 4 * t;
+                    *reinterpret_cast<uint32_t *>(at + (((2 * (step & 3)) ^ g) << 4)) = h0;
+                    *reinterpret_cast<uint32_t *>(at + (((2 * (step & 3) + 1) ^ g) << 4)) = h1;
+                }
+            }
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&v_full[s]));
+            if (j + 1 < tiles) {
+                look(j + 1);
+                fetch(j + 1);
+            }
+        }
+    } else {
+        // ---- MMAs
+        const bool lead = elect_one();
+        constexpr uint32_t score_desc = 1u << 4 | (uint32_t)(KT >> 3) << 17 | (128u >> 4) << 24, out_desc = 1u << 4 | (uint32_t)(D >> 3) << 17 | (128u >> 4) << 24;
+        const uint64_t qd = make_kmajor_sw128_desc(qs), kd = make_kmajor_sw128_desc(ks), vd = make_kmajor_sw128_desc(vs);
+        auto scores = [&](int r, int s) {
+            if (lead) {
+#pragma unroll
+                for (uint32_t i = 0; i < D / 16; ++i)
+                    tcgen05_mma_f16(tmem + Sh::kScore + r * KT, qd + ((r * (D / 64) + (i >> 2)) * 16384 + (i & 3) * 32) / 16, kd + (s * Sh::kKv + (i >> 2) * (KT * 128) + (i & 3) * 32) / 16,
+                                    score_desc, i != 0);
+                tcgen05_commit(smem_u32(&s_full[r]));
+                if (r == active - 1) tcgen05_commit(smem_u32(&k_empty[s]));
+            }
+            __syncwarp();
+        };
+        ok = warp_all(mbar_wait(smem_u32(&q_bar), 0));
+        ok = ok && warp_all(mbar_wait(smem_u32(&k_full[0]), 0));
+        tcgen05_fence_after();
+        if (ok)
+            for (int r = 0; r < active; ++r) scores(r, 0);
+        for (int j = 0; ok && j < tiles; ++j) {
+            const int s = j & 1;
+            for (int r = 0; r < active; ++r) {
+                if (r == 0) ok = warp_all(mbar_wait(smem_u32(&v_full[s]), (j >> 1) & 1));
+                ok = ok && warp_all(mbar_wait(smem_u32(&p_full[r]), j & 1));
+                if (!ok) break;
+                tcgen05_fence_after();
+                if (lead) {
+#pragma unroll
+                    for (uint32_t i = 0; i < KT / 16; ++i)
+                        tcgen05_mma_f16_ts(tmem + Sh::kOut + r * D, tmem + Sh::kScore + r * KT + i * 8, vd + (s * Sh::kKv + (i >> 2) * (D * 128) + (i & 3) * 32) / 16, out_desc,
+                                           (j | (int)i) != 0);
+                    if (r == active - 1) tcgen05_commit(smem_u32(&v_empty[s]));
+                    if (j + 1 == tiles) tcgen05_commit(smem_u32(&o_full[r]));
+                }
+                __syncwarp();
+                if (j + 1 < tiles) {
+                    if (r == 0) {
+                        ok = warp_all(mbar_wait(smem_u32(&k_full[s ^ 1]), ((j + 1) >> 1) & 1));
+                        if (!ok) break;
+                        tcgen05_fence_after();
+                    }
+                    scores(r, s ^ 1);
+                }
+            }
+        }
+    }
+    if (!ok) atomicCAS(c.status, 0u, (uint32_t)TMAN_ERR_TIMEOUT);
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == Sh::kSoft + Sh::kLoad) {
+        tcgen05_fence_after();
+        tcgen05_dealloc(tmem, 512);
+    }
+}
+
+template <typename T, int D> tman_status launch_prompt(const PromptParams &p, cudaStream_t s)
+{
+    using Sh = PromptShape<D>;
+    auto kern = attend_prompt_kernel<T, D>;
+    static std::atomic<bool> raised[kMaxDevices];
+    int dev = 0;
+    if (!device_info(&dev)) return TMAN_ERR_CUDA;
+    // blocks of rows: a sequence of n rows has at most n / kRows + 1, and n / least
+    const long long rows = (long long)p.c.T * p.group;
+    const long long most = rows / Sh::kRows + (rows / p.least < p.c.S ? rows / p.least : p.c.S);
+    if (most * p.c.heads > INT32_MAX) return TMAN_ERR_SHAPE;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(most * p.c.heads));
+    cfg.blockDim = dim3(Sh::kThreads);
+    cfg.dynamicSmemBytes = Sh::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return launch_with_smem(kern, Sh::kSmem, dev, raised, [&] { return cudaLaunchKernelEx(&cfg, kern, p); });
+}
+
+}  // namespace
+}  // namespace tman

@@ -117,6 +117,36 @@ def test_attention(page, kv, heads, width, lens, new, ty):
         attend(q, lens, new, heads, ty, rng, window=window, size=1.5)
 
 
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("page,kv,heads,width,lens,new", [
+    (16, 1, 4, 128, [1300, 40, 700, 9], [500, 1, 129, 9]), (64, 2, 2, 64, [900, 640], [640, 640]), (128, 1, 2, 192, [700], [300]), (32, 1, 3, 256, [610, 77], [210, 77])])
+def test_prompts_beside_single_tokens(page, kv, heads, width, lens, new, ty):
+    """Rows of many tiles, over rings of many turns; sequences of one token in the same call."""
+    rng = np.random.default_rng(sum(lens) + width)
+    q = Sequences(io, lens, page, kv, width, rng)
+    q.append(lens, lens, ty, rng)
+    for window, size in ((0, 1.5), (0, 12.0), (150, 1.5)):
+        attend(q, lens, new, heads, ty, rng, window=window, size=size)
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+def test_prompt_over_growing_scores_and_pages_of_zeros(ty):
+    """Scores that rise from tile to tile (the running maximum moves every time) and fall again, values of very different sizes, whole pages of zeros."""
+    rng = np.random.default_rng(31)
+    n = 900
+    q = Sequences(io, [n], 16, 1, 64, rng)
+    k, v = rng.standard_normal((n, 64)) * 0.1, rng.standard_normal((n, 64))
+    k += np.interp(np.arange(n), [0, 600, n], [-4.0, 4.0, -4.0])[:, None] * np.sign(rng.standard_normal(64))
+    v[100:300] *= 2.0 ** -9
+    v[304:320] = 0
+    v[640:656] = 0
+    v[700:] *= 20.0
+    k[700:] *= 0.5
+    q.append([n], [n], ty, rng, k=k, v=v)
+    x = np.sign(k[600])[None] * rng.uniform(0.0, 3.0, (402, 1)) + 0.05 * rng.standard_normal((402, 64))
+    attend(q, [n], [400], 1, ty, rng, q16=x)
+
+
 def test_more_sequences_than_threads_and_no_starts():
     rng = np.random.default_rng(8)
     lens = [int(v) for v in rng.integers(0, 60, 900)]
