@@ -16,7 +16,7 @@ namespace tman {
 namespace {
 
 constexpr int kPromptRows = 64;          // rows of a sequence from which the kernel for prompts takes it
-constexpr int kShortSteps = 48;          // heads of so few steps are not cut
+constexpr int kShortSteps = 96;          // heads of so few steps are not cut
 constexpr uint32_t kNoneYet = 0x7FA5A5A5u;      // what tman_workspace_init writes: a counter at rest
 
 template <int D> struct AttendShape {
@@ -73,6 +73,7 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
     constexpr int W = Sh::kWarps, NT = D / 8, PIECES = D / 32;      // tiles of columns of the output, pieces of a lane
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long before[Sh::kThreads + 1];               // steps of the sequences in front of thread t's
+    __shared__ CacheSeq known[Sh::kThreads];                     // the sequence of thread t, if each has one
     __shared__ long long place[4];
     __shared__ float row_factor[16], warp_max[W][16], warp_lmax[W][16], warp_sum[W][16];
     __shared__ uint32_t last_flag;
@@ -85,15 +86,19 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
     grid_launch_next();
 
     const int per = (c.S + Sh::kThreads - 1) / Sh::kThreads;
-    auto units_of = [&](int s) -> long long {
-        const CacheSeq q = cache_seq(c, s);
+    auto seq_of = [&](int s) { return per == 1 ? known[s] : cache_seq(c, s); };
+    auto units_of = [&](const CacheSeq &q) -> long long {
         long long n = 0;
         for (int i = 0; i < tiles_of(p, q); ++i) n += tile_keys(p, q, i).steps;
         return n * c.heads;
     };
     {
         long long mine = 0;
-        for (int s = min(tid * per, c.S); s < min(tid * per + per, c.S); ++s) mine += units_of(s);
+        for (int s = min(tid * per, c.S); s < min(tid * per + per, c.S); ++s) {
+            const CacheSeq q = cache_seq(c, s);
+            if (per == 1) known[tid] = q;
+            mine += units_of(q);
+        }
         long long upto = mine;
         for (int d = 1; d < 32; d <<= 1) {
             const long long o = __shfl_up_sync(0xffffffffu, upto, d);
@@ -110,8 +115,7 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
     }
     const long long total = before[Sh::kThreads];
     long long run = (total + gridDim.x - 1) / gridDim.x;
-    run = (run + W - 1) / W * W;
-    if (run < 4 * W) run = 4 * W;
+    run = max((run + W - 1) / W, 1ll) * W;
 
     // Sequence, head and tile of a unit, by all threads alike.
     struct Item { int s, head, tile; long long at; CacheSeq q; TileKeys k; };
@@ -125,12 +129,12 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
         it.at = before[lo];
         it.s = lo * per;
         for (;;) {
-            const long long n = per > 1 ? units_of(it.s) : before[lo + 1] - before[lo];
+            const long long n = per > 1 ? units_of(cache_seq(c, it.s)) : before[lo + 1] - before[lo];
             if (u < it.at + n) break;
             it.at += n;
             ++it.s;
         }
-        it.q = cache_seq(c, it.s);
+        it.q = seq_of(it.s);
         const int tiles = tiles_of(p, it.q);
         long long one = 0;
         if (tiles > 1)
@@ -169,28 +173,41 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
         const uint8_t *codes = c.cache + (size_t)it.head * 2 * D * (page_mask + 1);
         const size_t page_bytes = (size_t)c.heads * 2 * D * (page_mask + 1);
         const float *scales = reinterpret_cast<const float *>(c.cache + c.scales_off) + it.head * 2;
-        auto fetch = [&](int step, int slot, float2 &sc) {       // step: of the head
-            sc = make_float2(0.f, 0.f);
-            const int token = (it.k.step0 + step) * 16;
+        // Lane i looks up page and scales of the warp's step 32 b + i, for two b at a time.
+        struct Look { int id; float ks, vs; };
+        auto look = [&](int b) {
+            Look l = {-1, -1.f, 0.f};                            // (scale -1: masked)
+            const int step = s0 + warp + (32 * b + lane) * W, token = (it.k.step0 + step) * 16;
             if (step < s1 && token < it.k.hi) {
-                const int id = cache_page(c, it.s, token >> c.page_sh);
+                l.id = cache_page(c, it.s, token >> c.page_sh);
+                if (l.id >= 0) {
+                    const float *f = scales + (size_t)l.id * c.heads * 2;
+                    l.ks = ld_dependent(f);
+                    l.vs = ld_dependent(f + 1);
+                }
+            }
+            return l;
+        };
+        int looked = 0;                                          // b of `now`
+        Look now = look(0), next = {-1, -1.f, 0.f};
+        const int mine = s1 - s0 > warp ? (s1 - s0 - warp + W - 1) / W : 0;      // steps of this warp
+        auto fetch = [&](int i, int slot) {                      // the warp's step i into a slot of the ring
+            if (i < mine) {
+                const int id = __shfl_sync(0xffffffffu, (i >> 5) == looked ? now.id : next.id, i & 31);
                 if (id >= 0) {
+                    const int token = (it.k.step0 + s0 + warp + i * W) * 16;
                     const uint8_t *k = codes + id * page_bytes + (size_t)(token & page_mask) * D + lane * 16, *v = k + (size_t)D * (page_mask + 1);
                     const uint32_t dst = ring + slot * Sh::kStep;
 #pragma unroll
-                    for (int i = 0; i < PIECES; ++i) copy16(dst + i * 512, k + i * 512);
+                    for (int j = 0; j < PIECES; ++j) copy16(dst + j * 512, k + j * 512);
 #pragma unroll
-                    for (int i = 0; i < PIECES; ++i) copy16(dst + 16 * D + i * 512, v + i * 512);
-                    const float *f = scales + (size_t)id * c.heads * 2;
-                    sc = make_float2(ld_dependent(f), ld_dependent(f + 1));
-                } else sc.x = -1.f;
+                    for (int j = 0; j < PIECES; ++j) copy16(dst + 16 * D + j * 512, v + j * 512);
+                }
             }
             copy_commit();
         };
-        float2 page_scale[Sh::kStages];                          // of the steps in flight
-        const int w0 = s0 + warp;
 #pragma unroll
-        for (int i = 0; i < Sh::kStages - 1; ++i) fetch(w0 + i * W, i, page_scale[i]);
+        for (int i = 0; i < Sh::kStages - 1; ++i) fetch(i, i);
 
         // ---- queries: rows of the tile as A operands, zero behind the last
         if (warp < 16) {
@@ -315,14 +332,15 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
                 }
             }
         };
-        for (int step = w0; step < s1;) {
-#pragma unroll
-            for (int i = 0; i < Sh::kStages; ++i) {
-                if (step >= s1) break;
-                fetch(step + (Sh::kStages - 1) * W, (i + Sh::kStages - 1) % Sh::kStages, page_scale[(i + Sh::kStages - 1) % Sh::kStages]);
-                copy_wait<Sh::kStages - 1>();
-                take(step, i, page_scale[i]);
-                step += W;
+        for (int i = 0, slot = 0; i < mine; ++i) {
+            if ((i & 31) == 0) next = look((i >> 5) + 1);
+            fetch(i + Sh::kStages - 1, slot == 0 ? Sh::kStages - 1 : slot - 1);
+            copy_wait<Sh::kStages - 1>();
+            take(s0 + warp + i * W, slot, make_float2(__shfl_sync(0xffffffffu, now.ks, i & 31), __shfl_sync(0xffffffffu, now.vs, i & 31)));
+            if (++slot == Sh::kStages) slot = 0;
+            if ((i & 31) == 31) {
+                now = next;
+                ++looked;
             }
         }
         copy_wait<0>();

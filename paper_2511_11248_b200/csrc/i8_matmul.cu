@@ -1,47 +1,62 @@
 // 8-bit integer products: token quantization and the choice of the kernel.
 #include "i8_pair.cuh"
-#include "i8_stream.cuh"
 
 namespace tman {
 namespace {
 
-// ---- token quantization: a row a CTA -----------------------------------------------------------------------------------------
-template <typename T>
-__global__ void __launch_bounds__(256) i8_quantize_kernel(const T *x, int ldx, int K, int8_t *a, float *row_scale)
+// ---- token quantization: a row a CTA, VPT pieces of eight values a thread, read once ----------------------------------------------
+template <typename T, int VPT>
+__global__ void __launch_bounds__(1024) i8_quantize_kernel(const T *x, int ldx, int K, int8_t *a, float *row_scale)
 {
-    __shared__ uint32_t tops[8];
+    __shared__ uint32_t tops[32];
     const int tid = threadIdx.x, pieces = K >> 3;
     const uint4 *row = reinterpret_cast<const uint4 *>(x + (size_t)blockIdx.x * ldx);
     uint2 *out = reinterpret_cast<uint2 *>(a + (size_t)blockIdx.x * K);
+    if (tid < 32) tops[tid] = 0;
+    __syncthreads();
     grid_wait();
     grid_launch_next();
+    uint4 v[VPT];
     uint32_t top = 0;
-    for (int i = tid; i < pieces; i += 256) {
-        const uint4 v = ld_dependent(row + i);
-        top = i8_larger(top, i8_larger(i8_larger(i8_magnitudes(v.x), i8_magnitudes(v.y)), i8_larger(i8_magnitudes(v.z), i8_magnitudes(v.w))));
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        const int at = tid + i * blockDim.x;
+        v[i] = at < pieces ? ld_dependent(row + at) : make_uint4(0, 0, 0, 0);
     }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+        top = i8_larger(top, i8_larger(i8_larger(i8_magnitudes(v[i].x), i8_magnitudes(v[i].y)), i8_larger(i8_magnitudes(v[i].z), i8_magnitudes(v[i].w))));
     top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16));
     if ((tid & 31) == 0) tops[tid >> 5] = top;
     __syncthreads();
-    top = __reduce_max_sync(0xffffffffu, tops[tid & 7]);
+    top = __reduce_max_sync(0xffffffffu, tops[tid & 31]);
     const float scale = top == 0 ? 1.f : i8_scale<T>(top);
     if (tid == 0) row_scale[blockIdx.x] = scale;
     const I8Divisor d(scale);
-    for (int i = tid; i < pieces; i += 256) out[i] = i8_codes<T>(d, ld_dependent(row + i));
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        const int at = tid + i * blockDim.x;
+        if (at < pieces) out[at] = i8_codes<T>(d, v[i]);
+    }
 }
 
 template <typename T> tman_status quantize(const void *x, int ldx, int M, int K, int8_t *a, float *row_scale, cudaStream_t s)
 {
+    // few rows: the latency of one row counts, as many threads as there are; many rows: four pieces a thread
+    const int pieces = K / 8, least = (pieces + 1023) / 1024, want = M > 2 * kGemvPlanSms && least < 4 ? 4 : least;
+    const int vpt = want <= 1 ? 1 : want <= 2 ? 2 : want <= 4 ? 4 : want <= 8 ? 8 : 16;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)M);
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3((unsigned)(((pieces + vpt - 1) / vpt + 31) / 32 * 32));
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return call_status(cudaLaunchKernelEx(&cfg, i8_quantize_kernel<T>, static_cast<const T *>(x), ldx, K, a, row_scale));
+    auto kern = vpt == 1 ? i8_quantize_kernel<T, 1> : vpt == 2 ? i8_quantize_kernel<T, 2> : vpt == 4 ? i8_quantize_kernel<T, 4> : vpt == 8 ? i8_quantize_kernel<T, 8>
+                                                                                                                                         : i8_quantize_kernel<T, 16>;
+    return call_status(cudaLaunchKernelEx(&cfg, kern, static_cast<const T *>(x), ldx, K, a, row_scale));
 }
 
 }  // namespace
@@ -51,20 +66,32 @@ tman_status launch_i8_quantize(const void *x, int ldx, int dtype, int M, int K, 
     return dtype == kF4TypeHalf ? quantize<__half>(x, ldx, M, K, a, row_scale, s) : quantize<__nv_bfloat16>(x, ldx, M, K, a, row_scale, s);
 }
 
-size_t i8_workspace_bytes(int, int, int) { return kWsStatusBytes; }
+// Rows of 16 bits whose codes every CTA of the product works out itself; others are quantized by a launch of their own.
+static bool i8_fused(int M, int K) { return (long long)M * K <= (M == 1 ? 16384 : 8192); }
+
+size_t i8_workspace_bytes(int op, int M, int K)
+{
+    return kWsStatusBytes + (op == 0 && !i8_fused(M, K) ? up256((size_t)M * K) + up256(M * sizeof(float)) : 0);
+}
 
 tman_status launch_i8_gemv(const int8_t *w, int ldw, const float *w_scale, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N,
-                           void *, cudaStream_t s)
+                           void *ws, cudaStream_t s)
 {
-    const I8StreamParams p = {w, x, w_scale, nullptr, y, ldw, ldx, ldy, M, K, N, 0};
-    return dtype == kF4TypeHalf ? launch_i8_stream<__half, false>(p, s) : launch_i8_stream<__nv_bfloat16, false>(p, s);
+    uint8_t *w8 = static_cast<uint8_t *>(ws);
+    const I8StreamParams p = {w, x, w_scale, nullptr, y, ldw, ldx, ldy, M, K, N, 0, 0};
+    if (i8_fused(M, K)) return dtype == kF4TypeHalf ? launch_i8_stream<__half, false>(p, s) : launch_i8_stream<__nv_bfloat16, false>(p, s);
+    int8_t *a = reinterpret_cast<int8_t *>(w8 + kWsStatusBytes);
+    float *a_scale = reinterpret_cast<float *>(w8 + kWsStatusBytes + up256((size_t)M * K));
+    const tman_status st = launch_i8_quantize(x, ldx, dtype, M, K, a, a_scale, s);
+    if (st != TMAN_OK) return st;
+    return launch_i8_gemm(w, ldw, w_scale, a, a_scale, y, ldy, dtype, M, K, N, ws, s);
 }
 
 tman_status launch_i8_gemm(const int8_t *w, int ldw, const float *w_scale, const int8_t *a, const float *a_scale, void *y, int ldy, int dtype, int M,
                            int K, int N, void *ws, cudaStream_t s)
 {
     if (M <= 8) {
-        const I8StreamParams p = {w, a, w_scale, a_scale, y, ldw, K, ldy, M, K, N, 0};
+        const I8StreamParams p = {w, a, w_scale, a_scale, y, ldw, K, ldy, M, K, N, 0, 0};
         return dtype == kF4TypeHalf ? launch_i8_stream<__half, true>(p, s) : launch_i8_stream<__nv_bfloat16, true>(p, s);
     }
     I8PairParams p = {};

@@ -7,7 +7,7 @@
 // What bounds it: 256 x 256 x 128 products take a pair 512 clocks, in which each CTA takes 32 KB from L2.
 #pragma once
 
-#include "i8.cuh"
+#include "i8_stream.cuh"
 
 #include <type_traits>
 
