@@ -16,13 +16,15 @@ namespace tman {
 namespace {
 
 constexpr int kPromptRows = 64;          // rows of a sequence from which the kernel for prompts takes it
+constexpr int kItemCost = 48;            // steps that beginning and ending a head are worth
 constexpr int kShortSteps = 96;          // heads of so few steps are not cut
 constexpr uint32_t kNoneYet = 0x7FA5A5A5u;      // what tman_workspace_init writes: a counter at rest
 
 template <int D> struct AttendShape {
     static constexpr int kWarps = D <= 128 ? 12 : 8, kThreads = 32 * kWarps, kStages = D == 64 ? 6 : D == 128 ? 4 : 3;
     static constexpr int kStep = 32 * D, kRing = kStages * kStep, kQ = 32 * D, kSmem = kWarps * kRing + kQ;
-    static_assert(kRing >= 16 * D * 4, "a warp's sums fit its ring");
+    static constexpr int kSumRow = D + 8;     // floats from a row of a warp's sums to the next: rows start at different banks
+    static_assert(kRing >= 16 * kSumRow * 4, "a warp's sums fit its ring");
 };
 
 struct AttendParams {
@@ -32,6 +34,7 @@ struct AttendParams {
     float *parts;
     uint32_t *counters;
     int ldq, ldy, group, window, least;  // group: query heads of a key head; sequences of `least` rows (tokens x group) and more are done elsewhere
+    uint32_t group_mul;                  // 2^32 / group, rounded up; 0: a group of one
     float scale;
 };
 
@@ -47,12 +50,15 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src)
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// Tokens of the first n rows (n and the group are below 2^16).
+__device__ __forceinline__ int token_of(const AttendParams &p, int n) { return p.group_mul ? (int)__umulhi((uint32_t)n, p.group_mul) : n; }
+
 // The keys that a tile of rows sees: tokens [lo, hi), and steps of 16 of them, one at least.
 struct TileKeys { int first, lo, hi, step0, steps; };            // first: position of the tile's first token
 __device__ __forceinline__ TileKeys tile_keys(const AttendParams &p, const CacheSeq &q, int tile)
 {
     TileKeys k;
-    const int rows = q.rows * p.group, i0 = tile * kAttendRows / p.group, i1 = min(tile * kAttendRows + kAttendRows - 1, rows - 1) / p.group;
+    const int rows = q.rows * p.group, i0 = token_of(p, tile * kAttendRows), i1 = token_of(p, min(tile * kAttendRows + kAttendRows - 1, rows - 1));
     k.first = q.len - q.rows + i0;
     k.hi = max(q.len - q.rows + i1 + 1, 0);
     k.lo = p.window > 0 ? max(k.first - p.window + 1, 0) : 0;
@@ -72,13 +78,12 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
     using Sh = AttendShape<D>;
     constexpr int W = Sh::kWarps, NT = D / 8, PIECES = D / 32;      // tiles of columns of the output, pieces of a lane
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long before[Sh::kThreads + 1];               // steps of the sequences in front of thread t's
+    __shared__ int before[Sh::kThreads + 1];                     // steps of the sequences in front of thread t's
     __shared__ CacheSeq known[Sh::kThreads];                     // the sequence of thread t, if each has one
-    __shared__ long long place[4];
-    __shared__ float row_factor[16], warp_max[W][16], warp_lmax[W][16], warp_sum[W][16];
+    __shared__ float row_factor[16], warp_max[W][16], warp_lmax[W][16], warp_sum[W][16], share_of[W][16], row_max[16], row_lmax[16], row_sum[16];
     __shared__ uint32_t last_flag;
     const CacheSeqs &c = p.c;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, page_mask = (1 << c.page_sh) - 1;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t = lane & 3, page_mask = (1 << c.page_sh) - 1;
     uint4 *qs = reinterpret_cast<uint4 *>(smem + W * Sh::kRing);
     const uint32_t ring = smem_u32(smem) + warp * Sh::kRing + lane * 16;
     const uint8_t *ring_at = smem + warp * Sh::kRing + lane * 16;
@@ -86,41 +91,43 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
     grid_launch_next();
 
     const int per = (c.S + Sh::kThreads - 1) / Sh::kThreads;
-    auto seq_of = [&](int s) { return per == 1 ? known[s] : cache_seq(c, s); };
-    auto units_of = [&](const CacheSeq &q) -> long long {
-        long long n = 0;
-        for (int i = 0; i < tiles_of(p, q); ++i) n += tile_keys(p, q, i).steps;
+    auto units_of = [&](const CacheSeq &q) {
+        int n = 0;
+#pragma unroll 1
+        for (int i = 0; i < tiles_of(p, q); ++i) n += tile_keys(p, q, i).steps + kItemCost;
         return n * c.heads;
     };
     {
-        long long mine = 0;
+        int mine = 0;
+#pragma unroll 1
         for (int s = min(tid * per, c.S); s < min(tid * per + per, c.S); ++s) {
             const CacheSeq q = cache_seq(c, s);
             if (per == 1) known[tid] = q;
             mine += units_of(q);
         }
-        long long upto = mine;
+        int upto = mine;
+#pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const long long o = __shfl_up_sync(0xffffffffu, upto, d);
+            const int o = __shfl_up_sync(0xffffffffu, upto, d);
             if (lane >= d) upto += o;
         }
+        if (lane == 31) warp_sum[0][warp] = __int_as_float(upto);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w) upto += w < warp ? __float_as_int(warp_sum[0][w]) : 0;
         before[tid + 1] = upto;
-        __syncthreads();
-        long long add = 0;
-        for (int w = 0; w < warp; ++w) add += before[w * 32 + 32];
-        __syncthreads();
-        before[tid + 1] = upto + add;
         if (tid == 0) before[0] = 0;
         __syncthreads();
     }
-    const long long total = before[Sh::kThreads];
-    long long run = (total + gridDim.x - 1) / gridDim.x;
-    run = max((run + W - 1) / W, 1ll) * W;
+    const int total = before[Sh::kThreads];                      // (below 2^31: checked by the host)
+    int run = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+    run = max((run + W - 1) / W, 1) * W;
 
     // Sequence, head and tile of a unit, by all threads alike.
-    struct Item { int s, head, tile; long long at; CacheSeq q; TileKeys k; };
-    auto item_of = [&](long long u) {
-        int lo = 0, hi = Sh::kThreads;
+    struct Item { int s, head, tile, at; CacheSeq q; TileKeys k; };      // at: unit of its first step
+    auto item_of = [&](int u) {
+        int lo = 0, hi = min(Sh::kThreads, c.S);
+#pragma unroll 1
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (before[mid] <= u) lo = mid; else hi = mid;
@@ -128,46 +135,53 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
         Item it;
         it.at = before[lo];
         it.s = lo * per;
-        for (;;) {
-            const long long n = per > 1 ? units_of(cache_seq(c, it.s)) : before[lo + 1] - before[lo];
-            if (u < it.at + n) break;
-            it.at += n;
-            ++it.s;
+        if (per == 1) it.q = known[lo];
+        else {
+#pragma unroll 1
+            for (;; ++it.s) {
+                it.q = cache_seq(c, it.s);
+                const int n = units_of(it.q);
+                if (u < it.at + n) break;
+                it.at += n;
+            }
         }
-        it.q = seq_of(it.s);
         const int tiles = tiles_of(p, it.q);
-        long long one = 0;
-        if (tiles > 1)
-            for (int i = 0; i < tiles; ++i) one += tile_keys(p, it.q, i).steps;
-        else one = tile_keys(p, it.q, 0).steps;
-        it.head = (int)((u - it.at) / one);
-        it.at += it.head * one;
         it.tile = 0;
-        for (;;) {
-            it.k = tile_keys(p, it.q, it.tile);
-            if (u < it.at + it.k.steps) break;
-            it.at += it.k.steps;
-            ++it.tile;
+        it.k = tile_keys(p, it.q, 0);
+        int one = it.k.steps + kItemCost;
+#pragma unroll 1
+        for (int i = 1; i < tiles; ++i) one += tile_keys(p, it.q, i).steps + kItemCost;
+        it.head = (u - it.at) / one;
+        it.at += it.head * one;
+#pragma unroll 1
+        while (u >= it.at + kItemCost + it.k.steps) {
+            it.at += kItemCost + it.k.steps;
+            it.k = tile_keys(p, it.q, ++it.tile);
         }
+        it.at += kItemCost;
         return it;
     };
-    // Where the runs of the CTAs begin: a short head belongs to the CTA that its first step falls to.
-    auto begin_of = [&](long long cta) {
-        const long long u = cta * run;
-        if (u >= total || u <= 0) return u <= 0 ? 0ll : total;
-        const Item it = item_of(u);
-        return it.at != u && it.k.steps <= kShortSteps ? it.at + it.k.steps : u;
-    };
-    if (tid < 2) place[tid] = begin_of((long long)blockIdx.x + tid);
-    __syncthreads();
-    const long long begin = place[0], end = place[1];
-
-    for (long long u = begin; u < end;) {
-        const Item it = item_of(u);
-        const int s0 = (int)(u - it.at), s1 = (int)min((long long)it.k.steps, end - it.at);       // steps of this run
+    // The first turn finds where the runs of this CTA and of the next begin (lanes 0 and 1): a short head belongs to the CTA that its first step
+    // falls to.
+    int u = 0, end = 0;
+#pragma unroll 1
+    for (int turn = 0;; ++turn) {
+        const long long from = ((long long)blockIdx.x + (lane & 1)) * run;
+        const int at_u = turn > 0 ? u : from < total ? (int)from : total;
+        Item it = {};
+        if (at_u < total) it = item_of(at_u);
+        if (turn == 0) {
+            const int begin = at_u < total && at_u > it.at && it.k.steps <= kShortSteps ? it.at + it.k.steps : at_u;
+            u = __shfl_sync(0xffffffffu, begin, 0);
+            end = __shfl_sync(0xffffffffu, begin, 1);
+            if (u >= end) break;
+            continue;
+        }
+        const int s0 = max(u - it.at, 0), s1 = min(it.k.steps, end - it.at);       // steps of this run
         const bool whole = s0 == 0 && s1 == it.k.steps;
         const int rows = min(kAttendRows, it.q.rows * p.group - it.tile * kAttendRows);
-        u = it.at + s1;
+        u = it.at + it.k.steps;
+        if (s1 <= s0) break;                                     // (the run ends in front of the head's first step)
 
         // ---- the warp's first copies
         const uint8_t *codes = c.cache + (size_t)it.head * 2 * D * (page_mask + 1);
@@ -206,50 +220,56 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
             }
             copy_commit();
         };
+        // Queries on their way: rows warp and warp + W of the tile.
+        constexpr int QR = (16 + W - 1) / W, QW = (D / 4 + 31) / 32;
+        uint2 raw[QR][QW];
 #pragma unroll
+        for (int a = 0; a < QR; ++a) {
+            const int r = warp + a * W, rho = it.tile * kAttendRows + min(r, rows - 1), i = token_of(p, rho);
+            const T *src = static_cast<const T *>(p.q) + (size_t)(it.q.row + i) * p.ldq + (size_t)(it.head * p.group + rho - i * p.group) * D;
+#pragma unroll
+            for (int b = 0; b < QW; ++b) {
+                raw[a][b] = make_uint2(0, 0);
+                if (r < rows && lane + 32 * b < D / 4)
+                    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(raw[a][b].x), "=r"(raw[a][b].y) : "l"(reinterpret_cast<const uint2 *>(src) + lane + 32 * b) : "memory");
+            }
+        }
+#pragma unroll 1
         for (int i = 0; i < Sh::kStages - 1; ++i) fetch(i, i);
 
-        // ---- queries: rows of the tile as A operands, zero behind the last
-        if (warp < 16) {
-            for (int r = warp; r < 16; r += W) {
-                const int rho = it.tile * kAttendRows + r;
+        // ---- queries as A operands, zero behind the last row: columns 64 i + 16 t + 4 j of row r in step 4 i + j of k, lane 4 (r % 8) + t, words r / 8 and r / 8 + 2
+#pragma unroll
+        for (int a = 0; a < QR; ++a) {
+            const int r = warp + a * W;
+            if (r >= 16) break;
+            float f = 1.f;
+            if constexpr (!std::is_same<T, __half>::value) {
                 uint32_t top = 0;
-                const T *src = static_cast<const T *>(p.q) + (size_t)(it.q.row + rho / p.group) * p.ldq + (size_t)(it.head * p.group + rho % p.group) * D;
-                float f = 1.f;
+#pragma unroll
+                for (int b = 0; b < QW; ++b) top = i8_larger(top, i8_larger(i8_magnitudes(raw[a][b].x), i8_magnitudes(raw[a][b].y)));
+                top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16));
+                // largest value in [2^e, 2^(e + 1)), e = top / 128 - 127
+                f = top == 0 || top >= i8_infinity<T>() ? 1.f : __uint_as_float((uint32_t)(127 + min(141 - (int)(top >> 7), 100)) << 23);
+            }
+            if (lane == 0) row_factor[r] = p.scale * kLog2e / f;
+#pragma unroll
+            for (int b = 0; b < QW; ++b) {
+                const int i = lane + 32 * b;
+                if (i >= D / 4) break;
+                uint2 h = raw[a][b];
                 if constexpr (!std::is_same<T, __half>::value) {
-                    if (r < rows)
-                        for (int i = lane; i < D / 8; i += 32) {
-                            const uint4 v = ld_dependent(reinterpret_cast<const uint4 *>(src) + i);
-                            top = i8_larger(top, i8_larger(i8_larger(i8_magnitudes(v.x), i8_magnitudes(v.y)), i8_larger(i8_magnitudes(v.z), i8_magnitudes(v.w))));
-                        }
-                    top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16));
-                    const int e = (int)(top >> 7) - 127;          // largest value in [2^e, 2^(e + 1))
-                    f = top == 0 || top >= i8_infinity<T>() ? 1.f : __uint_as_float((uint32_t)(127 + min(14 - e, 100)) << 23);
+                    const float2 x = f4_to_float2<T>(h.x), y = f4_to_float2<T>(h.y);
+                    h = make_uint2(f4_from_float2<__half>(x.x * f, x.y * f), f4_from_float2<__half>(y.x * f, y.y * f));
                 }
-                if (lane == 0) row_factor[r] = p.scale * kLog2e / f;
-                // columns 64 i + 16 t + 4 j of row r: step 4 i + j of k, lane 4 (r % 8) + t, words (r / 8) and (r / 8) + 2
-                for (int i = lane; i < D / 4; i += 32) {
-                    uint2 h = make_uint2(0, 0);
-                    if (r < rows) {
-                        uint2 raw;
-                        asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(raw.x), "=r"(raw.y) : "l"(reinterpret_cast<const uint2 *>(src) + i) : "memory");
-                        if constexpr (std::is_same<T, __half>::value) h = raw;
-                        else {
-                            const float2 a = f4_to_float2<T>(raw.x), b = f4_to_float2<T>(raw.y);
-                            h = make_uint2(f4_from_float2<__half>(a.x * f, a.y * f), f4_from_float2<__half>(b.x * f, b.y * f));
-                        }
-                    }
-                    const int step = (i >> 4) * 4 + (i & 3), l = (r & 7) * 4 + ((i >> 2) & 3);
-                    uint32_t *at = reinterpret_cast<uint32_t *>(qs + step * 32 + l) + (r >> 3);
-                    at[0] = h.x;
-                    at[2] = h.y;
-                }
+                uint32_t *at = reinterpret_cast<uint32_t *>(qs + ((i >> 4) * 4 + (i & 3)) * 32 + (r & 7) * 4 + ((i >> 2) & 3)) + (r >> 3);
+                at[0] = h.x;
+                at[2] = h.y;
             }
         }
         __syncthreads();
 
         const float rf0 = row_factor[g], rf1 = row_factor[g + 8];
-        auto limit_of = [&](int r) { return it.q.len - it.q.rows + (it.tile * kAttendRows + min(r, rows - 1)) / p.group; };
+        auto limit_of = [&](int r) { return it.q.len - it.q.rows + token_of(p, it.tile * kAttendRows + min(r, rows - 1)); };
         const int lim0 = limit_of(g), lim1 = limit_of(g + 8);
         const int low0 = p.window > 0 ? lim0 - p.window + 1 : INT_MIN, low1 = p.window > 0 ? lim1 - p.window + 1 : INT_MIN;
         const int all_from = p.window > 0 ? it.k.hi - p.window : INT_MIN;       // tokens [all_from, first] are seen by every row
@@ -367,45 +387,59 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
         float *os = reinterpret_cast<float *>(smem + warp * Sh::kRing);
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            *reinterpret_cast<float2 *>(os + g * D + 8 * i + 2 * t) = make_float2(o[i][0], o[i][1]);
-            *reinterpret_cast<float2 *>(os + (g + 8) * D + 8 * i + 2 * t) = make_float2(o[i][2], o[i][3]);
+            *reinterpret_cast<float2 *>(os + g * Sh::kSumRow + 8 * i + 2 * t) = make_float2(o[i][0], o[i][1]);
+            *reinterpret_cast<float2 *>(os + (g + 8) * Sh::kSumRow + 8 * i + 2 * t) = make_float2(o[i][2], o[i][3]);
         }
         __syncthreads();
-        const long long first_cta = it.at / run;
-        float *part = p.parts + ((size_t)blockIdx.x * 2 + (s0 == 0 ? 1 : 0)) * (kAttendRows * (D + 4));
-        // y of (row, column) from sums relative to `m`, probabilities relative to `lm`
-        auto store = [&](int r, int col, float v, float m, float lm, float l) {
-            const int rho = it.tile * kAttendRows + r;
-            const float out = l == 0.f ? 0.f : v * exp2_fast((m == -INFINITY ? 0.f : m) - (lm == -INFINITY ? 0.f : lm)) / l;
-            static_cast<T *>(p.y)[(size_t)(it.q.row + rho / p.group) * p.ldy + (size_t)(it.head * p.group + rho % p.group) * D + col] = f4_from_float<T>(out);
-        };
-        for (int i = tid; i < rows * D; i += Sh::kThreads) {
-            const int r = i / D, col = i % D;
-            float m = -INFINITY, lm = -INFINITY;
+        const int first_cta = it.at / run, cells = rows * (D / 4);
+        if (tid < W * 16) {
+            const int w = tid >> 4, r = tid & 15;
+            float m = -INFINITY, lm = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                m = fmaxf(m, warp_max[w][r]);
-                lm = fmaxf(lm, warp_lmax[w][r]);
+            for (int i = 0; i < W; ++i) {
+                m = fmaxf(m, warp_max[i][r]);
+                lm = fmaxf(lm, warp_lmax[i][r]);
             }
-            const float um = m == -INFINITY ? 0.f : m, ul = lm == -INFINITY ? 0.f : lm;
-            float v = 0.f, l = 0.f;
+            share_of[w][r] = exp2_fast(warp_max[w][r] - (m == -INFINITY ? 0.f : m));
+            if (w == 0) {
+                const float ul = lm == -INFINITY ? 0.f : lm;
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                v += reinterpret_cast<const float *>(smem + w * Sh::kRing)[i] * exp2_fast(warp_max[w][r] - um);
-                l += warp_sum[w][r] * exp2_fast(warp_lmax[w][r] - ul);
-            }
-            if (whole) store(r, col, v, m, lm, l);
-            else {
-                __stcg(part + i, v);
-                if (col == 0) {
-                    __stcg(part + 16 * D + r, m);
-                    __stcg(part + 16 * D + 16 + r, lm);
-                    __stcg(part + 16 * D + 32 + r, l);
-                }
+                for (int i = 0; i < W; ++i) l += warp_sum[i][r] * exp2_fast(warp_lmax[i][r] - ul);
+                row_max[r] = m;
+                row_lmax[r] = lm;
+                row_sum[r] = l;
             }
         }
+        __syncthreads();
+        // y of four columns from their sums, relative to row_max, and the row's probabilities, relative to row_lmax
+        auto store = [&](int r, int col, float4 v) {
+            const int rho = it.tile * kAttendRows + r, i = token_of(p, rho);
+            const float m = row_max[r], lm = row_lmax[r], l = row_sum[r];
+            const float f = l == 0.f ? 0.f : exp2_fast((m == -INFINITY ? 0.f : m) - (lm == -INFINITY ? 0.f : lm)) / l;
+            T *at = static_cast<T *>(p.y) + (size_t)(it.q.row + i) * p.ldy + (size_t)(it.head * p.group + rho - i * p.group) * D + col;
+            *reinterpret_cast<uint2 *>(at) = make_uint2(f4_from_float2<T>(v.x * f, v.y * f), f4_from_float2<T>(v.z * f, v.w * f));
+        };
+        float *part = p.parts + ((size_t)blockIdx.x * 2 + (s0 == 0 ? 1 : 0)) * (kAttendRows * (D + 4));
+#pragma unroll 1
+        for (int i = tid; i < cells; i += Sh::kThreads) {
+            const int r = i / (D / 4);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float4 x = *reinterpret_cast<const float4 *>(smem + w * Sh::kRing + (r * Sh::kSumRow + i % (D / 4) * 4) * 4);
+                const float f = share_of[w][r];
+                v = make_float4(fmaf(x.x, f, v.x), fmaf(x.y, f, v.y), fmaf(x.z, f, v.z), fmaf(x.w, f, v.w));
+            }
+            if (whole) store(r, i % (D / 4) * 4, v);
+            else __stcg(reinterpret_cast<float4 *>(part) + i, v);
+        }
         if (!whole) {
-            const int pieces = (int)((it.at + it.k.steps - 1) / run - first_cta) + 1;
+            if (tid < rows) {
+                __stcg(part + 16 * D + tid, row_max[tid]);
+                __stcg(part + 16 * D + 16 + tid, row_lmax[tid]);
+                __stcg(part + 16 * D + 32 + tid, row_sum[tid]);
+            }
+            const int pieces = (it.at + it.k.steps - 1) / run - first_cta + 1;
             __threadfence();
             __syncthreads();
             if (tid == 0) {
@@ -416,24 +450,75 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
             }
             __syncthreads();
             if (last_flag) {
+                // ---- all parts of the head, in their order: first what each counts for, then the sums
                 auto part_of = [&](int i) { return p.parts + ((size_t)(first_cta + i) * 2 + (i == 0 ? 1 : 0)) * (kAttendRows * (D + 4)); };
-                for (int i = tid; i < rows * D; i += Sh::kThreads) {
-                    const int r = i / D, col = i % D;
-                    float m = -INFINITY, lm = -INFINITY, v = 0.f, l = 0.f;
-                    for (int k = 0; k < pieces; ++k) {
-                        m = fmaxf(m, __ldcg(part_of(k) + 16 * D + r));
-                        lm = fmaxf(lm, __ldcg(part_of(k) + 16 * D + 16 + r));
+                float *pm = reinterpret_cast<float *>(smem), *plm = pm + kAttendCtas * 16, *pl = plm + kAttendCtas * 16;
+                float4 *sums = reinterpret_cast<float4 *>(pl + kAttendCtas * 16);
+                for (int i = tid; i < pieces * 16; i += Sh::kThreads) {
+                    const int k = i >> 4, r = i & 15;
+                    if (r < rows) {
+                        const float *at = part_of(k) + 16 * D + r;
+                        pm[i] = __ldcg(at);
+                        plm[i] = __ldcg(at + 16);
+                        pl[i] = __ldcg(at + 32);
+                    }
+                }
+                __syncthreads();
+                for (int r = warp; r < rows; r += W) {
+                    float m = -INFINITY, lm = -INFINITY, l = 0.f;
+                    for (int k = lane; k < pieces; k += 32) {
+                        m = fmaxf(m, pm[k * 16 + r]);
+                        lm = fmaxf(lm, plm[k * 16 + r]);
+                    }
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) {
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                        lm = fmaxf(lm, __shfl_xor_sync(0xffffffffu, lm, d));
                     }
                     const float um = m == -INFINITY ? 0.f : m, ul = lm == -INFINITY ? 0.f : lm;
-                    for (int k = 0; k < pieces; ++k) {
-                        v += __ldcg(part_of(k) + i) * exp2_fast(__ldcg(part_of(k) + 16 * D + r) - um);
-                        l += __ldcg(part_of(k) + 16 * D + 32 + r) * exp2_fast(__ldcg(part_of(k) + 16 * D + 16 + r) - ul);
+                    for (int k = lane; k < pieces; k += 32) {
+                        l += pl[k * 16 + r] * exp2_fast(plm[k * 16 + r] - ul);
+                        pm[k * 16 + r] = exp2_fast(pm[k * 16 + r] - um);
                     }
-                    store(r, col, v, m, lm, l);
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+                    if (lane == 0) {
+                        row_max[r] = m;
+                        row_lmax[r] = lm;
+                        row_sum[r] = l;
+                    }
+                }
+                __syncthreads();
+                // (few cells: several threads share the parts of one)
+                const int teams = cells * 4 <= Sh::kThreads ? 4 : cells * 2 <= Sh::kThreads ? 2 : 1;
+#pragma unroll 1
+                for (int i = tid; i < cells * teams; i += Sh::kThreads) {
+                    const int cell = i % cells, team = i / cells, r = cell / (D / 4);
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+                    for (int k = team; k < pieces; k += teams) {
+                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(part_of(k)) + cell);
+                        const float f = pm[k * 16 + r];
+                        v = make_float4(fmaf(x.x, f, v.x), fmaf(x.y, f, v.y), fmaf(x.z, f, v.z), fmaf(x.w, f, v.w));
+                    }
+                    if (teams == 1) store(r, cell % (D / 4) * 4, v);
+                    else sums[i] = v;
+                }
+                if (teams > 1) {
+                    __syncthreads();
+                    if (tid < cells) {
+                        float4 v = sums[tid];
+                        for (int k = 1; k < teams; ++k) {
+                            const float4 x = sums[k * cells + tid];
+                            v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+                        }
+                        store(tid / (D / 4), tid % (D / 4) * 4, v);
+                    }
                 }
             }
         }
         __syncthreads();
+        if (u >= end) break;
     }
 }
 
@@ -445,6 +530,10 @@ template <typename T, int D> tman_status launch(AttendParams p, cudaStream_t s)
     const DeviceInfo *info = device_info(&dev);
     if (!info) return TMAN_ERR_CUDA;
     const int sms = info->sms.load(std::memory_order_relaxed);
+    // steps are counted in 32 bits
+    const long long steps = ((long long)p.c.ldt << p.c.page_sh) / 16 + kItemCost, rows = p.c.starts ? (long long)p.c.T * p.group : p.group;
+    const long long tiles = ((rows < p.least ? rows : p.least) + kAttendRows - 1) / kAttendRows;
+    if (tiles * steps > INT32_MAX || tiles * steps * p.c.heads > INT32_MAX || tiles * steps * p.c.heads * p.c.S > INT32_MAX) return TMAN_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(sms < kAttendCtas ? sms : kAttendCtas));
     cfg.blockDim = dim3(AttendShape<D>::kThreads);
@@ -486,8 +575,9 @@ tman_status launch_attend_i8(const CacheSeqs &c, const void *q, int ldq, void *y
                              cudaStream_t s)
 {
     uint8_t *w8 = static_cast<uint8_t *>(ws);
+    const int group = q_heads / c.heads;
     const AttendParams p = {c, q, y, reinterpret_cast<float *>(w8 + kWsStatusBytes + kAttendCtas * 4), reinterpret_cast<uint32_t *>(w8 + kWsStatusBytes),
-                            ldq, ldy, q_heads / c.heads, window, INT_MAX, scale};
+                            ldq, ldy, group, window, INT_MAX, group == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)group + 1u, scale};
     return dtype == kF4TypeHalf ? launch_width<__half>(p, s) : launch_width<__nv_bfloat16>(p, s);
 }
 
