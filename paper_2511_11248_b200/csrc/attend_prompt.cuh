@@ -1,9 +1,9 @@
 // Attention over the 8-bit cache for many new tokens of a sequence.
 //
 // What bounds it is the exponential function (16 a clock and SM) and the tensor cores, which take as long.  A CTA has up to 256 rows (new tokens x
-// query heads of one key head) in two tiles of 128, and walks over the keys 128 at a time (64 where heads are wide).  Eight warps bring keys and values from
+// query heads of one key head) in two tiles of 128, and walks over the keys 128 at a time (64 where heads are wide).  Four warps bring keys and values from
 // the cache, make fp16 of the bytes and lay them out as the tensor cores' operands; one thread issues the MMAs (scores: rows x keys; output: rows x
-// columns, both in tensor memory); four warps a tile of rows, one thread a row, do the softmax.  While one tile's scores are worked on, the
+// columns, both in tensor memory); eight warps a tile of rows, two threads a row, do the softmax.  While one tile's scores are worked on, the
 // other's are multiplied.
 // A thread reads its row of scores twice, for the maximum and for the probabilities, which go back to tensor memory as the A operand of the second
 // product, over the scores.  A key's score is (q . code) x (key page's scale) x scale; probabilities carry the value page's scale, p' = 2^(s + log2 vs - M), so that
@@ -17,9 +17,12 @@ namespace tman {
 namespace {
 
 template <int D> struct PromptShape {
-    static constexpr int kKeys = D <= 128 ? 128 : 64, kTiles = D <= 192 ? 2 : 1, kSoft = 4 * kTiles, kLoad = 8;
-    static constexpr int kThreads = 32 * (kSoft + kLoad + 1), kRows = 128 * kTiles;
+    static constexpr int kKeys = D <= 128 ? 128 : 64, kTiles = D <= 192 ? 2 : 1, kSoft = 8 * kTiles, kLoad = 4;
+    static constexpr int kThreads = 32 * (kSoft + kLoad + 4), kRows = 128 * kTiles;
     static constexpr int kQ = kRows * D * 2, kKv = kKeys * D * 2, kSmem = kQ + 4 * kKv + 1024;
+    // Registers: with two tiles of rows the threads that work take what the fourth of a warpgroup that issues leaves (24 warps of 80 at launch).
+    static constexpr bool kSplit = kTiles == 2;
+    static_assert(!kSplit || (kThreads == 768 && 128 * (4 * 88 + 96 + 32) <= 768 * 80), "what the block is launched with");
     static constexpr int kScore = 0, kOut = kTiles * kKeys;      // columns of tensor memory
     static_assert(kOut + kTiles * D <= 512 && kSmem <= 227 * 1024, "it fits");
 };
@@ -32,6 +35,22 @@ struct PromptParams {
     float scale;
 };
 
+constexpr float kPromptSlack = 10.f;     // a score above the maximum so far by this much raises it
+
+// Pairs of numbers in one instruction.
+__device__ __forceinline__ float2 two(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
+    return *reinterpret_cast<float2 *>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return *reinterpret_cast<float2 *>(&r);
+}
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <typename T, int D>
@@ -40,9 +59,11 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
     using Sh = PromptShape<D>;
     constexpr int KT = Sh::kKeys, RT = Sh::kTiles, GROUPS = KT / 16;
     extern __shared__ __align__(1024) uint8_t prompt_smem[];
-    __shared__ __align__(8) uint64_t q_bar, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+    __shared__ __align__(8) uint64_t q_bar, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], pair_bar[4 * RT];
     __shared__ uint32_t tmem_slot;
     __shared__ float4 page_consts[4][GROUPS];                    // of 16 keys: scale of the keys, log2 of the values' scale and its reciprocal
+    __shared__ float row_of[Sh::kSoft][32];                      // what the two threads of a row tell each other
+    __shared__ uint32_t votes[Sh::kSoft];
     __shared__ int found[2], sums[Sh::kThreads / 32 + 1];
     const CacheSeqs &c = p.c;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, page_mask = (1 << c.page_sh) - 1;
@@ -50,16 +71,17 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
     uint8_t *smem = prompt_smem + (base - smem_u32(prompt_smem));
     const uint32_t qs = base, ks = base + Sh::kQ, vs = ks + 2 * Sh::kKv;
     if (tid == 0) {
-        mbar_init(smem_u32(&q_bar), 4 * RT);
+        mbar_init(smem_u32(&q_bar), 8 * RT);
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&k_full[i]), Sh::kLoad);
             mbar_init(smem_u32(&v_full[i]), Sh::kLoad);
             mbar_init(smem_u32(&k_empty[i]), 1);
             mbar_init(smem_u32(&v_empty[i]), 1);
             mbar_init(smem_u32(&s_full[i]), 1);
-            mbar_init(smem_u32(&p_full[i]), 4);
+            mbar_init(smem_u32(&p_full[i]), 8);
             mbar_init(smem_u32(&o_full[i]), 1);
         }
+        for (int i = 0; i < 4 * RT; ++i) mbar_init(smem_u32(&pair_bar[i]), 2);
         found[0] = -1;
         fence_barrier_init();
     }
@@ -117,7 +139,16 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
 
     if (warp < Sh::kSoft) {
         // ---- softmax: a thread has a row
-        const int r = warp >> 2, local = (warp & 3) * 32 + lane, row = r * 128 + local;
+        if constexpr (Sh::kSplit) asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
+        const int r = warp >> 3, half = (warp >> 2) & 1, local = (warp & 3) * 32 + lane, row = r * 128 + local, other = warp ^ 4;
+        uint32_t turn = 0;
+        auto meet = [&] {                                        // the two warps of the same rows
+            const uint32_t bar = smem_u32(&pair_bar[r * 4 + (warp & 3)]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+            ok = warp_all(mbar_wait(bar, turn)) && ok;
+            turn ^= 1u;
+        };
         if (r >= active) {
             if (lane == 0) mbar_arrive(smem_u32(&q_bar));
         } else {
@@ -136,7 +167,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                 f = top == 0 || top >= i8_infinity<T>() ? 1.f : __uint_as_float((uint32_t)(127 + min(141 - (int)(top >> 7), 100)) << 23);
             }
 #pragma unroll 4
-            for (int i = 0; i < D / 8; ++i) {
+            for (int i = half * (D / 16); i < (half + 1) * (D / 16); ++i) {
                 uint4 v = make_uint4(0, 0, 0, 0);
                 if (real) v = ld_dependent(reinterpret_cast<const uint4 *>(src) + i);
                 if constexpr (!std::is_same<T, __half>::value) {
@@ -154,74 +185,97 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             const int limit = pos0 + token, low = p.window > 0 ? limit - p.window + 1 : INT_MIN;
             const int least_limit = __reduce_min_sync(0xffffffffu, limit), most_low = __reduce_max_sync(0xffffffffu, low);
             const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16), score = at + Sh::kScore + r * KT, out = at + Sh::kOut + r * D;
+            constexpr int HC = KT / 2, HD = D / 2;               // columns of scores and of the output that a thread has
             float M = -INFINITY, l = 0.f;
             for (int j = 0; j < tiles; ++j) {
-                const int k0 = (tile0 + j) * KT;
-                const bool plain = k0 + KT - 1 <= least_limit && k0 >= most_low;
+                const int k0 = (tile0 + j) * KT + half * HC;
+                const bool plain = k0 + HC - 1 <= least_limit && k0 >= most_low;
                 const int upto = limit - k0, from = low == INT_MIN ? INT_MIN : low - k0;      // columns that this row sees
-                const float4 *consts = page_consts[j & 3];
+                const float4 *consts = page_consts[j & 3] + half * (GROUPS / 2);
                 ok = warp_all(mbar_wait(smem_u32(&s_full[r]), j & 1)) && ok;
                 if (!ok) break;
                 tcgen05_fence_after();
-                float mx = -INFINITY;
+                uint32_t h[HC / 2];
+                float sum;
 #pragma unroll 1
-                for (int i = 0; i < KT; i += 32) {
-                    uint32_t z[32];
-                    tcgen05_ld_32x32b_x32(score + (uint32_t)i, z);
-                    const float4 c0 = consts[i >> 4], c1 = consts[(i >> 4) + 1];
-                    const float f0 = c0.x * rf, f1 = c1.x * rf;
-                    tcgen05_wait_ld();
-                    if (plain) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) mx = fmaxf(mx, fmaf(__uint_as_float(z[e]), e < 16 ? f0 : f1, e < 16 ? c0.y : c1.y));
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const float t = fmaf(__uint_as_float(z[e]), e < 16 ? f0 : f1, e < 16 ? c0.y : c1.y);
-                            mx = fmaxf(mx, i + e <= upto && i + e >= from ? t : -INFINITY);
-                        }
-                    }
-                }
-                if (__any_sync(0xffffffffu, mx > M + 8.f || (M == -INFINITY && mx != M))) {
-                    const float next = mx > M + 8.f || M == -INFINITY ? fmaxf(mx, M) : M;
-                    const float g = next == M ? 1.f : exp2_fast(M - next);
-                    M = next;
-                    l *= g;
-                    if (j > 0) {
+                for (bool raise = j == 0;; raise = true) {
+                    if (raise) {                                 // the maximum first
+                        float mx = -INFINITY;
 #pragma unroll 1
-                        for (int i = 0; i < D; i += 16) {
-                            uint32_t z[16];
-                            tcgen05_ld_32x32b_x16(out + (uint32_t)i, z);
+                        for (int i = 0; i < HC; i += 32) {
+                            uint32_t z[32];
+                            tcgen05_ld_32x32b_x32(score + (uint32_t)(half * HC + i), z);
+                            const float4 c0 = consts[i >> 4], c1 = consts[(i >> 4) + 1];
+                            const float f0 = c0.x * rf, f1 = c1.x * rf;
                             tcgen05_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(__uint_as_float(z[e]) * g);
-                            tcgen05_st_32x32b_x16(out + (uint32_t)i, z);
+                            for (int e = 0; e < 32; ++e) {
+                                const float x = fmaf(__uint_as_float(z[e]), e < 16 ? f0 : f1, e < 16 ? c0.y : c1.y);
+                                mx = fmaxf(mx, i + e <= upto && i + e >= from ? x : -INFINITY);
+                            }
                         }
-                    }
-                }
-                const float Mu = M == -INFINITY ? 0.f : M;
+                        row_of[warp][lane] = mx;
+                        meet();
+                        mx = fmaxf(mx, row_of[other][lane]);
+                        const float next = mx > M + kPromptSlack || M == -INFINITY ? fmaxf(mx, M) : M;
+                        const float g = next == M ? 1.f : exp2_fast(M - next);
+                        M = next;
+                        l *= g;
+                        if (j > 0) {
 #pragma unroll 1
-                for (int i = 0; i < KT; i += 32) {
-                    uint32_t z[32], h[16];
-                    tcgen05_ld_32x32b_x32(score + (uint32_t)i, z);
-                    const float4 c0 = consts[i >> 4], c1 = consts[(i >> 4) + 1];
-                    const float f0 = c0.x * rf, f1 = c1.x * rf, b0 = c0.y - Mu, b1 = c1.y - Mu;
-                    tcgen05_wait_ld();
-                    float l0 = 0.f, l1 = 0.f;
+                            for (int i = half * HD; i < (half + 1) * HD; i += 16) {
+                                uint32_t z[16];
+                                tcgen05_ld_32x32b_x16(out + (uint32_t)i, z);
+                                tcgen05_wait_ld();
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        float a = exp2_fast(fmaf(__uint_as_float(z[e]), e < 16 ? f0 : f1, e < 16 ? b0 : b1));
-                        float b = exp2_fast(fmaf(__uint_as_float(z[e + 1]), e < 16 ? f0 : f1, e < 16 ? b0 : b1));
-                        if (!plain) {
-                            a = i + e <= upto && i + e >= from ? a : 0.f;
-                            b = i + e + 1 <= upto && i + e + 1 >= from ? b : 0.f;
+                                for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(__uint_as_float(z[e]) * g);
+                                tcgen05_st_32x32b_x16(out + (uint32_t)i, z);
+                            }
                         }
-                        if (e < 16) l0 += a + b; else l1 += a + b;
-                        h[e / 2] = f4_from_float2<__half>(a, b);
                     }
-                    l += l0 * c0.z + l1 * c1.z;
-                    tcgen05_st_32x32b_x16(score + (uint32_t)(i / 2), h);
+                    const float Mu = M == -INFINITY ? 0.f : M;
+                    float mx = -INFINITY;
+                    sum = 0.f;
+                    uint32_t z[2][32];
+                    tcgen05_ld_32x32b_x32(score + (uint32_t)(half * HC), z[0]);
+#pragma unroll
+                    for (int i = 0; i < HC / 32; ++i) {
+                        uint32_t (&y)[32] = z[i & 1];
+                        float4 c0, c1;                           // (read here and not earlier: all of them would take 32 registers)
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(c0.x), "=f"(c0.y), "=f"(c0.z), "=f"(c0.w) : "r"(smem_u32(consts + 2 * i)) : "memory");
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(c1.x), "=f"(c1.y), "=f"(c1.z), "=f"(c1.w) : "r"(smem_u32(consts + 2 * i + 1)) : "memory");
+                        const float2 f0 = two(c0.x * rf), f1 = two(c1.x * rf), b0 = two(c0.y - Mu), b1 = two(c1.y - Mu);
+                        tcgen05_wait_ld();
+                        if (i + 1 < HC / 32) tcgen05_ld_32x32b_x32(score + (uint32_t)(half * HC + 32 * (i + 1)), z[(i + 1) & 1]);
+                        float x[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[e] = fmaf(__uint_as_float(y[e]), e < 16 ? f0.x : f1.x, e < 16 ? b0.x : b1.x);
+                        if (!plain) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] = 32 * i + e <= upto && 32 * i + e >= from ? x[e] : -INFINITY;
+                        }
+                        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            mx = fmaxf(mx, fmaxf(x[e], x[e + 1]));
+                            const float u = exp2_fast(x[e]), v = exp2_fast(x[e + 1]);
+                            if (e < 16) { s0 += u; s1 += v; } else { s2 += u; s3 += v; }
+                            h[16 * i + e / 2] = f4_from_float2<__half>(u, v);
+                        }
+                        sum = fmaf(s0 + s1, c0.z, fmaf(s2 + s3, c1.z, sum));
+                        asm volatile("" : "+f"(sum), "+f"(mx));          // (added up here: put off, the 32 values would stay in registers)
+                    }
+                    // Both threads of a row raise it, or none (once: what the maximum was taken of is rounded apart from this by less than a unit).  Behind
+                    // the meeting all scores have been read.
+                    const bool above = __any_sync(0xffffffffu, mx > kPromptSlack || (M == -INFINITY && mx != -INFINITY));
+                    if (lane == 0) votes[warp] = above;
+                    meet();
+                    const bool again = !raise && (above || *reinterpret_cast<volatile uint32_t *>(&votes[other]) != 0);
+                    if (!again || !ok) break;
                 }
+                l += sum;
+#pragma unroll
+                for (int i = 0; i < HC / 2; i += 16) tcgen05_st_32x32b_x16(score + (uint32_t)(half * (HC / 2) + i), *reinterpret_cast<uint32_t(*)[16]>(h + i));
                 tcgen05_wait_st();
                 tcgen05_fence_before();
                 __syncwarp();
@@ -230,10 +284,13 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             if (ok) {
                 ok = warp_all(mbar_wait(smem_u32(&o_full[r]), 0));
                 tcgen05_fence_after();
+                row_of[warp][lane] = l;
+                meet();
+                l += row_of[other][lane];
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 T *dst = static_cast<T *>(p.y) + (size_t)(q.row + token) * p.ldy + head_at;
 #pragma unroll 1
-                for (int i = 0; ok && i < D; i += 16) {
+                for (int i = half * HD; ok && i < (half + 1) * HD; i += 16) {
                     uint32_t z[16];
                     tcgen05_ld_32x32b_x16(out + (uint32_t)i, z);
                     tcgen05_wait_ld();
@@ -248,37 +305,40 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             }
         }
     } else if (warp < Sh::kSoft + Sh::kLoad) {
-        // ---- keys and values: a warp has 16 tokens of a tile (with 64 keys a tile, half of their pieces)
-        constexpr int PARTS = 128 / KT, PIECES = D / 32 / PARTS;
-        const int w = warp - Sh::kSoft, step = w / PARTS, part = w % PARTS, g = lane >> 2, t = lane & 3;
+        // ---- keys and values: a warp has every fourth 16 tokens of a tile
+        if constexpr (Sh::kSplit) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+        constexpr int MINE = GROUPS / Sh::kLoad, PIECES = D / 32;
+        const int w = warp - Sh::kSoft, g = lane >> 2, t = lane & 3;
         const uint8_t *codes = c.cache + (size_t)head * 2 * D * (page_mask + 1) + lane * 16;
         const size_t page_bytes = (size_t)c.heads * 2 * D * (page_mask + 1);
         const float *scales = reinterpret_cast<const float *>(c.cache + c.scales_off) + head * 2;
-        // Lane i looks up 16 keys' page and scales for group i of the tile.
-        int id = -1;
+        // Lane i looks up the page of group i of a tile, a tile before its codes and scales are asked for.
+        int id = -1, next_id = -1;
         float key_scale = 0.f, value_scale = 0.f, seen = 0.f;
         auto look = [&](int j) {
             const int token = (tile0 + j) * KT + 16 * (lane & (GROUPS - 1));
-            id = -1;
+            return j < tiles && lane < GROUPS && token < hi ? cache_page(c, seq, token >> c.page_sh) : -1;
+        };
+        uint4 kr[MINE][PIECES], vr[MINE][PIECES];
+        auto fetch = [&](int j) {
+            id = next_id;
+            next_id = look(j + 1);
             key_scale = value_scale = 0.f;
-            if (j < tiles && lane < GROUPS && token < hi) {
-                id = cache_page(c, seq, token >> c.page_sh);
-                if (id >= 0) {
-                    key_scale = ld_dependent(scales + (size_t)id * c.heads * 2);
-                    value_scale = ld_dependent(scales + (size_t)id * c.heads * 2 + 1);
-                }
+            if (id >= 0) {
+                key_scale = ld_dependent(scales + (size_t)id * c.heads * 2);
+                value_scale = ld_dependent(scales + (size_t)id * c.heads * 2 + 1);
+            }
+#pragma unroll
+            for (int n = 0; n < MINE; ++n) {
+                const int step = w + n * Sh::kLoad, at = __shfl_sync(0xffffffffu, id, step), token = (tile0 + j) * KT + 16 * step;
+                const uint8_t *k = codes + (at < 0 ? 0 : at) * page_bytes + (size_t)(token & page_mask) * D, *v = k + (size_t)D * (page_mask + 1);
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) kr[n][i] = at >= 0 ? ld_dependent(reinterpret_cast<const uint4 *>(k + i * 512)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) vr[n][i] = at >= 0 ? ld_dependent(reinterpret_cast<const uint4 *>(v + i * 512)) : make_uint4(0, 0, 0, 0);
             }
         };
-        uint4 kr[PIECES], vr[PIECES];
-        auto fetch = [&](int j) {
-            const int mine = __shfl_sync(0xffffffffu, id, step), token = (tile0 + j) * KT + 16 * step;
-            const uint8_t *k = codes + (mine < 0 ? 0 : mine) * page_bytes + (size_t)(token & page_mask) * D + part * PIECES * 512, *v = k + (size_t)D * (page_mask + 1);
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) kr[i] = mine >= 0 ? ld_dependent(reinterpret_cast<const uint4 *>(k + i * 512)) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < PIECES; ++i) vr[i] = mine >= 0 ? ld_dependent(reinterpret_cast<const uint4 *>(v + i * 512)) : make_uint4(0, 0, 0, 0);
-        };
-        look(0);
+        next_id = look(0);
         fetch(0);
         for (int j = 0; j < tiles; ++j) {
             const int s = j & 1;
@@ -294,44 +354,48 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             }
             uint8_t *kt = smem + Sh::kQ + s * Sh::kKv, *vt = smem + Sh::kQ + (2 + s) * Sh::kKv;
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) {                   // piece 2 p + h: token 8 h + g, columns 64 p + 16 t ..
-                const int piece = part * PIECES + i, row = step * 16 + (piece & 1) * 8 + g;
-                uint32_t h[8];
-                bytes_to_half(kr[i].x, h[0], h[1]);
-                bytes_to_half(kr[i].y, h[2], h[3]);
-                bytes_to_half(kr[i].z, h[4], h[5]);
-                bytes_to_half(kr[i].w, h[6], h[7]);
-                uint8_t *at = kt + (piece >> 1) * (KT * 128) + row * 128;
-                *reinterpret_cast<uint4 *>(at + (((2 * t) ^ g) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-                *reinterpret_cast<uint4 *>(at + (((2 * t + 1) ^ g) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
-            }
+            for (int n = 0; n < MINE; ++n)
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) {               // piece 2 p + h: token 8 h + g, columns 64 p + 16 t ..
+                    const int row = (w + n * Sh::kLoad) * 16 + (i & 1) * 8 + g;
+                    const uint4 u = kr[n][i];
+                    uint32_t h[8];
+                    bytes_to_half(u.x, h[0], h[1]);
+                    bytes_to_half(u.y, h[2], h[3]);
+                    bytes_to_half(u.z, h[4], h[5]);
+                    bytes_to_half(u.w, h[6], h[7]);
+                    uint8_t *at = kt + (i >> 1) * (KT * 128) + row * 128;
+                    *reinterpret_cast<uint4 *>(at + (((2 * t) ^ g) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                    *reinterpret_cast<uint4 *>(at + (((2 * t + 1) ^ g) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+                }
             fence_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&k_full[s]));
             if (j > 1 && !warp_all(mbar_wait(smem_u32(&v_empty[s]), ph))) { ok = false; break; }
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) {                   // bytes 4 e ..: column 8 (4 piece + e) + g, tokens 2t, 2t + 1, 2t + 8, 2t + 9
-                const int piece = part * PIECES + i;
-                uint8_t *atom = vt + (step >> 2) * (D * 128);
+            for (int n = 0; n < MINE; ++n) {
+                const int step = w + n * Sh::kLoad;
+                uint8_t *atom = vt + (step >> 2) * (D * 128) + g * 128 + 4 * t;
+                const uint32_t lo = ((2 * (step & 3)) ^ g) << 4, hi2 = ((2 * (step & 3) + 1) ^ g) << 4;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t h0, h1;
-                    bytes_to_half(e == 0 ? vr[i].x : e == 1 ? vr[i].y : e == 2 ? vr[i].z : vr[i].w, h0, h1);
-                    uint8_t *at = atom + ((4 * piece + e) * 8 + g) * 128 + 4 * t;
-                    *reinterpret_cast<uint32_t *>(at + (((2 * (step & 3)) ^ g) << 4)) = h0;
-                    *reinterpret_cast<uint32_t *>(at + (((2 * (step & 3) + 1) ^ g) << 4)) = h1;
-                }
+                for (int i = 0; i < PIECES; ++i)                 // bytes 4 e ..: column 8 (4 i + e) + g, tokens 2t, 2t + 1, 2t + 8, 2t + 9
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t h0, h1;
+                        bytes_to_half(e == 0 ? vr[n][i].x : e == 1 ? vr[n][i].y : e == 2 ? vr[n][i].z : vr[n][i].w, h0, h1);
+                        *reinterpret_cast<uint32_t *>(atom + (4 * i + e) * 1024 + lo) = h0;
+                        *reinterpret_cast<uint32_t *>(atom + (4 * i + e) * 1024 + hi2) = h1;
+                    }
             }
             fence_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&v_full[s]));
-            if (j + 1 < tiles) {
-                look(j + 1);
-                fetch(j + 1);
-            }
+            if (j + 1 < tiles) fetch(j + 1);
         }
     } else {
-        // ---- MMAs
+        // ---- MMAs (the warp's group keeps its registers down with it)
+        if constexpr (Sh::kSplit) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+        if (warp == Sh::kSoft + Sh::kLoad) {
         const bool lead = elect_one();
         constexpr uint32_t score_desc = 1u << 4 | (uint32_t)(KT >> 3) << 17 | (128u >> 4) << 24, out_desc = 1u << 4 | (uint32_t)(D >> 3) << 17 | (128u >> 4) << 24;
         const uint64_t qd = make_kmajor_sw128_desc(qs), kd = make_kmajor_sw128_desc(ks), vd = make_kmajor_sw128_desc(vs);
@@ -376,6 +440,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                     scores(r, s ^ 1);
                 }
             }
+        }
         }
     }
     if (!ok) atomicCAS(c.status, 0u, (uint32_t)TMAN_ERR_TIMEOUT);
