@@ -1,14 +1,16 @@
 // Attention over the 8-bit cache for many new tokens of a sequence.
 //
 // What bounds it is the exponential function (16 a clock and SM) and the tensor cores, which take as long.  A CTA has up to 256 rows (new tokens x
-// query heads of one key head) in two tiles of 128, and walks over the keys 128 at a time (64 where heads are wide).  Four warps bring keys and values from
-// the cache, make fp16 of the bytes and lay them out as the tensor cores' operands; one thread issues the MMAs (scores: rows x keys; output: rows x
-// columns, both in tensor memory); eight warps a tile of rows, two threads a row, do the softmax.  While one tile's scores are worked on, the
-// other's are multiplied.
-// A thread reads its row of scores twice, for the maximum and for the probabilities, which go back to tensor memory as the A operand of the second
-// product, over the scores.  A key's score is (q . code) x (key page's scale) x scale; probabilities carry the value page's scale, p' = 2^(s + log2 vs - M), so that
-// codes are what they are multiplied with, and the row's sum is that of p' / vs.  M grows, and the output so far is scaled, only when a
-// score is above it by more than 8: then p' is at most 256, and rows seldom change it after their first keys.
+// query heads of one key head) in two tiles of 128 (one where heads are wide), and walks over the keys 64 at a time.  Four warps bring keys and
+// values from the cache, make fp16 of the bytes and lay them out as the tensor cores' operands; one thread issues the MMAs (scores: rows x keys; output:
+// rows x columns, both in tensor memory); four warps a tile of rows, a thread a row, do the softmax.  A tile of rows has two buffers of
+// scores: while one is worked on, the other is filled, so that the softmax warps need not wait for the tensor cores.
+// A score is (q . code) x (key page's scale) x scale; probabilities carry the value page's scale, p' = 2^(s + log2 vs - M), so that codes are what they are
+// multiplied with, and the row's sum is that of p' / vs.  They go back to tensor memory over the scores, as the A operand of the second product.  M
+// is the maximum so far and raised, and the output so far scaled, only when a score is above it by more than 10: p' is at most 2^10, rows seldom
+// raise it after their first keys, and one pass over the scores is enough; one that finds such a score is made again behind the raise.
+// 2 x 2048 new tokens over 4096, 32 heads of 128: scores twice from tensor memory and a wait for both products in turn 274 us; with one pass, keys 128 at
+// a time, 197; two threads a row instead of one made no difference.
 #pragma once
 
 #include "attend.cuh"
@@ -17,14 +19,12 @@ namespace tman {
 namespace {
 
 template <int D> struct PromptShape {
-    static constexpr int kKeys = D <= 128 ? 128 : 64, kTiles = D <= 192 ? 2 : 1, kSoft = 8 * kTiles, kLoad = 4;
-    static constexpr int kThreads = 32 * (kSoft + kLoad + 4), kRows = 128 * kTiles;
-    static constexpr int kQ = kRows * D * 2, kKv = kKeys * D * 2, kSmem = kQ + 4 * kKv + 1024;
-    // Registers: with two tiles of rows the threads that work take what the fourth of a warpgroup that issues leaves (24 warps of 80 at launch).
-    static constexpr bool kSplit = kTiles == 2;
-    static_assert(!kSplit || (kThreads == 768 && 128 * (4 * 88 + 96 + 32) <= 768 * 80), "what the block is launched with");
-    static constexpr int kScore = 0, kOut = kTiles * kKeys;      // columns of tensor memory
-    static_assert(kOut + kTiles * D <= 512 && kSmem <= 227 * 1024, "it fits");
+    static constexpr int kKeys = 64, kTiles = D <= 128 ? 2 : 1, kSoft = 4 * kTiles, kLoad = 4, kStages = D <= 128 ? 4 : D <= 192 ? 3 : 2;
+    static constexpr int kThreads = 32 * (kSoft + kLoad + kTiles), kRows = 128 * kTiles;
+    static constexpr int kQ = kRows * D * 2, kKv = kKeys * D * 2, kSmem = kQ + 2 * kStages * kKv + 1024;
+    static constexpr int kScore = 0, kOut = 2 * kTiles * kKeys;  // columns of tensor memory
+    static constexpr int kConsts = 8;                            // tiles whose pages' scales are kept: the loads are up to kStages + 1 ahead of the softmax
+    static_assert(kOut + kTiles * D <= 512 && kSmem <= 227 * 1024 && kStages + 2 <= kConsts, "it fits");
 };
 
 struct PromptParams {
@@ -37,51 +37,38 @@ struct PromptParams {
 
 constexpr float kPromptSlack = 10.f;     // a score above the maximum so far by this much raises it
 
-// Pairs of numbers in one instruction.
-__device__ __forceinline__ float2 two(float v) { return make_float2(v, v); }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
-    return *reinterpret_cast<float2 *>(&r);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
-    return *reinterpret_cast<float2 *>(&r);
-}
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptParams p)
 {
     using Sh = PromptShape<D>;
-    constexpr int KT = Sh::kKeys, RT = Sh::kTiles, GROUPS = KT / 16;
+    constexpr int KT = Sh::kKeys, RT = Sh::kTiles, GROUPS = KT / 16, NS = Sh::kStages;
     extern __shared__ __align__(1024) uint8_t prompt_smem[];
-    __shared__ __align__(8) uint64_t q_bar, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2], pair_bar[4 * RT];
+    __shared__ __align__(8) uint64_t q_bar, k_full[NS], k_empty[NS], v_full[NS], v_empty[NS], s_full[RT][2], p_full[RT][2], o_full[RT];
     __shared__ uint32_t tmem_slot;
-    __shared__ float4 page_consts[4][GROUPS];                    // of 16 keys: scale of the keys, log2 of the values' scale and its reciprocal
-    __shared__ float row_of[Sh::kSoft][32];                      // what the two threads of a row tell each other
-    __shared__ uint32_t votes[Sh::kSoft];
+    __shared__ float4 page_consts[Sh::kConsts][GROUPS];          // of 16 keys: scale of the keys, log2 of the values' scale and its reciprocal
     __shared__ int found[2], sums[Sh::kThreads / 32 + 1];
     const CacheSeqs &c = p.c;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, page_mask = (1 << c.page_sh) - 1;
     const uint32_t base = (smem_u32(prompt_smem) + 1023u) & ~1023u;
     uint8_t *smem = prompt_smem + (base - smem_u32(prompt_smem));
-    const uint32_t qs = base, ks = base + Sh::kQ, vs = ks + 2 * Sh::kKv;
+    const uint32_t qs = base, ks = base + Sh::kQ, vs = ks + NS * Sh::kKv;
     if (tid == 0) {
-        mbar_init(smem_u32(&q_bar), 8 * RT);
-        for (int i = 0; i < 2; ++i) {
+        mbar_init(smem_u32(&q_bar), 4 * RT);
+        for (int i = 0; i < NS; ++i) {
             mbar_init(smem_u32(&k_full[i]), Sh::kLoad);
             mbar_init(smem_u32(&v_full[i]), Sh::kLoad);
-            mbar_init(smem_u32(&k_empty[i]), 1);
-            mbar_init(smem_u32(&v_empty[i]), 1);
-            mbar_init(smem_u32(&s_full[i]), 1);
-            mbar_init(smem_u32(&p_full[i]), 8);
-            mbar_init(smem_u32(&o_full[i]), 1);
+            mbar_init(smem_u32(&k_empty[i]), RT);
+            mbar_init(smem_u32(&v_empty[i]), RT);
         }
-        for (int i = 0; i < 4 * RT; ++i) mbar_init(smem_u32(&pair_bar[i]), 2);
+        for (int r = 0; r < RT; ++r) {
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(smem_u32(&s_full[r][i]), 1);
+                mbar_init(smem_u32(&p_full[r][i]), 4);
+            }
+            mbar_init(smem_u32(&o_full[r]), 1);
+        }
         found[0] = -1;
         fence_barrier_init();
     }
@@ -125,7 +112,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
     const int row0 = found[1] * Sh::kRows, rows = min(q.rows * p.group - row0, Sh::kRows), pos0 = q.len - q.rows;
     const int first = pos0 + row0 / p.group, last = pos0 + (row0 + rows - 1) / p.group;      // positions of the first and the last row
     const int hi = max(last + 1, 0), lo = p.window > 0 ? max(first - p.window + 1, 0) : 0;
-    const int tile0 = lo / KT, tiles = max((hi + KT - 1) / KT - tile0, 1), active = rows > 128 ? 2 : 1;       // tiles of keys, of rows
+    const int tile0 = lo / KT, tiles = max((hi + KT - 1) / KT - tile0, 1), active = RT == 2 && rows > 128 ? 2 : 1;       // tiles of keys, of rows
     if (warp == Sh::kSoft + Sh::kLoad) {
         tcgen05_alloc(smem_u32(&tmem_slot), 512);
         tcgen05_relinquish();
@@ -139,16 +126,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
 
     if (warp < Sh::kSoft) {
         // ---- softmax: a thread has a row
-        if constexpr (Sh::kSplit) asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
-        const int r = warp >> 3, half = (warp >> 2) & 1, local = (warp & 3) * 32 + lane, row = r * 128 + local, other = warp ^ 4;
-        uint32_t turn = 0;
-        auto meet = [&] {                                        // the two warps of the same rows
-            const uint32_t bar = smem_u32(&pair_bar[r * 4 + (warp & 3)]);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar);
-            ok = warp_all(mbar_wait(bar, turn)) && ok;
-            turn ^= 1u;
-        };
+        const int r = warp >> 2, local = (warp & 3) * 32 + lane, row = r * 128 + local;
         if (r >= active) {
             if (lane == 0) mbar_arrive(smem_u32(&q_bar));
         } else {
@@ -167,7 +145,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                 f = top == 0 || top >= i8_infinity<T>() ? 1.f : __uint_as_float((uint32_t)(127 + min(141 - (int)(top >> 7), 100)) << 23);
             }
 #pragma unroll 4
-            for (int i = half * (D / 16); i < (half + 1) * (D / 16); ++i) {
+            for (int i = 0; i < D / 8; ++i) {
                 uint4 v = make_uint4(0, 0, 0, 0);
                 if (real) v = ld_dependent(reinterpret_cast<const uint4 *>(src) + i);
                 if constexpr (!std::is_same<T, __half>::value) {
@@ -184,46 +162,43 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             const float rf = p.scale * kLog2e / f;
             const int limit = pos0 + token, low = p.window > 0 ? limit - p.window + 1 : INT_MIN;
             const int least_limit = __reduce_min_sync(0xffffffffu, limit), most_low = __reduce_max_sync(0xffffffffu, low);
-            const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16), score = at + Sh::kScore + r * KT, out = at + Sh::kOut + r * D;
-            constexpr int HC = KT / 2, HD = D / 2;               // columns of scores and of the output that a thread has
+            const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16), out = at + Sh::kOut + r * D;
             float M = -INFINITY, l = 0.f;
             for (int j = 0; j < tiles; ++j) {
-                const int k0 = (tile0 + j) * KT + half * HC;
-                const bool plain = k0 + HC - 1 <= least_limit && k0 >= most_low;
+                const int k0 = (tile0 + j) * KT;
+                const bool plain = k0 + KT - 1 <= least_limit && k0 >= most_low;
                 const int upto = limit - k0, from = low == INT_MIN ? INT_MIN : low - k0;      // columns that this row sees
-                const float4 *consts = page_consts[j & 3] + half * (GROUPS / 2);
-                ok = warp_all(mbar_wait(smem_u32(&s_full[r]), j & 1)) && ok;
+                const float4 *consts = page_consts[j & (Sh::kConsts - 1)];
+                const uint32_t score = at + Sh::kScore + (r * 2 + (j & 1)) * KT;
+                ok = warp_all(mbar_wait(smem_u32(&s_full[r][j & 1]), (j >> 1) & 1));
                 if (!ok) break;
                 tcgen05_fence_after();
-                uint32_t h[HC / 2];
+                uint32_t h[KT / 2];
                 float sum;
 #pragma unroll 1
                 for (bool raise = j == 0;; raise = true) {
                     if (raise) {                                 // the maximum first
                         float mx = -INFINITY;
 #pragma unroll 1
-                        for (int i = 0; i < HC; i += 32) {
-                            uint32_t z[32];
-                            tcgen05_ld_32x32b_x32(score + (uint32_t)(half * HC + i), z);
-                            const float4 c0 = consts[i >> 4], c1 = consts[(i >> 4) + 1];
-                            const float f0 = c0.x * rf, f1 = c1.x * rf;
+                        for (int i = 0; i < GROUPS; ++i) {
+                            uint32_t z[16];
+                            tcgen05_ld_32x32b_x16(score + 16u * i, z);
+                            const float4 cc = consts[i];
+                            const float f = cc.x * rf;
                             tcgen05_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                const float x = fmaf(__uint_as_float(z[e]), e < 16 ? f0 : f1, e < 16 ? c0.y : c1.y);
-                                mx = fmaxf(mx, i + e <= upto && i + e >= from ? x : -INFINITY);
-                            }
+                            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, 16 * i + e <= upto && 16 * i + e >= from ? fmaf(__uint_as_float(z[e]), f, cc.y) : -INFINITY);
                         }
-                        row_of[warp][lane] = mx;
-                        meet();
-                        mx = fmaxf(mx, row_of[other][lane]);
                         const float next = mx > M + kPromptSlack || M == -INFINITY ? fmaxf(mx, M) : M;
                         const float g = next == M ? 1.f : exp2_fast(M - next);
                         M = next;
                         l *= g;
-                        if (j > 0) {
+                        if (j > 0) {                             // (behind the product of the tile before)
+                            ok = warp_all(mbar_wait(smem_u32(&o_full[r]), (j - 1) & 1));
+                            if (!ok) break;
+                            tcgen05_fence_after();
 #pragma unroll 1
-                            for (int i = half * HD; i < (half + 1) * HD; i += 16) {
+                            for (int i = 0; i < D; i += 16) {
                                 uint32_t z[16];
                                 tcgen05_ld_32x32b_x16(out + (uint32_t)i, z);
                                 tcgen05_wait_ld();
@@ -237,19 +212,18 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                     float mx = -INFINITY;
                     sum = 0.f;
                     uint32_t z[2][32];
-                    tcgen05_ld_32x32b_x32(score + (uint32_t)(half * HC), z[0]);
+                    tcgen05_ld_32x32b_x32(score, z[0]);
+                    tcgen05_ld_32x32b_x32(score + 32u, z[1]);
 #pragma unroll
-                    for (int i = 0; i < HC / 32; ++i) {
-                        uint32_t (&y)[32] = z[i & 1];
-                        float4 c0, c1;                           // (read here and not earlier: all of them would take 32 registers)
+                    for (int i = 0; i < 2; ++i) {
+                        float4 c0, c1;
                         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(c0.x), "=f"(c0.y), "=f"(c0.z), "=f"(c0.w) : "r"(smem_u32(consts + 2 * i)) : "memory");
                         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(c1.x), "=f"(c1.y), "=f"(c1.z), "=f"(c1.w) : "r"(smem_u32(consts + 2 * i + 1)) : "memory");
-                        const float2 f0 = two(c0.x * rf), f1 = two(c1.x * rf), b0 = two(c0.y - Mu), b1 = two(c1.y - Mu);
-                        tcgen05_wait_ld();
-                        if (i + 1 < HC / 32) tcgen05_ld_32x32b_x32(score + (uint32_t)(half * HC + 32 * (i + 1)), z[(i + 1) & 1]);
+                        const float f0 = c0.x * rf, f1 = c1.x * rf, b0 = c0.y - Mu, b1 = c1.y - Mu;
+                        if (i == 0) tcgen05_wait_ld();
                         float x[32];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[e] = fmaf(__uint_as_float(y[e]), e < 16 ? f0.x : f1.x, e < 16 ? b0.x : b1.x);
+                        for (int e = 0; e < 32; ++e) x[e] = fmaf(__uint_as_float(z[i][e]), e < 16 ? f0 : f1, e < 16 ? b0 : b1);
                         if (!plain) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) x[e] = 32 * i + e <= upto && 32 * i + e >= from ? x[e] : -INFINITY;
@@ -263,34 +237,29 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                             h[16 * i + e / 2] = f4_from_float2<__half>(u, v);
                         }
                         sum = fmaf(s0 + s1, c0.z, fmaf(s2 + s3, c1.z, sum));
-                        asm volatile("" : "+f"(sum), "+f"(mx));          // (added up here: put off, the 32 values would stay in registers)
+                        asm volatile("" : "+f"(sum), "+f"(mx));          // (added up here: put off, the values would stay in registers)
                     }
-                    // Both threads of a row raise it, or none (once: what the maximum was taken of is rounded apart from this by less than a unit).  Behind
-                    // the meeting all scores have been read.
-                    const bool above = __any_sync(0xffffffffu, mx > kPromptSlack || (M == -INFINITY && mx != -INFINITY));
-                    if (lane == 0) votes[warp] = above;
-                    meet();
-                    const bool again = !raise && (above || *reinterpret_cast<volatile uint32_t *>(&votes[other]) != 0);
-                    if (!again || !ok) break;
+                    // (once: what the maximum was taken of is rounded apart from this by less than a unit)
+                    if (raise || !__any_sync(0xffffffffu, mx > kPromptSlack || (M == -INFINITY && mx != -INFINITY))) break;
                 }
+                if (!ok) break;
                 l += sum;
 #pragma unroll
-                for (int i = 0; i < HC / 2; i += 16) tcgen05_st_32x32b_x16(score + (uint32_t)(half * (HC / 2) + i), *reinterpret_cast<uint32_t(*)[16]>(h + i));
+                for (int i = 0; i < KT / 2; i += 16) tcgen05_st_32x32b_x16(score + (uint32_t)i, *reinterpret_cast<uint32_t(*)[16]>(h + i));
                 tcgen05_wait_st();
                 tcgen05_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&p_full[r]));
+                if (lane == 0) mbar_arrive(smem_u32(&p_full[r][j & 1]));
             }
             if (ok) {
-                ok = warp_all(mbar_wait(smem_u32(&o_full[r]), 0));
+                // (the product of the tile before the last may still run: its turn of the barrier comes first)
+                if (tiles > 1) ok = warp_all(mbar_wait(smem_u32(&o_full[r]), tiles & 1));
+                ok = ok && warp_all(mbar_wait(smem_u32(&o_full[r]), (tiles - 1) & 1));
                 tcgen05_fence_after();
-                row_of[warp][lane] = l;
-                meet();
-                l += row_of[other][lane];
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 T *dst = static_cast<T *>(p.y) + (size_t)(q.row + token) * p.ldy + head_at;
 #pragma unroll 1
-                for (int i = half * HD; ok && i < (half + 1) * HD; i += 16) {
+                for (int i = 0; ok && i < D; i += 16) {
                     uint32_t z[16];
                     tcgen05_ld_32x32b_x16(out + (uint32_t)i, z);
                     tcgen05_wait_ld();
@@ -306,7 +275,6 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
         }
     } else if (warp < Sh::kSoft + Sh::kLoad) {
         // ---- keys and values: a warp has every fourth 16 tokens of a tile
-        if constexpr (Sh::kSplit) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
         constexpr int MINE = GROUPS / Sh::kLoad, PIECES = D / 32;
         const int w = warp - Sh::kSoft, g = lane >> 2, t = lane & 3;
         const uint8_t *codes = c.cache + (size_t)head * 2 * D * (page_mask + 1) + lane * 16;
@@ -340,19 +308,19 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
         };
         next_id = look(0);
         fetch(0);
+        int s = 0;
+        uint32_t ph = 1;                                         // (the first turn of the rings does not wait)
         for (int j = 0; j < tiles; ++j) {
-            const int s = j & 1;
-            const uint32_t ph = ((uint32_t)(j >> 1) & 1u) ^ 1u;
-            if (j > 1 && !warp_all(mbar_wait(smem_u32(&k_empty[s]), ph))) { ok = false; break; }
+            if (j >= NS && !warp_all(mbar_wait(smem_u32(&k_empty[s]), ph))) { ok = false; break; }
             // Pages of zero values have no say in how large the others count, so they pass for what is around them.
             float most = lane < GROUPS && id >= 0 && value_scale == value_scale ? value_scale : 0.f;
             most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
             if (most > 0.f) seen = most;
             if (w == 0 && lane < GROUPS) {
                 const float u = value_scale == 0.f ? (seen > 0.f ? seen : 1.f) : value_scale, v = u < 0x1p-120f ? 0x1p-120f : u;
-                page_consts[j & 3][lane] = id < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f) : make_float4(key_scale, __log2f(v), 1.f / v, 0.f);
+                page_consts[j & (Sh::kConsts - 1)][lane] = id < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f) : make_float4(key_scale, __log2f(v), 1.f / v, 0.f);
             }
-            uint8_t *kt = smem + Sh::kQ + s * Sh::kKv, *vt = smem + Sh::kQ + (2 + s) * Sh::kKv;
+            uint8_t *kt = smem + Sh::kQ + s * Sh::kKv, *vt = smem + Sh::kQ + (NS + s) * Sh::kKv;
 #pragma unroll
             for (int n = 0; n < MINE; ++n)
 #pragma unroll
@@ -371,7 +339,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             fence_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&k_full[s]));
-            if (j > 1 && !warp_all(mbar_wait(smem_u32(&v_empty[s]), ph))) { ok = false; break; }
+            if (j >= NS && !warp_all(mbar_wait(smem_u32(&v_empty[s]), ph))) { ok = false; break; }
 #pragma unroll
             for (int n = 0; n < MINE; ++n) {
                 const int step = w + n * Sh::kLoad;
@@ -391,56 +359,58 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&v_full[s]));
             if (j + 1 < tiles) fetch(j + 1);
+            if (++s == NS) { s = 0; ph ^= 1u; }
         }
     } else {
-        // ---- MMAs (the warp's group keeps its registers down with it)
-        if constexpr (Sh::kSplit) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-        if (warp == Sh::kSoft + Sh::kLoad) {
-        const bool lead = elect_one();
+        // ---- MMAs, a warp for each tile of rows (one for both spent its time between waits: 200 us).  Scores of tile j go to buffer j & 1, behind the
+        // product that read the probabilities of tile j - 2 there: the tensor cores work in the order of issue.
+        // (Addresses and descriptors are worked out by the whole warp, outside of what one lane issues, so that they sit in uniform registers.)
+        const int r = warp - Sh::kSoft - Sh::kLoad;
+        const bool lead = elect_one(), twice = active < RT;      // (the word of the tile of rows that is not there)
         constexpr uint32_t score_desc = 1u << 4 | (uint32_t)(KT >> 3) << 17 | (128u >> 4) << 24, out_desc = 1u << 4 | (uint32_t)(D >> 3) << 17 | (128u >> 4) << 24;
-        const uint64_t qd = make_kmajor_sw128_desc(qs), kd = make_kmajor_sw128_desc(ks), vd = make_kmajor_sw128_desc(vs);
-        auto scores = [&](int r, int s) {
+        const uint64_t qd = make_kmajor_sw128_desc(qs) + (uint32_t)r * (D / 64) * (16384 / 16), kd = make_kmajor_sw128_desc(ks), vd = make_kmajor_sw128_desc(vs);
+        const uint32_t score = tmem + Sh::kScore + r * 2 * KT, out = tmem + Sh::kOut + r * D;
+        const uint32_t sf = smem_u32(&s_full[r][0]), pf = smem_u32(&p_full[r][0]), of = smem_u32(&o_full[r]);
+        int sk = 0, sv = 0;                                      // stages of the next tile of keys, of values
+        uint32_t pk = 0, pv = 0;
+        auto scores = [&](int j) {                               // keys of tile j
+            ok = warp_all(mbar_wait(smem_u32(&k_full[sk]), pk));
+            if (!ok) return;
+            tcgen05_fence_after();
+            const uint64_t kj = kd + (uint32_t)sk * (Sh::kKv / 16);
+            const uint32_t to = score + (j & 1) * KT, full = sf + (j & 1) * 8, empty = smem_u32(&k_empty[sk]);
             if (lead) {
 #pragma unroll
                 for (uint32_t i = 0; i < D / 16; ++i)
-                    tcgen05_mma_f16(tmem + Sh::kScore + r * KT, qd + ((r * (D / 64) + (i >> 2)) * 16384 + (i & 3) * 32) / 16, kd + (s * Sh::kKv + (i >> 2) * (KT * 128) + (i & 3) * 32) / 16,
-                                    score_desc, i != 0);
-                tcgen05_commit(smem_u32(&s_full[r]));
-                if (r == active - 1) tcgen05_commit(smem_u32(&k_empty[s]));
+                    tcgen05_mma_f16(to, qd + ((i >> 2) * 16384 + (i & 3) * 32) / 16, kj + ((i >> 2) * (KT * 128) + (i & 3) * 32) / 16, score_desc, i != 0);
+                tcgen05_commit(full);
+                tcgen05_commit(empty);
+                if (twice) tcgen05_commit(empty);
             }
             __syncwarp();
+            if (++sk == NS) { sk = 0; pk ^= 1u; }
         };
-        ok = warp_all(mbar_wait(smem_u32(&q_bar), 0));
-        ok = ok && warp_all(mbar_wait(smem_u32(&k_full[0]), 0));
-        tcgen05_fence_after();
-        if (ok)
-            for (int r = 0; r < active; ++r) scores(r, 0);
-        for (int j = 0; ok && j < tiles; ++j) {
-            const int s = j & 1;
-            for (int r = 0; r < active; ++r) {
-                if (r == 0) ok = warp_all(mbar_wait(smem_u32(&v_full[s]), (j >> 1) & 1));
-                ok = ok && warp_all(mbar_wait(smem_u32(&p_full[r]), j & 1));
+        if (r < active) {
+            ok = warp_all(mbar_wait(smem_u32(&q_bar), 0));
+            tcgen05_fence_after();
+            for (int j = 0; ok && j < 2 && j < tiles; ++j) scores(j);
+            for (int j = 0; ok && j < tiles; ++j) {
+                ok = warp_all(mbar_wait(smem_u32(&v_full[sv]), pv) && mbar_wait(pf + (j & 1) * 8, (j >> 1) & 1));
                 if (!ok) break;
                 tcgen05_fence_after();
+                const uint64_t vj = vd + (uint32_t)sv * (Sh::kKv / 16);
+                const uint32_t from = score + (j & 1) * KT, empty = smem_u32(&v_empty[sv]);
                 if (lead) {
 #pragma unroll
-                    for (uint32_t i = 0; i < KT / 16; ++i)
-                        tcgen05_mma_f16_ts(tmem + Sh::kOut + r * D, tmem + Sh::kScore + r * KT + i * 8, vd + (s * Sh::kKv + (i >> 2) * (D * 128) + (i & 3) * 32) / 16, out_desc,
-                                           (j | (int)i) != 0);
-                    if (r == active - 1) tcgen05_commit(smem_u32(&v_empty[s]));
-                    if (j + 1 == tiles) tcgen05_commit(smem_u32(&o_full[r]));
+                    for (uint32_t i = 0; i < KT / 16; ++i) tcgen05_mma_f16_ts(out, from + i * 8, vj + i * 2, out_desc, i == 0 ? (uint32_t)j : 1u);
+                    tcgen05_commit(empty);
+                    if (twice) tcgen05_commit(empty);
+                    tcgen05_commit(of);
                 }
                 __syncwarp();
-                if (j + 1 < tiles) {
-                    if (r == 0) {
-                        ok = warp_all(mbar_wait(smem_u32(&k_full[s ^ 1]), ((j + 1) >> 1) & 1));
-                        if (!ok) break;
-                        tcgen05_fence_after();
-                    }
-                    scores(r, s ^ 1);
-                }
+                if (j + 2 < tiles) scores(j + 2);
+                if (++sv == NS) { sv = 0; pv ^= 1u; }
             }
-        }
         }
     }
     if (!ok) atomicCAS(c.status, 0u, (uint32_t)TMAN_ERR_TIMEOUT);
