@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
     using Sh = PromptShape<D>;
     constexpr int KT = Sh::kKeys, RT = Sh::kTiles, GROUPS = KT / 16, NS = Sh::kStages;
     extern __shared__ __align__(1024) uint8_t prompt_smem[];
-    __shared__ __align__(8) uint64_t q_bar, k_full[NS], k_empty[NS], v_full[NS], v_empty[NS], s_full[RT][2], p_full[RT][2], o_full[RT];
+    __shared__ __align__(8) uint64_t q_bar, k_full[NS], k_empty[NS], v_full[NS], v_empty[NS], s_full[RT][2], p_full[RT][2], o_full[RT], all_bar[RT];
     __shared__ uint32_t tmem_slot;
     __shared__ float4 page_consts[Sh::kConsts][GROUPS];          // of 16 keys: scale of the keys, log2 of the values' scale and its reciprocal
     __shared__ int found[2], sums[Sh::kThreads / 32 + 1];
@@ -68,6 +68,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                 mbar_init(smem_u32(&p_full[r][i]), 4);
             }
             mbar_init(smem_u32(&o_full[r]), 1);
+            mbar_init(smem_u32(&all_bar[r]), 1);
         }
         found[0] = -1;
         fence_barrier_init();
@@ -186,6 +187,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                             const float4 cc = consts[i];
                             const float f = cc.x * rf;
                             tcgen05_wait_ld();
+                            tcgen05_loaded(z);
 #pragma unroll
                             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, 16 * i + e <= upto && 16 * i + e >= from ? fmaf(__uint_as_float(z[e]), f, cc.y) : -INFINITY);
                         }
@@ -202,6 +204,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                                 uint32_t z[16];
                                 tcgen05_ld_32x32b_x16(out + (uint32_t)i, z);
                                 tcgen05_wait_ld();
+                                tcgen05_loaded(z);
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(__uint_as_float(z[e]) * g);
                                 tcgen05_st_32x32b_x16(out + (uint32_t)i, z);
@@ -221,6 +224,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(c1.x), "=f"(c1.y), "=f"(c1.z), "=f"(c1.w) : "r"(smem_u32(consts + 2 * i + 1)) : "memory");
                         const float f0 = c0.x * rf, f1 = c1.x * rf, b0 = c0.y - Mu, b1 = c1.y - Mu;
                         if (i == 0) tcgen05_wait_ld();
+                        tcgen05_loaded(z[i]);
                         float x[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) x[e] = fmaf(__uint_as_float(z[i][e]), e < 16 ? f0 : f1, e < 16 ? b0 : b1);
@@ -252,9 +256,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                 if (lane == 0) mbar_arrive(smem_u32(&p_full[r][j & 1]));
             }
             if (ok) {
-                // (the product of the tile before the last may still run: its turn of the barrier comes first)
-                if (tiles > 1) ok = warp_all(mbar_wait(smem_u32(&o_full[r]), tiles & 1));
-                ok = ok && warp_all(mbar_wait(smem_u32(&o_full[r]), (tiles - 1) & 1));
+                ok = warp_all(mbar_wait(smem_u32(&all_bar[r]), 0));
                 tcgen05_fence_after();
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 T *dst = static_cast<T *>(p.y) + (size_t)(q.row + token) * p.ldy + head_at;
@@ -263,6 +265,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                     uint32_t z[16];
                     tcgen05_ld_32x32b_x16(out + (uint32_t)i, z);
                     tcgen05_wait_ld();
+                    tcgen05_loaded(z);
                     if (real) {
                         uint32_t h[8];
 #pragma unroll
@@ -406,6 +409,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                     tcgen05_commit(empty);
                     if (twice) tcgen05_commit(empty);
                     tcgen05_commit(of);
+                    if (j + 1 == tiles) tcgen05_commit(smem_u32(&all_bar[r]));
                 }
                 __syncwarp();
                 if (j + 2 < tiles) scores(j + 2);

@@ -18,6 +18,21 @@ tman_status launch_i8_gemm(const int8_t *w, int ldw, const float *w_scale, const
 size_t      i8_workspace_bytes(int op, int M, int K);
 
 #ifdef __CUDACC__
+// What tcgen05.ld brings is there behind tcgen05.wait::ld only.  The compiler, which does not know, would be free to use it before: this says that it
+// changes here.
+__device__ __forceinline__ void tcgen05_loaded(uint32_t (&r)[16])
+{
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), 
+                      "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+__device__ __forceinline__ void tcgen05_loaded(uint32_t (&r)[32])
+{
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), 
+                      "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), 
+                      "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), 
+                      "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
+}
+
 // Magnitudes of two 16-bit floating-point numbers as integers, which are ordered like them; an infinity is above every number, a NaN above that.
 __device__ __forceinline__ uint32_t i8_magnitudes(uint32_t pair) { return pair & 0x7FFF7FFFu; }
 __device__ __forceinline__ uint32_t i8_larger(uint32_t a, uint32_t b) { return __vmaxu2(a, b); }

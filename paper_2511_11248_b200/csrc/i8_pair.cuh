@@ -193,6 +193,7 @@ __global__ void __launch_bounds__(kI8PairThreads) i8_pair_kernel(const __grid_co
                 uint32_t r[16];
                 tcgen05_ld_32x32b_x16(acc + (uint32_t)t, r);
                 tcgen05_wait_ld();
+                tcgen05_loaded(r);
                 if (whole && t + 16 <= end) store16(std::true_type(), t, r);
                 else store16(std::false_type(), t, r);
             }
@@ -221,6 +222,7 @@ __global__ void __launch_bounds__(kI8PairThreads) i8_pair_kernel(const __grid_co
                 const uint32_t cta = (uint32_t)to * 2u + rank, bar = mapa_u32(smem_u32(&sums_bar), cta),
                                dst = mapa_u32(ring, cta) + (uint32_t)((((int)share * own + t - to * own) * 128 + quad * 32 + lane) * 4);
                 tcgen05_wait_ld();
+                tcgen05_loaded(r);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) store_cluster(dst + 512u * e, __uint_as_float(r[e]), bar);
             }
