@@ -4,11 +4,52 @@
 namespace tman {
 namespace {
 
-constexpr int kCacheThreads = 128;
+constexpr int kCacheThreads = 256;
+
+// Which of the things that the sequences have in turn, `of(s)` of them each, is number `index`: found[0] is its sequence (-1: there are fewer),
+// found[1] its place in it.  All threads.
+template <typename Of> __device__ __forceinline__ void find_in_sequences(int S, int index, int (&found)[2], int (&warps)[kCacheThreads / 32], const Of &of)
+{
+    const int tid = threadIdx.x, lane = tid & 31, per = (S + kCacheThreads - 1) / kCacheThreads, s0 = min(tid * per, S), s1 = min(s0 + per, S);
+    int mine = 0;
+    for (int s = s0; s < s1; ++s) mine += of(s);
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 31) warps[tid >> 5] = upto;
+    if (tid == 0) found[0] = -1;
+    __syncthreads();
+    for (int w = 0; w < (tid >> 5); ++w) upto += warps[w];
+    int before = upto - mine;
+    if (index >= before && index < upto) {
+        int s = s0;
+        if (per > 1)
+            for (int n; index >= before + (n = of(s)); ++s) before += n;
+        found[0] = s;
+        found[1] = index - before;
+    }
+    __syncthreads();
+}
+// Steps of 2^sh tokens that a sequence's rows lie in; none of one whose rows are more than its tokens (the status word says so).
+__device__ __forceinline__ int steps_of(const CacheSeqs &c, int s, int sh)
+{
+    const CacheSeq q = cache_seq(c, s);
+    if (q.rows > q.len) {
+        atomicCAS(c.status, 0u, (uint32_t)TMAN_ERR_INDEX);
+        return 0;
+    }
+    return q.rows == 0 ? 0 : ((q.len - 1) >> sh) - ((q.len - q.rows) >> sh) + 1;
+}
 
 // ---- append: a CTA has one page that changes, one head, keys or values ----------------------------------------------------------
 // scale = max(old scale, max|new| / 127); codes that are there already become round(code x old / scale), new ones round(x / scale).  The page's
 // codes are put together in shared memory and leave as they came, in 16-byte pieces.
+// Bound by latency for few tokens (what sequence, what page, what maximum, one behind the other) and by reading the rows for many: a thread takes
+// eight columns of four tokens whose codes are neighbours in the cache (cache_i8.cuh), so that values need no byte stores, and keeps the first it takes
+// in registers between the maximum and the codes (pages of more than 8192 values are read twice).
 struct AppendParams {
     CacheSeqs c;
     const void *k, *v;
@@ -25,42 +66,7 @@ __global__ void __launch_bounds__(kCacheThreads) append_kernel(const __grid_cons
     const int tid = threadIdx.x, lane = tid & 31, head = blockIdx.y, values = blockIdx.z, page = 1 << c.page_sh, width = c.width;
     grid_wait();
     grid_launch_next();
-    // pages that change, counted over the sequences: which one is this CTA's
-    {
-        const int per = (c.S + kCacheThreads - 1) / kCacheThreads, s0 = min(tid * per, c.S), s1 = min(s0 + per, c.S);
-        auto pages_of = [&](int s) {
-            const CacheSeq q = cache_seq(c, s);
-            if (q.rows > q.len) {
-                atomicCAS(c.status, 0u, (uint32_t)TMAN_ERR_INDEX);
-                return 0;
-            }
-            return q.rows == 0 ? 0 : ((q.len - 1) >> c.page_sh) - ((q.len - q.rows) >> c.page_sh) + 1;
-        };
-        int mine = 0;
-        for (int s = s0; s < s1; ++s) mine += pages_of(s);
-        int upto = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += o;
-        }
-        if (lane == 31) warps[tid >> 5] = upto;
-        if (tid == 0) found[0] = -1;
-        __syncthreads();
-        for (int w = 0; w < (tid >> 5); ++w) upto += warps[w];
-        int before = upto - mine;
-        if ((int)blockIdx.x >= before && (int)blockIdx.x < upto)
-            for (int s = s0; s < s1; ++s) {
-                const int n = pages_of(s);
-                if ((int)blockIdx.x < before + n) {
-                    found[0] = s;
-                    found[1] = (int)blockIdx.x - before;
-                    break;
-                }
-                before += n;
-            }
-        __syncthreads();
-    }
+    find_in_sequences(c.S, blockIdx.x, found, warps, [&](int s) { return steps_of(c, s, c.page_sh); });
     const int s = found[0];
     if (s < 0) return;
     const CacheSeq q = cache_seq(c, s);
@@ -72,14 +78,35 @@ __global__ void __launch_bounds__(kCacheThreads) append_kernel(const __grid_cons
     uint8_t *codes = c.cache + (((size_t)id * c.heads + head) * 2 + values) * page * width;
     float *scale_at = reinterpret_cast<float *>(c.cache + c.scales_off) + ((size_t)id * c.heads + head) * 2 + values;
     const int end = (r1 + 15) >> 4, words = end * width;         // tiles, and their 16-byte pieces
+    const int quads = (end - (r0 >> 4)) * 4 * pieces;            // quadruples of rows in tiles with new ones x pieces of eight columns
+    // quadruple i: tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of a tile
+    auto rows_of = [&](int i, int &row, int &piece) {
+        piece = i % pieces;
+        const int n = i / pieces;
+        row = ((r0 >> 4) + (n >> 2)) * 16 + (n & 3) * 2;
+    };
+    auto row_in = [&](int row, int e) { const int r = row + (e >> 1) * 8 + (e & 1); return r >= r0 && r < r1; };
+    auto load = [&](int row, int piece, int e) {
+        return row_in(row, e) ? ld_dependent(reinterpret_cast<const uint4 *>(x + (ptrdiff_t)(row + (e >> 1) * 8 + (e & 1)) * ld) + piece) : make_uint4(0, 0, 0, 0);
+    };
+    uint4 held[4];
+    int row = 0, piece = 0;
+    rows_of(tid, row, piece);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) held[e] = tid < quads ? load(row, piece, e) : make_uint4(0, 0, 0, 0);
     uint4 *st = reinterpret_cast<uint4 *>(tiles);
     for (int i = tid; i < words; i += kCacheThreads) st[i] = r0 > 0 ? ld_dependent(reinterpret_cast<const uint4 *>(codes) + i) : make_uint4(0, 0, 0, 0);
     const float old = r0 > 0 ? ld_dependent(scale_at) : 0.f;
     uint32_t top = 0;
-    for (int i = tid; i < (r1 - r0) * pieces; i += kCacheThreads) {
-        const int r = r0 + i / pieces, j = i % pieces;
-        const uint4 v = ld_dependent(reinterpret_cast<const uint4 *>(x + (ptrdiff_t)r * ld) + j);
-        top = i8_larger(top, i8_larger(i8_larger(i8_magnitudes(v.x), i8_magnitudes(v.y)), i8_larger(i8_magnitudes(v.z), i8_magnitudes(v.w))));
+    uint4 v[4] = {held[0], held[1], held[2], held[3]};
+#pragma unroll 1
+    for (int i = tid;;) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = i8_larger(top, i8_larger(i8_larger(i8_magnitudes(v[e].x), i8_magnitudes(v[e].y)), i8_larger(i8_magnitudes(v[e].z), i8_magnitudes(v[e].w))));
+        if ((i += kCacheThreads) >= quads) break;
+        rows_of(i, row, piece);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = load(row, piece, e);
     }
     top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16));
     if (lane == 0) tops[tid >> 5] = top;
@@ -95,14 +122,32 @@ __global__ void __launch_bounds__(kCacheThreads) append_kernel(const __grid_cons
         }
     }
     const I8Divisor d(scale);
-    for (int i = tid; i < (r1 - r0) * pieces; i += kCacheThreads) {
-        const int r = r0 + i / pieces, j = i % pieces;
-        const uint2 v = i8_codes<T>(d, ld_dependent(reinterpret_cast<const uint4 *>(x + (ptrdiff_t)r * ld) + j));
-        uint8_t *tile = tiles + (r >> 4) * 16 * width;
-        if (!values) *reinterpret_cast<uint2 *>(tile + cache_key_at(r & 15, j * 8)) = v;
-        else {
+#pragma unroll 1
+    for (int i = tid; i < quads; i += kCacheThreads) {
+        rows_of(i, row, piece);
+        uint2 u[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) tile[cache_value_at(r & 15, j * 8 + e)] = (uint8_t)((e < 4 ? v.x : v.y) >> (8 * (e & 3)));
+        for (int e = 0; e < 4; ++e) u[e] = i8_codes<T>(d, i == tid ? held[e] : load(row, piece, e));
+        uint8_t *tile = tiles + (row >> 4) * 16 * width;
+        if (!values) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (row_in(row, e)) *reinterpret_cast<uint2 *>(tile + cache_key_at((row & 15) + (e >> 1) * 8 + (e & 1), piece * 8)) = u[e];
+        } else {
+            // the four tokens' bytes of a column are a word: all of it where all four are new
+            const bool all = row_in(row, 0) && row_in(row, 3);
+#pragma unroll
+            for (int col = 0; col < 8; ++col) {
+                const uint32_t sel = (col & 3) | (4 + (col & 3)) << 4;
+                const uint32_t lo = __byte_perm(col < 4 ? u[0].x : u[0].y, col < 4 ? u[1].x : u[1].y, sel), hi = __byte_perm(col < 4 ? u[2].x : u[2].y, col < 4 ? u[3].x : u[3].y, sel);
+                const uint32_t word = __byte_perm(lo, hi, 0x5410);
+                uint8_t *to = tile + cache_value_at(row & 15, piece * 8 + col);
+                if (all) *reinterpret_cast<uint32_t *>(to) = word;
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (row_in(row, e)) to[e] = (uint8_t)(word >> (8 * e));
+            }
         }
     }
     __syncthreads();
@@ -111,60 +156,64 @@ __global__ void __launch_bounds__(kCacheThreads) append_kernel(const __grid_cons
     if (tid == 0) *scale_at = scale;
 }
 
-// ---- read: tokens back in 16 bits ------------------------------------------------------------------------------------------------
+// ---- read: tokens back in 16 bits; a CTA has the 16 tokens of a tile and one head ---------------------------------------------------
+// Pieces come as they lie in the cache and are turned into rows in shared memory.
 struct ReadParams {
     CacheSeqs c;
     void *k, *v;
     int ldk, ldv;
 };
 
-// The sequence that row `row` belongs to: the last one that starts at or before it, if its rows reach so far.
-__device__ __forceinline__ int sequence_of(const CacheSeqs &c, int row)
-{
-    if (!c.starts) return row < c.S ? row : -1;
-    int lo = 0, hi = c.S;                                        // starts[lo] <= row < starts[hi]
-    if (ld_dependent(c.starts) > row || ld_dependent(c.starts + c.S) <= row) return -1;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (ld_dependent(c.starts + mid) <= row) lo = mid; else hi = mid;
-    }
-    return lo;
-}
-
 template <typename T>
 __global__ void __launch_bounds__(kCacheThreads) read_cache_kernel(const __grid_constant__ ReadParams p)
 {
+    extern __shared__ __align__(16) uint8_t tiles[];             // [keys, values][16 tokens][width + 8]
+    __shared__ int found[2], warps[kCacheThreads / 32];
     const CacheSeqs &c = p.c;
-    const int row = blockIdx.x, pieces = c.width >> 3, page = 1 << c.page_sh;
+    const int tid = threadIdx.x, head = blockIdx.y, width = c.width, pitch = width + 8, page = 1 << c.page_sh;
+    T *rows = reinterpret_cast<T *>(tiles);
     grid_wait();
     grid_launch_next();
-    if (row == 0)                                                // (what no row is found by is reported all the same)
-        for (int i = threadIdx.x; i < c.S; i += kCacheThreads) {
-            const CacheSeq q = cache_seq(c, i);
-            if (q.rows > q.len) atomicCAS(c.status, 0u, (uint32_t)TMAN_ERR_INDEX);
-        }
-    const int s = sequence_of(c, row);
+    find_in_sequences(c.S, blockIdx.x, found, warps, [&](int s) { return steps_of(c, s, 4); });
+    const int s = found[0];
     if (s < 0) return;
     const CacheSeq q = cache_seq(c, s);
-    if (row < q.row || row >= q.row + q.rows) return;
-    const int pos = q.len - q.rows + row - q.row;
-    if (pos < 0) return;
-    const int id = cache_page(c, s, pos >> c.page_sh), r = pos & (page - 1);
+    const int first = q.len - q.rows, token0 = ((first >> 4) + found[1]) * 16, id = cache_page(c, s, token0 >> c.page_sh);
     if (id < 0) return;
-    const float *scales = reinterpret_cast<const float *>(c.cache + c.scales_off) + (size_t)id * c.heads * 2;
-    for (int i = threadIdx.x; i < c.heads * 2 * pieces; i += kCacheThreads) {
-        const int h2 = i / pieces, j = i % pieces, values = h2 & 1;
-        const uint8_t *tile = c.cache + ((size_t)id * c.heads * 2 + h2) * page * c.width + (r >> 4) * 16 * c.width;
-        const float scale = ld_dependent(scales + h2);
-        float z[8];
+    const size_t at = ((size_t)id * c.heads + head) * 2;
+    const uint8_t *tile = c.cache + at * page * width + (token0 & (page - 1)) * width;
+    const float *scales = reinterpret_cast<const float *>(c.cache + c.scales_off) + at;
+    const float ks = ld_dependent(scales), vs = ld_dependent(scales + 1);
+#pragma unroll 2
+    for (int i = tid; i < 2 * width; i += kCacheThreads) {       // pieces of keys, then of values
+        const bool values = i >= width;
+        const int j = values ? i - width : i, piece = j >> 5, g = (j & 31) >> 2, t = j & 3;
+        const uint4 u = ld_dependent(reinterpret_cast<const uint4 *>(tile + (values ? (size_t)page * width : 0)) + j);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        const float f = values ? vs : ks;
+        if (!values) {
+            uint32_t h[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint8_t *b = tile + (values ? cache_value_at(r & 15, j * 8 + e) : cache_key_at(r & 15, j * 8 + e));
-            z[e] = (float)*reinterpret_cast<const volatile int8_t *>(b) * scale;
+            for (int e = 0; e < 8; ++e) h[e] = f4_from_float2<T>((float)(int8_t)(w[e >> 1] >> (16 * (e & 1))) * f, (float)(int8_t)(w[e >> 1] >> (16 * (e & 1) + 8)) * f);
+            uint4 *to = reinterpret_cast<uint4 *>(rows + ((piece & 1) * 8 + g) * pitch + (piece >> 1) * 64 + t * 16);
+            to[0] = make_uint4(h[0], h[1], h[2], h[3]);
+            to[1] = make_uint4(h[4], h[5], h[6], h[7]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    rows[(16 + 2 * t + (b >> 1) * 8 + (b & 1)) * pitch + (4 * piece + e) * 8 + g] = f4_from_float<T>((float)(int8_t)(w[e] >> (8 * b)) * f);
         }
-        T *out = values ? static_cast<T *>(p.v) + (size_t)row * p.ldv : static_cast<T *>(p.k) + (size_t)row * p.ldk;
-        *reinterpret_cast<uint4 *>(out + (h2 >> 1) * c.width + j * 8) =
-            make_uint4(f4_from_float2<T>(z[0], z[1]), f4_from_float2<T>(z[2], z[3]), f4_from_float2<T>(z[4], z[5]), f4_from_float2<T>(z[6], z[7]));
+    }
+    __syncthreads();
+    const int pieces = width >> 3, r0 = max(first - token0, 0), r1 = min(q.len - token0, 16);
+    for (int i = tid; i < 32 * pieces; i += kCacheThreads) {
+        const int r = i / pieces, j = i % pieces, values = r >> 4, token = r & 15;
+        if (token < r0 || token >= r1) continue;
+        const size_t row = (size_t)(q.row + token0 + token - first);
+        T *out = (values ? static_cast<T *>(p.v) + row * p.ldv : static_cast<T *>(p.k) + row * p.ldk) + (size_t)head * width;
+        reinterpret_cast<uint4 *>(out)[j] = *reinterpret_cast<const uint4 *>(rows + r * pitch + j * 8);
     }
 }
 
@@ -198,8 +247,10 @@ tman_status launch_append_i8(const CacheSeqs &c, const void *k, int ldk, const v
 tman_status launch_read_cache_i8(const CacheSeqs &c, void *k, int ldk, void *v, int ldv, int dtype, cudaStream_t s)
 {
     const ReadParams p = {c, k, v, ldk, ldv};
-    const dim3 grid((unsigned)c.T);
-    return dtype == kF4TypeHalf ? launch(read_cache_kernel<__half>, p, grid, 0, s) : launch(read_cache_kernel<__nv_bfloat16>, p, grid, 0, s);
+    const long long most = ((long long)c.T >> 4) + 2ll * c.S;    // (tiles, as above)
+    const dim3 grid((unsigned)(most < c.T ? most : c.T), (unsigned)c.heads);
+    const size_t smem = (size_t)32 * (c.width + 8) * 2;
+    return dtype == kF4TypeHalf ? launch(read_cache_kernel<__half>, p, grid, smem, s) : launch(read_cache_kernel<__nv_bfloat16>, p, grid, smem, s);
 }
 
 }  // namespace tman

@@ -47,28 +47,37 @@ template <typename T> __device__ __forceinline__ float i8_scale(uint32_t top)
     return top >= i8_infinity<T>() ? __uint_as_float(0x7FFFFFFFu) : __fdiv_rn(i8_value<T>(top), 127.f);
 }
 
-// round(x / scale) of the quotient rounded to 32 bits.  The product with the reciprocal is off by 127 x 2^-23 at most, so that only a quotient
-// next to a half needs the division; so do scales whose reciprocal is none (a scale of 0 stands for zeros).
+// round(x / scale) of the quotient rounded to 32 bits, to nearest even.  Added to 2^23 + 2^22, the product with the reciprocal is rounded to an integer,
+// which is in the low bits; it is off by 127 x 2^-23 at most, so that only a quotient next to a half needs the division; so do scales whose reciprocal
+// is none (0 stands for zeros, and so does a scale that is no number).  No code is beyond 127: x is at most the scale's 127-fold.
 struct I8Divisor {
     float scale, inv;
     __device__ __forceinline__ explicit I8Divisor(float s) : scale(s), inv(s >= 1e-30f ? 1.f / s : 0.f) {}
-    __device__ __forceinline__ int code(float x) const
+    __device__ __noinline__ static uint32_t divided(float x, float scale)
     {
-        const float q = x * inv;
-        float r = rintf(q);
-        if (fabsf(q - r) > 0.4999f || inv == 0.f) r = scale > 0.f ? rintf(__fdiv_rn(x, scale)) : 0.f;       // (scale NaN: 0)
-        return (int)fminf(fmaxf(r, -127.f), 127.f);
+        const float r = scale > 0.f ? rintf(__fdiv_rn(x, scale)) : 0.f;
+        return (uint32_t)(int)fminf(fmaxf(r, -127.f), 127.f) & 0xFFu;
     }
 };
-__device__ __forceinline__ uint32_t i8_pack(int a, int b, int c, int d)
-{
-    return __byte_perm(__byte_perm((uint32_t)a, (uint32_t)b, 0x0040), __byte_perm((uint32_t)c, (uint32_t)d, 0x0040), 0x5410);
-}
 // Eight codes of eight 16-bit values.
 template <typename T> __device__ __forceinline__ uint2 i8_codes(const I8Divisor &d, const uint4 &v)
 {
-    const float2 a = f4_to_float2<T>(v.x), b = f4_to_float2<T>(v.y), c = f4_to_float2<T>(v.z), e = f4_to_float2<T>(v.w);
-    return make_uint2(i8_pack(d.code(a.x), d.code(a.y), d.code(b.x), d.code(b.y)), i8_pack(d.code(c.x), d.code(c.y), d.code(e.x), d.code(e.y)));
+    constexpr float kMagic = 12582912.f;
+    const float2 p[4] = {f4_to_float2<T>(v.x), f4_to_float2<T>(v.y), f4_to_float2<T>(v.z), f4_to_float2<T>(v.w)};
+    uint32_t c[8];
+    float far = 0.f;                                             // how far a quotient is from its integer at most
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = i & 1 ? p[i >> 1].y : p[i >> 1].x, r = fmaf(x, d.inv, kMagic);
+        far = fmaxf(far, fabsf(fmaf(x, d.inv, kMagic - r)));
+        c[i] = __float_as_uint(r);
+    }
+    if (far > 0.4999f || d.inv == 0.f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = I8Divisor::divided(i & 1 ? p[i >> 1].y : p[i >> 1].x, d.scale);
+    }
+    return make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
 }
 
 // sum x (token's scale x channel's scale).  The scales' product in 32 bits where it and what it multiplies stay in range, else in 64.

@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kI8Threads, 1) i8_stream_kernel(const __grid_c
         int c[TILES][4] = {};
         for (u = first; u.i < units;) {
             // the warp's tiles of a block
-            const int block = u.block, t0 = u.tile, t1 = min(tiles, t0 + units - u.i);
+            const int t0 = u.tile, t1 = min(tiles, t0 + units - u.i);
             const uint4 q0 = next[0], q1 = next[1];
             for (int i = t0; i < t1; ++i) on(u);
             codes_of(u.i < units ? u.block : first.block, next);
