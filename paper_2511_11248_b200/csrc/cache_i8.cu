@@ -4,7 +4,7 @@
 namespace tman {
 namespace {
 
-constexpr int kCacheThreads = 256;
+constexpr int kCacheThreads = 128;
 
 // Which of the things that the sequences have in turn, `of(s)` of them each, is number `index`: found[0] is its sequence (-1: there are fewer),
 // found[1] its place in it.  All threads.
@@ -49,7 +49,7 @@ __device__ __forceinline__ int steps_of(const CacheSeqs &c, int s, int sh)
 // codes are put together in shared memory and leave as they came, in 16-byte pieces.
 // Bound by latency for few tokens (what sequence, what page, what maximum, one behind the other) and by reading the rows for many: a thread takes
 // eight columns of four tokens whose codes are neighbours in the cache (cache_i8.cuh), so that values need no byte stores, and keeps the first it takes
-// in registers between the maximum and the codes (pages of more than 8192 values are read twice).
+// in registers between the maximum and the codes (pages of more than 4096 values are read twice).
 struct AppendParams {
     CacheSeqs c;
     const void *k, *v;

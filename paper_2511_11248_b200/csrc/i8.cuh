@@ -48,7 +48,7 @@ template <typename T> __device__ __forceinline__ float i8_scale(uint32_t top)
 }
 
 // round(x / scale) of the quotient rounded to 32 bits, to nearest even.  Added to 2^23 + 2^22, the product with the reciprocal is rounded to an integer,
-// which is in the low bits; it is off by 127 x 2^-23 at most, so that only a quotient next to a half needs the division; so do scales whose reciprocal
+// which is in the low bits; it is off by 127 x 2^-24 at most, and the quotient's own rounding by 2^-18, so that only one next to a half needs the division; so do scales whose reciprocal
 // is none (0 stands for zeros, and so does a scale that is no number).  No code is beyond 127: x is at most the scale's 127-fold.
 struct I8Divisor {
     float scale, inv;
@@ -62,7 +62,7 @@ struct I8Divisor {
 // Eight codes of eight 16-bit values.
 template <typename T> __device__ __forceinline__ uint2 i8_codes(const I8Divisor &d, const uint4 &v)
 {
-    constexpr float kMagic = 12582912.f;
+    constexpr float kMagic = 12582912.f, kNear = 0.499985f;
     const float2 p[4] = {f4_to_float2<T>(v.x), f4_to_float2<T>(v.y), f4_to_float2<T>(v.z), f4_to_float2<T>(v.w)};
     uint32_t c[8];
     float far = 0.f;                                             // how far a quotient is from its integer at most
@@ -72,9 +72,12 @@ template <typename T> __device__ __forceinline__ uint2 i8_codes(const I8Divisor 
         far = fmaxf(far, fabsf(fmaf(x, d.inv, kMagic - r)));
         c[i] = __float_as_uint(r);
     }
-    if (far > 0.4999f || d.inv == 0.f) {
+    if (far > kNear || d.inv == 0.f) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = I8Divisor::divided(i & 1 ? p[i >> 1].y : p[i >> 1].x, d.scale);
+        for (int i = 0; i < 8; ++i) {
+            const float x = i & 1 ? p[i >> 1].y : p[i >> 1].x;
+            if (d.inv == 0.f || fabsf(fmaf(x, d.inv, kMagic - __uint_as_float(c[i]))) > kNear) c[i] = I8Divisor::divided(x, d.scale);
+        }
     }
     return make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
                       __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
