@@ -85,6 +85,8 @@ template <typename T> __device__ __forceinline__ uint2 i8_codes(const I8Divisor 
 
 // sum x (token's scale x channel's scale).  The scales' product in 32 bits where it and what it multiplies stay in range, else in 64.
 __device__ __noinline__ inline float i8_scaled64(int sum, float a_scale, float w_scale) { return (float)((double)sum * (double)a_scale * (double)w_scale); }
+// Two such scales have a product that i8_scaled takes in 32 bits.
+__device__ __forceinline__ bool i8_ordinary(float s) { return s >= 1e-15f && s <= 1e14f; }
 __device__ __forceinline__ float i8_scaled(int sum, float a_scale, float w_scale)
 {
     const float s = a_scale * w_scale;

@@ -47,6 +47,7 @@ __global__ void __launch_bounds__(kI8PairThreads) i8_pair_kernel(const __grid_co
     extern __shared__ __align__(1024) uint8_t pair_smem[];
     __shared__ __align__(8) uint64_t full_bar[kI8PairStages], empty_bar[kI8PairStages], accf_bar[2], acce_bar[2], sums_bar;
     __shared__ uint32_t tmem_slot;
+    __shared__ float token_scale[8][kI8PairCols / 2];            // of an epilogue warp's tokens
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     // a cluster: the pairs with the shares of k of a tile, one tile each (split > 1), or one pair that walks over tiles
     const uint32_t crank = cluster_ctarank(), rank = crank & 1u, share = crank >> 1;
@@ -163,20 +164,28 @@ __global__ void __launch_bounds__(kI8PairThreads) i8_pair_kernel(const __grid_co
             const uint32_t b = ti & 1u;
             const int m0 = tile_m(tile) * p.nt, n = tile_n(tile) * 256 + (int)rank * 128 + quad * 32 + lane, n2 = n & ~1;
             const int end = p.M - m0, t0 = warp >= 6 ? half : 0;
-            const bool put = n2 < p.N, put1 = n2 + 1 < p.N, whole = warp_all(put && put1 && pairs_ok);
+            const bool put = n2 < p.N, put1 = n2 + 1 < p.N;
+            bool whole = put && put1 && pairs_ok;
             const size_t row2 = 2 * (size_t)p.ldy;
             const float w0 = ld_dependent(p.w_scale + min(n2, p.N - 1)), w1 = ld_dependent(p.w_scale + min(n2 + 1, p.N - 1));
             T *y = static_cast<T *>(p.y) + (size_t)(m0 + (odd ? 1 : 0)) * p.ldy + n2;
             const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + b * kI8PairCols;
             auto store16 = [&](auto whole_c, int t, const uint32_t (&r)[16]) {
                 constexpr bool WHOLE = decltype(whole_c)::value;
-                const float as = ld_dependent(p.a_scale + min(m0 + t + (lane & 15), p.M - 1));
+                const float *as = token_scale[warp - 2] + (t - t0) + (odd ? 1 : 0);
                 T *yt = y + (size_t)t * p.ldy;
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
                     const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? r[e] : r[e + 1], 1), keep = odd ? r[e + 1] : r[e];
-                    const float f = __shfl_sync(0xffffffffu, as, e + (odd ? 1 : 0));
-                    const float c0 = i8_scaled((int)(odd ? got : keep), f, w0), c1 = i8_scaled((int)(odd ? keep : got), f, w1);
+                    const float f = as[e];
+                    float c0, c1;
+                    if constexpr (WHOLE) {
+                        c0 = (float)(int)(odd ? got : keep) * (f * w0);
+                        c1 = (float)(int)(odd ? keep : got) * (f * w1);
+                    } else {
+                        c0 = i8_scaled((int)(odd ? got : keep), f, w0);
+                        c1 = i8_scaled((int)(odd ? keep : got), f, w1);
+                    }
                     if constexpr (WHOLE) st_policy(yt, f4_from_float2<T>(c0, c1), y_policy);
                     else if (t + e + (odd ? 1 : 0) < end && put) {
                         yt[0] = f4_from_float<T>(c0);
@@ -185,6 +194,15 @@ __global__ void __launch_bounds__(kI8PairThreads) i8_pair_kernel(const __grid_co
                     yt += row2;
                 }
             };
+            // (the tokens' scales before the sums are there: asked for sixteen at a time behind them, 777 x 3584 x 4608 spent 6.5 us here)
+            __syncwarp();
+            whole = whole && i8_ordinary(w0) && i8_ordinary(w1);
+            for (int i = lane; i < half; i += 32) {
+                const float f = ld_dependent(p.a_scale + min(m0 + t0 + i, p.M - 1));
+                token_scale[warp - 2][i] = f;
+                whole = whole && i8_ordinary(f);
+            }
+            whole = warp_all(whole);                             // pairs of channels, scales whose products are in range
             ok = warp_all(mbar_wait(accf0 + 8 * b, (ti >> 1) & 1u));
             if (!ok) break;
             tcgen05_fence_after();
@@ -205,13 +223,18 @@ __global__ void __launch_bounds__(kI8PairThreads) i8_pair_kernel(const __grid_co
     if (split > 1) {
         // ---- shares of a tile: column c of the tile is added up by share c / own in the CTA of the same channels; everyone sends it its sums,
         // [share][own column][channel] on the ring, which is idle everywhere once all accumulators are complete
-        if (warp >= 2) {
+        const int own = p.nt >> p.split_sh, m0 = tile_m(worker) * p.nt + (int)share * own, n0 = tile_n(worker) * 256 + (int)rank * 128;
+        const int ch = ((int)threadIdx.x & 63) * 2, n = n0 + ch;       // two channels of each of a thread's tokens
+        float w0 = 0.f, w1 = 0.f;
+        if (warp >= 2) {                                         // (scales before the sums are there)
+            w0 = ld_dependent(p.w_scale + min(n, p.N - 1));
+            w1 = ld_dependent(p.w_scale + min(n + 1, p.N - 1));
+            for (int i = lane; i < own; i += 32) token_scale[warp - 2][i] = ld_dependent(p.a_scale + min(m0 + i, p.M - 1));
             ok = warp_all(mbar_wait(accf0, 0)) && ok;
             tcgen05_fence_after();
         }
         __syncwarp();
         cluster_sync_all();
-        const int own = p.nt >> p.split_sh, m0 = tile_m(worker) * p.nt + (int)share * own, n0 = tile_n(worker) * 256 + (int)rank * 128;
         if (warp >= 2) {
             const int quad = warp & 3, half = p.nt >> 1, t0 = warp >= 6 ? half : 0;
 #pragma unroll 1
@@ -230,8 +253,9 @@ __global__ void __launch_bounds__(kI8PairThreads) i8_pair_kernel(const __grid_co
             for (int i = 0; i < 8 && !all; ++i) all = warp_all(mbar_wait(smem_u32(&sums_bar), 0));
             ok = ok && all;
             const int *sums = reinterpret_cast<const int *>(pair_smem + (ring - smem_u32(pair_smem)));
-            for (int i = threadIdx.x - 64; i < own * 64; i += kI8PairThreads - 64) {
-                const int c = i >> 6, ch = (i & 63) * 2, m = m0 + c, n = n0 + ch;
+#pragma unroll 2
+            for (int c = ((int)threadIdx.x - 64) >> 6; c < own; c += (kI8PairThreads - 64) / 64) {
+                const int m = m0 + c;
                 int v0 = 0, v1 = 0;
                 for (int r = 0; r < split; ++r) {
                     const int2 v = *reinterpret_cast<const int2 *>(sums + (r * own + c) * 128 + ch);
@@ -239,8 +263,7 @@ __global__ void __launch_bounds__(kI8PairThreads) i8_pair_kernel(const __grid_co
                     v1 += v.y;
                 }
                 if (ok && m < p.M && n < p.N) {
-                    const float f = ld_dependent(p.a_scale + m);
-                    const float c0 = i8_scaled(v0, f, ld_dependent(p.w_scale + n)), c1 = i8_scaled(v1, f, ld_dependent(p.w_scale + min(n + 1, p.N - 1)));
+                    const float f = token_scale[warp - 2][c], c0 = i8_scaled(v0, f, w0), c1 = i8_scaled(v1, f, w1);
                     T *y = static_cast<T *>(p.y) + (size_t)m * p.ldy + n;
                     if (pairs_ok) *reinterpret_cast<uint32_t *>(y) = f4_from_float2<T>(c0, c1);
                     else {
