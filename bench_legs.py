@@ -5,6 +5,7 @@
     python bench.py --leg config3 [--dense]        # one decoder layer's projections, bits {2,3,4} x M {1,2,4,8}
     python bench.py --leg config5 [--dense] [--all-groups]   # prefill shapes, M in {128,512,2048,8192}
     python bench.py --leg ternary                  # integer decode: ternary weights, 16-bit integer activations, BitNet sizes
+    python bench.py --leg attention                # a layer's attention half in 8 bits: decode steps and prompts
     python bench.py --leg ablation                 # prefill with ConvertDQ / LoadFull / sequential in place of the product path
     python bench.py --leg microbench               # lookup rates, load paths, cluster exchange
     TMAN_LIBRARY=paper_2511_11248_b200/libtman_stamps.so python bench.py --leg stamps   # where the prefill roles wait
@@ -450,6 +451,75 @@ def ternary(args, rest=()):
     for r in ternary_results(torch, B, H):
         print(json.dumps(r), flush=True)
     for r in ternary_prefill_results(torch, B, H):
+        print(json.dumps(r), flush=True)
+
+
+# ---- the attention half of a layer in 8 bits ----------------------------------------------------------------
+
+def attention_results(torch, B, reps=7, hidden=4096, heads=32, kv=8, width=128, page=16):
+    """q | k | v product, norm and rotation, append, attention over the cache, output product: Llama-3-8B's sizes, weights and cache in 8 bits.
+    One decode step of several sequences, or a prompt on top of what the cache holds; from a CUDA graph of four layers, a cache and
+    weights each."""
+    out, layers, nq, nk = [], 4, heads * width, kv * width
+    ld, scale = nq + 2 * nk, width ** -0.5
+    freq = (10000.0 ** (-torch.arange(0, width, 2, device="cuda", dtype=torch.float64) / width)).float()
+    norm = [torch.ones(width, dtype=torch.float16, device="cuda") for _ in range(2)]
+    for S, length, new in ((1, 1000, 1), (8, 8000, 1), (32, 8000, 1), (1, 2048, 2048), (1, 8192, 2048)):
+        T, pages = S * new, (length + page - 1) // page
+        table = torch.randperm(S * pages, device="cuda").to(torch.int32).view(S, pages)
+        lens = torch.full((S,), length, dtype=torch.int32, device="cuda")
+        full, starts = (torch.arange(S + 1, dtype=torch.int32, device="cuda") * n for n in (length, new))
+        positions = (lens[:, None] - new + torch.arange(new, dtype=torch.int32, device="cuda")).reshape(-1).contiguous()
+        x = torch.randn(T, hidden, device="cuda").half()
+        qkv, att, y = (torch.empty(T, n, dtype=torch.float16, device="cuda") for n in (ld, nq, hidden))
+        a, a_scale = torch.empty(T, hidden, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+        ws = torch.empty(B.tman_workspace_bytes_attend(width), dtype=torch.uint8, device="cuda")
+        op, M = (B.OP_GEMV, T) if T <= 8 else (B.OP_GEMM, T)
+        wp = torch.empty(max(B.tman_workspace_bytes_i8(op, M, k, n) for k, n in ((hidden, ld), (nq, hidden))), dtype=torch.uint8, device="cuda")
+        for w in (ws, wp):
+            B.tman_workspace_init(w)
+        sets = []
+        for _ in range(layers):
+            w = [torch.randint(-127, 128, s, dtype=torch.int8, device="cuda") for s in ((ld, hidden), (hidden, nq))]
+            cache = torch.zeros(B.tman_cache_bytes_i8(S * pages, page, kv, width), dtype=torch.uint8, device="cuda")
+            k, v = (torch.randn(S * length, nk, device="cuda").half() for _ in range(2))
+            B.tman_append_i8(cache, S * pages, page, kv, width, k, nk, v, nk, B.DTYPE_F16, table, pages, lens, full, S, S * length, ws)
+            sets.append((w, [torch.full((n,), 1e-4, device="cuda") for n in (ld, hidden)], cache))
+
+        def product(w, s, x, y, K, N):
+            if T <= 8:
+                B.tman_mpgemv_i8(w, K, s, x, K, y, N, B.DTYPE_F16, T, K, N, wp)
+            else:
+                B.tman_quantize_tokens_i8(x, K, B.DTYPE_F16, T, K, a, a_scale)
+                B.tman_mpgemm_i8(w, K, s, a, a_scale, y, N, B.DTYPE_F16, T, K, N, wp)
+
+        def step():
+            for w, s, cache in sets:
+                product(w[0], s[0], x, qkv, hidden, ld)
+                B.tman_norm_rotate(qkv, ld, qkv, ld, B.DTYPE_F16, T, heads, kv, width, width, 0, *norm, 1e-6, positions, freq)
+                B.tman_append_i8(cache, S * pages, page, kv, width, qkv[:, nq:], ld, qkv[:, nq + nk:], ld, B.DTYPE_F16, table, pages, lens, starts, S, T, ws)
+                B.tman_attend_i8(qkv, ld, att, nq, B.DTYPE_F16, heads, cache, S * pages, page, kv, width, table, pages, lens, starts, S, T, scale, 0, ws)
+                product(w[1], s[1], att, y, nq, hidden)
+
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        us, best = event_us(torch, graph.replay, reps)
+        assert B.tman_read_status(ws) == 0 and B.tman_read_status(wp) == 0
+        read = hidden * ld + nq * hidden + 2 * S * length * nk
+        out.append({"leg": "attention", "sequences": S, "tokens": length, "new": new, "us_per_layer": round(us / layers, 1), "best": round(best / layers, 1),
+                    "weight_and_cache_GBps": round(read / us * layers / 1e3, 1)})
+        del sets, graph
+        torch.cuda.empty_cache()
+    return out
+
+
+def attention(args, rest=()):
+    import torch
+    from paper_2511_11248_b200 import binding as B
+    for r in attention_results(torch, B):
         print(json.dumps(r), flush=True)
 
 

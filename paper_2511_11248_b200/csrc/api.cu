@@ -517,7 +517,7 @@ tman_status tman_attend_i8(const void *q, int ldq, void *y, int ldy, int dtype, 
                            float scale, int window, void *workspace, size_t ws_bytes, tman_stream_t stream)
 {
     TMAN_F4_CHECK(check_cache(cache, cache_bytes, pages, page, kv_heads, width, table, ld_table, lens, starts, S, T));
-    if (heads < 1 || heads % kv_heads != 0 || window < 0) return TMAN_ERR_SHAPE;
+    if (heads < 1 || heads % kv_heads != 0 || heads / kv_heads > 4096 || window < 0) return TMAN_ERR_SHAPE;
     TMAN_F4_CHECK(check_cache_rows(q, ldq, dtype, (long long)heads * width, T));
     TMAN_F4_CHECK(check_cache_rows(y, ldy, dtype, (long long)heads * width, T));
     TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, attend_workspace_bytes(width)));

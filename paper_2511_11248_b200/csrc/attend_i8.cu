@@ -530,10 +530,6 @@ template <typename T, int D> tman_status launch(AttendParams p, cudaStream_t s)
     const DeviceInfo *info = device_info(&dev);
     if (!info) return TMAN_ERR_CUDA;
     const int sms = info->sms.load(std::memory_order_relaxed);
-    // steps are counted in 32 bits
-    const long long steps = ((long long)p.c.ldt << p.c.page_sh) / 16 + kItemCost, rows = p.c.starts ? (long long)p.c.T * p.group : p.group;
-    const long long tiles = ((rows < p.least ? rows : p.least) + kAttendRows - 1) / kAttendRows;
-    if (tiles * steps > INT32_MAX || tiles * steps * p.c.heads > INT32_MAX || tiles * steps * p.c.heads * p.c.S > INT32_MAX) return TMAN_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(sms < kAttendCtas ? sms : kAttendCtas));
     cfg.blockDim = dim3(AttendShape<D>::kThreads);
@@ -550,8 +546,7 @@ template <typename T, int D> tman_status launch(AttendParams p, cudaStream_t s)
 template <typename T, int D> tman_status launch_both(AttendParams p, cudaStream_t s)
 {
     // Sequences of many rows go to the kernel for prompts, where the call has room for one; which do is known on the device only.
-    if (p.c.starts && (long long)p.c.T * p.group >= kPromptRows) {
-        p.least = kPromptRows;
+    if (p.least == kPromptRows) {
         const PromptParams q = {p.c, p.q, p.y, p.ldq, p.ldy, p.group, p.window, kPromptRows, p.scale};
         const tman_status st = launch_prompt<T, D>(q, s);
         if (st != TMAN_OK) return st;
@@ -576,8 +571,13 @@ tman_status launch_attend_i8(const CacheSeqs &c, const void *q, int ldq, void *y
 {
     uint8_t *w8 = static_cast<uint8_t *>(ws);
     const int group = q_heads / c.heads;
+    const long long rows = c.starts ? (long long)c.T * group : group;
+    const bool prompts = c.starts && rows >= kPromptRows;
+    // steps are counted in 32 bits
+    const long long steps = ((long long)c.ldt << c.page_sh) / 16 + kItemCost, tiles = ((prompts ? kPromptRows : rows) + kAttendRows - 1) / kAttendRows;
+    if (tiles * steps > INT32_MAX || tiles * steps * c.heads > INT32_MAX || tiles * steps * c.heads * c.S > INT32_MAX) return TMAN_ERR_UNSUPPORTED;
     const AttendParams p = {c, q, y, reinterpret_cast<float *>(w8 + kWsStatusBytes + kAttendCtas * 4), reinterpret_cast<uint32_t *>(w8 + kWsStatusBytes),
-                            ldq, ldy, group, window, INT_MAX, group == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)group + 1u, scale};
+                            ldq, ldy, group, window, prompts ? kPromptRows : INT_MAX, group == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)group + 1u, scale};
     return dtype == kF4TypeHalf ? launch_width<__half>(p, s) : launch_width<__nv_bfloat16>(p, s);
 }
 

@@ -275,6 +275,49 @@ def test_more_rows_than_tokens():
     assert B.tman_read_status(q.ws) == 9
 
 
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+def test_prompts_of_more_rows_than_tokens_and_heads_of_one_key_head(ty):
+    """Tiles of rows that begin in front of the first token; many query heads of one key head; a prompt whose last tile of rows has one."""
+    rng = np.random.default_rng(14)
+    lens, new = [20, 0, 70, 129], [100, 70, 70, 129]
+    q = Sequences(io, lens, 16, 1, 64, rng)
+    q.append(lens, lens, ty, rng)
+    for window in (0, 5):
+        attend(q, lens, new, 1, ty, rng, window=window)
+    attend(q, lens, [3, 0, 2, 1], 80, ty, rng)
+    q128 = Sequences(io, [40], 16, 1, 128, rng)
+    q128.append([40], [40], ty, rng)
+    attend(q128, [40], [3], 86, ty, rng)                  # 258 rows: two blocks, the second of two rows
+
+
+def test_two_graphs_with_workspaces_of_their_own_side_by_side():
+    """Two captured steps on two streams, replayed at the same time: each with its workspace, over one cache."""
+    rng = np.random.default_rng(15)
+    lens = [3000, 700]
+    q = Sequences(io, lens, 16, 2, 128, rng)
+    q.append(lens, lens, "f16", rng)
+    st = np.array([0, 1, 2], dtype=np.int32)
+    lens_d, starts = up(np.array(lens, dtype=np.int32)), up(st)
+    runs = []
+    for _ in range(2):
+        xd, xv = rows_on_device(rng.standard_normal((2, 1024)), 1024, torch.float16)
+        y, ws, stream = H.alloc_matrix(2, 1024, torch.float16), workspace(B.tman_workspace_bytes_attend(128)), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            for _ in range(3):
+                B.tman_attend_i8(xd, 1024, y, 1024, B.DTYPE_F16, 8, q.cache, *q.geometry(), q.table_d, q.table.shape[1], lens_d, starts, 2, 2, 0.09, 0, ws, stream=stream)
+        runs.append((graph, stream, xv, y, ws, xd))
+    for _ in range(5):
+        for graph, stream, *_ in runs:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, _, xv, y, ws, _ in runs:
+        assert B.tman_read_status(ws) == 0
+        check(f64(y), *io.attend(xv.reshape(2, 8, 128), q.oracle, q.table, lens, st, float(np.float32(0.09)), 0), 128, "f16")
+
+
 def test_cache_offsets_beyond_32_bits():
     rng = np.random.default_rng(13)
     pages, page, heads, width = 140000, 16, 8, 128        # 4.6 GB
