@@ -60,7 +60,7 @@ odd = lambda i, by: Fake((1 << 30) + (i << 25) + by, 1 << 24)
     (dict(ldk=120), 2, ("append", "read")), (dict(ldv=132), 2, ("append", "read")), (dict(k=odd(12, 2)), 2, ("append", "read")), (dict(v=Fake(0, 9)), 1, ("append", "read")),
     (dict(ldq=248), 2, ("attend",)), (dict(q=odd(17, 2)), 2, ("attend",)), (dict(heads=5), 2, ("attend",)), (dict(heads=0), 2, ("attend",)), (dict(window=-1), 2, ("attend",)),
     (dict(ws=Fake(1 << 30, 1000)), 4, ("attend",)), (dict(T=1 << 30), 2, CACHED), (dict(kv=1, heads=4097, ldq=1 << 20, ldo=1 << 20), 2, ("attend",)),
-    (dict(ld_table=1 << 27, S=5), 3, ("attend",))])
+    (dict(ld_table=1 << 28, S=5), 3, ("attend",))])
 def test_wrong_arguments_are_refused_before_any_launch(lib, over, status, calls):
     from paper_2511_11248_b200 import binding as B
     table = _calls(B, **over)
