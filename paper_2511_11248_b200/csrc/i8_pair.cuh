@@ -4,7 +4,9 @@
 // A pair of CTAs (cta_group::2) has a tile of 256 channels (the rows of the tensor-core tile, 128 a CTA) x up to 256 tokens (its columns, each CTA
 // loads half of them).  128 bytes of k of both operands are a stage of a ring, brought by TMA into 128-byte swizzled tiles; one thread of the pair
 // issues the MMAs.  Tensor memory holds two accumulators of 256 columns, so that a tile's epilogue runs behind the next tile's MMAs.
-// What bounds it: 256 x 256 x 128 products take a pair 512 clocks, in which each CTA takes 32 KB from L2.
+// What bounds it: 256 x 256 x 128 products take a pair 512 clocks, in which each CTA takes 32 KB from L2; long calls by the power limit: 8192 x 4096 x 14336 295 us (3.27 POPS,
+// twice the measured bf16 rate), 8192 x 18944 x 3584 340 to 355, 2048 x 4096 x 14336 79.  One round of tiles has start and epilogue around it: 777 x 3584 x 4608 15.4
+// us, 7.5 of them MMAs; few tokens stream the weights: 40 x 4096 x 14336 14 to 16 (floor 9.2).
 #pragma once
 
 #include "i8_stream.cuh"

@@ -7,8 +7,10 @@
 // as integers: exact, whatever their order.
 // Codes come from global memory, a unit's as its weights are waited for.  Rows of 16 bits are quantized by every CTA itself, which spares a launch, as
 // long as there are few values (i8_matmul.cu).
-// Other ways: weights straight to registers, two batches of eight loads (1 x 4096 x 14336 14.9 us, this one XX); TMA boxes of 64 bytes x the CTA's
-// channels (12.4, but 4096 x 1024 5.9 instead of 2.9 and 14336 x 4096 21 instead of 15.5: the rows of a box cost two nanoseconds each).
+// In a graph, weights not in L2 (the product alone; floor): 1 x 4096 x 14336 13.7 us (9.0), 8 x 14336 x 4096 13.4 (9.0), 8 x 18944 x 3584 15.9 (10.4), 1 x 4096 x 1024 3.6:
+// 4.9 TB/s with some 3 us around the stream.  Other ways: weights straight to registers, two batches of eight loads (1 x 4096 x 14336 14.9); TMA
+// boxes of 64 bytes x the CTA's channels (12.4, but 4096 x 1024 5.9 and 14336 x 4096 21: the rows of a box cost two nanoseconds each); units channels
+// first, the codes fetched again for each (8 x 4096 x 14336 16.4, now 14.1).
 #pragma once
 
 #include "i8.cuh"
