@@ -54,6 +54,8 @@ __global__ void __launch_bounds__(kHeadThreads) norm_rotate_kernel(const __grid_
         if (head >= chunk || token > tokens) token = tokens;
         head += head0;
     };
+    grid_wait();                         // (the rows, their positions and the output are other kernels' until here)
+    grid_launch_next();
     uint4 held[TURNS];
 #pragma unroll
     for (int n = 0; n < TURNS; ++n) {
