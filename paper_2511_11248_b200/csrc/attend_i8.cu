@@ -200,6 +200,10 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
                     const float *f = scales + (size_t)l.id * c.heads * 2;
                     l.ks = ld_dependent(f);
                     l.vs = ld_dependent(f + 1);
+                    if (l.vs != l.vs) {                          // values that are none: in the scores, whose masked ones do not count
+                        l.ks = l.vs;
+                        l.vs = 1.f;
+                    }
                 }
             }
             return l;

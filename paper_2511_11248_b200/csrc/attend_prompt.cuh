@@ -320,8 +320,9 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
             if (most > 0.f) seen = most;
             if (w == 0 && lane < GROUPS) {
-                const float u = value_scale == 0.f ? (seen > 0.f ? seen : 1.f) : value_scale, v = u < 0x1p-120f ? 0x1p-120f : u;
-                page_consts[j & (Sh::kConsts - 1)][lane] = id < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f) : make_float4(key_scale, __log2f(v), 1.f / v, 0.f);
+                const bool none = value_scale != value_scale;     // values that are none: in the scores, whose masked ones do not count
+                const float u = value_scale == 0.f || none ? (seen > 0.f ? seen : 1.f) : value_scale, v = u < 0x1p-120f ? 0x1p-120f : u;
+                page_consts[j & (Sh::kConsts - 1)][lane] = id < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f) : make_float4(none ? value_scale : key_scale, __log2f(v), 1.f / v, 0.f);
             }
             uint8_t *kt = smem + Sh::kQ + s * Sh::kKv, *vt = smem + Sh::kQ + (NS + s) * Sh::kKv;
 #pragma unroll

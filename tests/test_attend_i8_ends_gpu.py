@@ -1,0 +1,30 @@
+"""Attention over the 8-bit cache at the ends of what it takes: pages that stand for NaN, windows and lengths next to 2^31, values of any size."""
+import numpy as np
+import pytest
+import torch
+
+from i8_common import TYPES, Sequences, f64, rows_on_device, up, within, workspace
+from oracle import i8_oracle as io
+from paper_2511_11248_b200 import binding as B, helpers as H
+from test_attend_i8_gpu import attend
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("page,lens,new,at,bad", [(16, [34, 9], [4, 1], 33, np.inf), (16, [50, 33], [3, 2], 40, -np.inf), (64, [130, 20], [5, 3], 129, np.nan),
+                                                  (16, [120, 40], [100, 40], 70, np.inf), (64, [333, 64], [300, 1], 200, np.nan),
+                                                  (16, [333, 70], [300, 70], 332, np.inf), (128, [700, 3], [290, 3], 600, -np.inf)])
+def test_a_value_page_that_is_no_number_is_seen_by_the_rows_that_see_it_only(page, lens, new, at, bad, ty):
+    """The bad value is in the middle of the new tokens, so that rows in front of its page and, with a window, behind it share a tile with rows that see
+    it; in one of two key heads, and then a bad key of another page too."""
+    rng = np.random.default_rng(at)
+    for keys in (False, True):
+        q = Sequences(io, lens, page, 2, 64, rng)
+        k, v = rng.standard_normal((sum(lens), 128)), rng.standard_normal((sum(lens), 128))
+        v[at, 70] = bad                                   # head 1
+        if keys:
+            k[at - page if at >= page else at, 3] = bad   # head 0
+        q.append(lens, lens, ty, rng, k=k, v=v)
+        for window in (0, 1, 2, 20, 100):
+            attend(q, lens, new, 4, ty, rng, window=window)
