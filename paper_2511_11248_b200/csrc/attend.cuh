@@ -17,6 +17,8 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// The first token that a row at `position` sees, of a window (0: none).  The position may be negative and the window any: their difference need not be a number.
+__device__ __forceinline__ int window_from(int position, int window) { return window > 0 && position >= window ? position - window + 1 : 0; }
 // Four signed bytes as fp16: with the top bit turned they are 0..255, which in the low byte of 0x6400 is 1024 + that.
 __device__ __forceinline__ void bytes_to_half(uint32_t w, uint32_t &lo, uint32_t &hi)
 {

@@ -63,7 +63,7 @@ __device__ __forceinline__ TileKeys tile_keys(const AttendParams &p, const Cache
     const int rows = q.rows * p.group, i0 = token_of(p, tile * kAttendRows), i1 = token_of(p, min(tile * kAttendRows + kAttendRows - 1, rows - 1));
     k.first = q.len - q.rows + i0;
     k.hi = max(q.len - q.rows + i1 + 1, 0);
-    k.lo = p.window > 0 ? max(k.first - p.window + 1, 0) : 0;
+    k.lo = window_from(k.first, p.window);
     k.step0 = k.lo >> 4;
     k.steps = max(((k.hi + 15) >> 4) - k.step0, 1);
     return k;
@@ -277,8 +277,8 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
         const float rf0 = row_factor[g], rf1 = row_factor[g + 8];
         auto limit_of = [&](int r) { return it.q.len - it.q.rows + token_of(p, it.tile * kAttendRows + min(r, rows - 1)); };
         const int lim0 = limit_of(g), lim1 = limit_of(g + 8);
-        const int low0 = p.window > 0 ? lim0 - p.window + 1 : INT_MIN, low1 = p.window > 0 ? lim1 - p.window + 1 : INT_MIN;
-        const int all_from = p.window > 0 ? it.k.hi - p.window : INT_MIN;       // tokens [all_from, first] are seen by every row
+        const int low0 = window_from(lim0, p.window), low1 = window_from(lim1, p.window);
+        const int all_from = p.window > 0 ? it.k.hi - p.window : 0;      // tokens [all_from, first] are seen by every row
         float o[NT][4];
 #pragma unroll
         for (int i = 0; i < NT; ++i)

@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
     const CacheSeq q = cache_seq(c, seq);
     const int row0 = found[1] * Sh::kRows, rows = min(q.rows * p.group - row0, Sh::kRows), pos0 = q.len - q.rows;
     const int first = pos0 + row0 / p.group, last = pos0 + (row0 + rows - 1) / p.group;      // positions of the first and the last row
-    const int hi = max(last + 1, 0), lo = p.window > 0 ? max(first - p.window + 1, 0) : 0;
+    const int hi = max(last + 1, 0), lo = window_from(first, p.window);
     const int tile0 = lo / KT, tiles = max((hi + KT - 1) / KT - tile0, 1), active = RT == 2 && rows > 128 ? 2 : 1;       // tiles of keys, of rows
     if (warp == Sh::kSoft + Sh::kLoad) {
         tcgen05_alloc(smem_u32(&tmem_slot), 512);
@@ -161,14 +161,14 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             if (lane == 0) mbar_arrive(smem_u32(&q_bar));
 
             const float rf = p.scale * kLog2e / f;
-            const int limit = pos0 + token, low = p.window > 0 ? limit - p.window + 1 : INT_MIN;
+            const int limit = pos0 + token, low = window_from(limit, p.window);
             const int least_limit = __reduce_min_sync(0xffffffffu, limit), most_low = __reduce_max_sync(0xffffffffu, low);
             const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16), out = at + Sh::kOut + r * D;
             float M = -INFINITY, l = 0.f;
             for (int j = 0; j < tiles; ++j) {
                 const int k0 = (tile0 + j) * KT;
                 const bool plain = k0 + KT - 1 <= least_limit && k0 >= most_low;
-                const int upto = limit - k0, from = low == INT_MIN ? INT_MIN : low - k0;      // columns that this row sees
+                const int upto = limit - k0, from = low - k0;      // columns that this row sees
                 const float4 *consts = page_consts[j & (Sh::kConsts - 1)];
                 const uint32_t score = at + Sh::kScore + (r * 2 + (j & 1)) * KT;
                 ok = warp_all(mbar_wait(smem_u32(&s_full[r][j & 1]), (j >> 1) & 1));

@@ -28,3 +28,17 @@ def test_a_value_page_that_is_no_number_is_seen_by_the_rows_that_see_it_only(pag
         q.append(lens, lens, ty, rng, k=k, v=v)
         for window in (0, 1, 2, 20, 100):
             attend(q, lens, new, 4, ty, rng, window=window)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 3, 2 ** 31 - 90])
+def test_windows_next_to_the_largest_number(window):
+    """Such a window is none, also for rows in front of the first token, whose positions are negative."""
+    rng = np.random.default_rng(12)
+    lens = [3, 20, 0, 129]
+    for heads in (1, 2):
+        q = Sequences(io, lens, 16, 1, 64, rng)
+        q.append(lens, lens, "f16", rng)
+        attend(q, lens, [5, 2, 1, 3], heads, "f16", rng, window=window)
+        attend(q, lens, [5, 30, 0, 10], heads, "f16", rng, window=window)
+        attend(q, lens, [100, 70, 70, 129], heads, "f16", rng, window=window)
+        attend(q, lens, [300, 2, 70, 64], heads, "f16", rng, window=window)
