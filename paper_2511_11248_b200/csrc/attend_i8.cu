@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
         __syncthreads();
     }
     const int total = before[Sh::kThreads];                      // (below 2^31: checked by the host)
-    int run = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+    int run = total / (int)gridDim.x + (total % (int)gridDim.x != 0);
     run = max((run + W - 1) / W, 1) * W;
 
     // Sequence, head and tile of a unit, by all threads alike.

@@ -42,3 +42,17 @@ def test_windows_next_to_the_largest_number(window):
         attend(q, lens, [5, 30, 0, 10], heads, "f16", rng, window=window)
         attend(q, lens, [100, 70, 70, 129], heads, "f16", rng, window=window)
         attend(q, lens, [300, 2, 70, 64], heads, "f16", rng, window=window)
+
+
+def test_as_many_steps_as_a_call_may_have():
+    """49 for each head of an empty sequence: 43 less than 2^31, so that a sum with the number of multiprocessors is beyond it."""
+    S, heads, width = 788, 55617, 64
+    assert 2 ** 31 - 148 < S * heads * 49 < 2 ** 31
+    row = heads * width
+    q, y = torch.zeros(S, row, dtype=torch.float16, device="cuda"), torch.full((S, row), float("nan"), dtype=torch.float16, device="cuda")
+    cache = torch.zeros(B.tman_cache_bytes_i8(1, 16, heads, width), dtype=torch.uint8, device="cuda")
+    table, lens = torch.zeros(S, 1, dtype=torch.int32, device="cuda"), torch.zeros(S, dtype=torch.int32, device="cuda")
+    ws = workspace(B.tman_workspace_bytes_attend(width))
+    B.tman_attend_i8(q, row, y, row, B.DTYPE_F16, heads, cache, 1, 16, heads, width, table, 1, lens, None, S, S, 0.125, 0, ws)
+    assert B.tman_read_status(ws) == 0
+    assert bool((y == 0).all())
