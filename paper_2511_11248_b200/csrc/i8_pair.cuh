@@ -204,6 +204,7 @@ __global__ void __launch_bounds__(kI8PairThreads) i8_pair_kernel(const __grid_co
                 token_scale[warp - 2][i] = f;
                 whole = whole && i8_ordinary(f);
             }
+            __syncwarp();                        // (the lanes read one another's scales)
             whole = warp_all(whole);                             // pairs of channels, scales whose products are in range
             ok = warp_all(mbar_wait(accf0 + 8 * b, (ti >> 1) & 1u));
             if (!ok) break;

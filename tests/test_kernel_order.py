@@ -57,3 +57,15 @@ def test_a_kernel_that_may_start_early_waits_and_lets_the_next_one_start_behind_
 def test_activations_are_read_behind_the_wait(name, kernel, body):
     """Of the 8-bit operators, which have no rule about what the kernels ahead write: nothing is loaded ahead of the wait (prefetches into L2 apart)."""
     assert not re.search(r"ld\.global|ld_dependent\(|load_runs\(|__ldg\(|atomic", body[:WAIT.search(body).start()]), kernel
+
+
+def test_scales_that_a_warp_passes_on_through_shared_memory_are_behind_a_barrier():
+    """i8_pair_kernel: a lane writes tokens' scales that the others of its warp read; a vote orders no memory."""
+    body = next(k[2] for k in kernels() if k[1] == "i8_pair_kernel")
+    writes = [m.start() for m in re.finditer(r"token_scale\[warp - 2\]\[i\] = ", body)]
+    assert len(writes) == 2
+    for at in writes:
+        after = body[at:]
+        barrier = re.search(r"__syncwarp\(\);|__syncthreads\(\);", after)
+        wait = after.index("mbar_wait(")                   # what stands between a write and the reads of the same tile
+        assert barrier and (barrier.start() < wait or not re.search(r"store16\(|token_scale", after[wait:barrier.start()])), after[:200]
