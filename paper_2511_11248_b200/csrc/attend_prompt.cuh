@@ -6,7 +6,9 @@
 // rows x columns, both in tensor memory); four warps a tile of rows, a thread a row, do the softmax.  A tile of rows has two buffers of
 // scores: while one is worked on, the other is filled, so that the softmax warps need not wait for the tensor cores.
 // A score is (q . code) x (key page's scale) x scale; probabilities carry the value page's scale, p' = 2^(s + log2 vs - M), so that codes are what they are
-// multiplied with, and the row's sum is that of p' / vs.  They go back to tensor memory over the scores, as the A operand of the second product.  M
+// multiplied with, and the row's sum is that of p' / vs, of p' as fp16 holds it: what the rounding takes from a probability it takes from the sum too, so that one
+// that counts for nearly all is not off (with sums ahead of the rounding it was, by up to 2^-12, since M need not be the maximum).  Pages whose values are small
+// beside others' may count for much in the sum and be far down in fp16's range: theirs are added up ahead of the rounding.  They go back to tensor memory over the scores, as the A operand of the second product.  M
 // is the maximum so far and raised, and the output so far scaled, only when a score is above it by more than 10: p' is at most 2^10, rows seldom
 // raise it after their first keys, and one pass over the scores is enough; one that finds such a score is made again behind the raise.
 // 2 x 2048 new tokens over 4096, 32 heads of 128 (floor 87): scores twice from tensor memory and a wait for both products in turn 274 us; with one pass, keys
@@ -35,8 +37,14 @@ struct PromptParams {
     float scale;
 };
 
+constexpr float kPromptSmall = 0.125f;   // scales of values below this much of the largest are small
 constexpr float kPromptSlack = 10.f;     // a score above the maximum so far by this much raises it
 
+// Two fp16 numbers added to two sums in 32 bits.
+__device__ __forceinline__ void add_halves(float &lo, float &hi, uint32_t pair)
+{
+    asm("{\n.reg .f16 a, b;\nmov.b32 {a, b}, %2;\nadd.rn.f32.f16 %0, a, %0;\nadd.rn.f32.f16 %1, b, %1;\n}" : "+f"(lo), "+f"(hi) : "r"(pair));
+}
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <typename T, int D>
@@ -47,7 +55,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
     extern __shared__ __align__(1024) uint8_t prompt_smem[];
     __shared__ __align__(8) uint64_t q_bar, k_full[NS], k_empty[NS], v_full[NS], v_empty[NS], s_full[RT][2], p_full[RT][2], o_full[RT], all_bar[RT];
     __shared__ uint32_t tmem_slot;
-    __shared__ float4 page_consts[Sh::kConsts][GROUPS];          // of 16 keys: scale of the keys, log2 of the values' scale and its reciprocal
+    __shared__ float4 page_consts[Sh::kConsts][GROUPS];          // of 16 keys: scale of the keys, log2 of the values' scale and its reciprocal, negative: sums ahead of the rounding
     __shared__ int found[2], sums[Sh::kThreads / 32 + 1];
     const CacheSeqs &c = p.c;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, page_mask = (1 << c.page_sh) - 1;
@@ -232,15 +240,23 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
 #pragma unroll
                             for (int e = 0; e < 32; ++e) x[e] = 32 * i + e <= upto && 32 * i + e >= from ? x[e] : -INFINITY;
                         }
-                        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            mx = fmaxf(mx, fmaxf(x[e], x[e + 1]));
-                            const float u = exp2_fast(x[e]), v = exp2_fast(x[e + 1]);
-                            if (e < 16) { s0 += u; s1 += v; } else { s2 += u; s3 += v; }
-                            h[16 * i + e / 2] = f4_from_float2<__half>(u, v);
+                        for (int half = 0; half < 2; ++half) {
+                            float s0 = 0.f, s1 = 0.f;
+                            const float unit = half == 0 ? c0.z : c1.z;
+                            const auto add16 = [&](auto as_rounded) {
+#pragma unroll
+                                for (int e = 16 * half; e < 16 * half + 16; e += 2) {
+                                    mx = fmaxf(mx, fmaxf(x[e], x[e + 1]));
+                                    const float u = exp2_fast(x[e]), v = exp2_fast(x[e + 1]);
+                                    h[16 * i + e / 2] = f4_from_float2<__half>(u, v);
+                                    if constexpr (decltype(as_rounded)::value) add_halves(s0, s1, h[16 * i + e / 2]);
+                                    else { s0 += u; s1 += v; }
+                                }
+                            };
+                            if (unit >= 0.f) add16(std::true_type()); else add16(std::false_type());
+                            sum = fmaf(s0 + s1, fabsf(unit), sum);
                         }
-                        sum = fmaf(s0 + s1, c0.z, fmaf(s2 + s3, c1.z, sum));
                         asm volatile("" : "+f"(sum), "+f"(mx));          // (added up here: put off, the values would stay in registers)
                     }
                     // (once: what the maximum was taken of is rounded apart from this by less than a unit)
@@ -285,7 +301,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
         const float *scales = reinterpret_cast<const float *>(c.cache + c.scales_off) + head * 2;
         // Lane i looks up the page of group i of a tile, a tile before its codes and scales are asked for.
         int id = -1, next_id = -1;
-        float key_scale = 0.f, value_scale = 0.f, seen = 0.f;
+        float key_scale = 0.f, value_scale = 0.f, seen = 0.f, top = 0.f;      // seen: the largest scale of values of the last tile that has any; top: of all
         auto look = [&](int j) {
             const int token = (tile0 + j) * KT + 16 * (lane & (GROUPS - 1));
             return j < tiles && lane < GROUPS && token < hi ? cache_page(c, seq, token >> c.page_sh) : -1;
@@ -319,10 +335,11 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             float most = lane < GROUPS && id >= 0 && value_scale == value_scale ? value_scale : 0.f;
             most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
             if (most > 0.f) seen = most;
+            top = fmaxf(top, most);
             if (w == 0 && lane < GROUPS) {
                 const bool none = value_scale != value_scale;     // values that are none: in the scores, whose masked ones do not count
                 const float u = value_scale == 0.f || none ? (seen > 0.f ? seen : 1.f) : value_scale, v = u < 0x1p-120f ? 0x1p-120f : u;
-                page_consts[j & (Sh::kConsts - 1)][lane] = id < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f) : make_float4(none ? value_scale : key_scale, __log2f(v), 1.f / v, 0.f);
+                page_consts[j & (Sh::kConsts - 1)][lane] = id < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f) : make_float4(none ? value_scale : key_scale, __log2f(v), (v >= top * kPromptSmall ? 1.f : -1.f) / v, 0.f);
             }
             uint8_t *kt = smem + Sh::kQ + s * Sh::kKv, *vt = smem + Sh::kQ + (NS + s) * Sh::kKv;
 #pragma unroll

@@ -56,3 +56,39 @@ def test_as_many_steps_as_a_call_may_have():
     B.tman_attend_i8(q, row, y, row, B.DTYPE_F16, heads, cache, 1, 16, heads, width, table, 1, lens, None, S, S, 0.125, 0, ws)
     assert B.tman_read_status(ws) == 0
     assert bool((y == 0).all())
+
+
+@pytest.mark.parametrize("page,n,new,width", [(16, 300, 300, 64), (64, 900, 100, 128), (32, 700, 200, 192), (16, 500, 70, 256)])
+def test_prompts_over_equal_values_are_those(page, n, new, width):
+    """All tokens have the same value, so every row is that, whatever its probabilities: as long as the row's sum is that of the probabilities that were multiplied.
+    In 32 bits: sums of n / 16 tiles and 64 parts, 2^-23 each, and four roundings more; then fp16's own."""
+    rng = np.random.default_rng(n)
+    q = Sequences(io, [n], page, 1, width, rng)
+    v = np.tile(rng.uniform(0.5, 1.0, (1, width)) * rng.choice([-1.0, 1.0], (1, width)), (n, 1))
+    q.append([n], [n], "f16", rng, v=v)
+    _, held = q.oracle.tokens(0, q.table, n)
+    for scale in (0.02, 0.3, 1.0):
+        xd, _ = rows_on_device(rng.standard_normal((new, width)), width, torch.float16)
+        y = H.alloc_matrix(new, width, torch.float16)
+        B.tman_attend_i8(xd, width, y, width, B.DTYPE_F16, 1, q.cache, *q.geometry(), q.table_d, q.table.shape[1], up(np.array([n], dtype=np.int32)),
+                         up(np.array([0, new], dtype=np.int32)), 1, new, scale, 0, q.ws)
+        assert B.tman_read_status(q.ws) == 0
+        ref = np.tile(held[0, 0], (new, 1))
+        within(f64(y), ref, (2.0 ** -11 + (n / 16 + 68) * 2.0 ** -23) * np.abs(ref))
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("small", [2.0 ** -2, 2.0 ** -4, 2.0 ** -12, 2.0 ** -19])
+def test_prompts_that_look_at_pages_of_small_values(small, ty):
+    """Most of each row's probability lies on tokens of values that are small beside the others': what is left of those is right all the same."""
+    rng = np.random.default_rng(23)
+    n = 420
+    q = Sequences(io, [n], 16, 1, 64, rng)
+    k, v = rng.standard_normal((n, 64)) * 0.2, rng.standard_normal((n, 64))
+    for a in (0, 128, 224):
+        k[a:a + 16] += 1.0
+        v[a:a + 16] *= small
+    q.append([n], [n], ty, rng, k=k, v=v)
+    for size in (0.1, 0.4):
+        x = np.abs(rng.standard_normal((202, 64))) * size
+        attend(q, [n], [200], 1, ty, rng, q16=x, scale=0.5)
