@@ -379,8 +379,8 @@ tman_status tman_read_cache_i8(const void *cache, size_t cache_bytes, int pages,
  * TMAN_ERR_UNSUPPORTED.  The cache holds the row's own token already (tman_append_i8).  A row that sees no token (of a sequence of length 0, or of more rows
  * than tokens) is 0.
  * Precision: queries as they are (bf16: exact down to 2^-38 of the row's largest), scores, maxima and sums in 32 bits, probabilities times the value page's
- * scale rounded to 11 bits (or to 2^-25 of the largest so far).  For sequences of 64 rows x heads a key head and more, pages of zero values count in that
- * like their neighbours, and value scales below 2^-120 as that.  The result does not depend on timing. */
+ * scale rounded to 11 bits (or to 2^-25 of the largest so far).  For sequences of 64 rows x heads a key head and more, value scales below 2^-64 of the largest
+ * of the pages in front count as that.  The result does not depend on timing. */
 tman_status tman_attend_i8(const void *q, int ldq, void *y, int ldy, int dtype, int heads, const void *cache, size_t cache_bytes, int pages, int page,
                            int kv_heads, int width, const int32_t *table, int ld_table, const int32_t *lens, const int32_t *starts, int S, int T,
                            float scale, int window, void *workspace, size_t ws_bytes, tman_stream_t stream);

@@ -421,9 +421,11 @@ __global__ void __launch_bounds__(AttendShape<D>::kThreads, 1) attend_kernel(con
         auto store = [&](int r, int col, float4 v) {
             const int rho = it.tile * kAttendRows + r, i = token_of(p, rho);
             const float m = row_max[r], lm = row_lmax[r], l = row_sum[r];
-            const float f = l == 0.f ? 0.f : exp2_fast((m == -INFINITY ? 0.f : m) - (lm == -INFINITY ? 0.f : lm)) / l;
+            // (half of the exponent at a time: values may be so small that all of it is below the least number)
+            const float f1 = exp2_fast(0.5f * ((m == -INFINITY ? 0.f : m) - (lm == -INFINITY ? 0.f : lm))), f2 = l == 0.f ? 0.f : f1 / l;
+            v = make_float4(v.x * f1, v.y * f1, v.z * f1, v.w * f1);
             T *at = static_cast<T *>(p.y) + (size_t)(it.q.row + i) * p.ldy + (size_t)(it.head * p.group + rho - i * p.group) * D + col;
-            *reinterpret_cast<uint2 *>(at) = make_uint2(f4_from_float2<T>(v.x * f, v.y * f), f4_from_float2<T>(v.z * f, v.w * f));
+            *reinterpret_cast<uint2 *>(at) = make_uint2(f4_from_float2<T>(v.x * f2, v.y * f2), f4_from_float2<T>(v.z * f2, v.w * f2));
         };
         float *part = p.parts + ((size_t)blockIdx.x * 2 + (s0 == 0 ? 1 : 0)) * (kAttendRows * (D + 4));
 #pragma unroll 1

@@ -8,7 +8,8 @@
 // A score is (q . code) x (key page's scale) x scale; probabilities carry the value page's scale, p' = 2^(s + log2 vs - M), so that codes are what they are
 // multiplied with, and the row's sum is that of p' / vs, of p' as fp16 holds it: what the rounding takes from a probability it takes from the sum too, so that one
 // that counts for nearly all is not off (with sums ahead of the rounding it was, by up to 2^-12, since M need not be the maximum).  Pages whose values are small
-// beside others' may count for much in the sum and be far down in fp16's range: theirs are added up ahead of the rounding.  They go back to tensor memory over the scores, as the A operand of the second product.  M
+// beside others' may count for much in the sum and be far down in fp16's range: theirs are added up ahead of the rounding.  1 / vs is relative to a power of two
+// that follows the largest vs, so that values of any size have their sum in range; the maximum does not see pages of zeros, whose vs is taken as very small.  They go back to tensor memory over the scores, as the A operand of the second product.  M
 // is the maximum so far and raised, and the output so far scaled, only when a score is above it by more than 10: p' is at most 2^10, rows seldom
 // raise it after their first keys, and one pass over the scores is enough; one that finds such a score is made again behind the raise.
 // 2 x 2048 new tokens over 4096, 32 heads of 128 (floor 87): scores twice from tensor memory and a wait for both products in turn 274 us; with one pass, keys
@@ -38,6 +39,8 @@ struct PromptParams {
 };
 
 constexpr float kPromptSmall = 0.125f;   // scales of values below this much of the largest are small
+constexpr float kPromptLeast = 0x1p-64f; // relative to 2^unit: smaller ones, and zero, count as this
+constexpr int kPromptMargin = 16;        // a scale that is larger than 2^unit by 2^this raises the unit
 constexpr float kPromptSlack = 10.f;     // a score above the maximum so far by this much raises it
 
 // Two fp16 numbers added to two sums in 32 bits.
@@ -55,7 +58,8 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
     extern __shared__ __align__(1024) uint8_t prompt_smem[];
     __shared__ __align__(8) uint64_t q_bar, k_full[NS], k_empty[NS], v_full[NS], v_empty[NS], s_full[RT][2], p_full[RT][2], o_full[RT], all_bar[RT];
     __shared__ uint32_t tmem_slot;
-    __shared__ float4 page_consts[Sh::kConsts][GROUPS];          // of 16 keys: scale of the keys, log2 of the values' scale and its reciprocal, negative: sums ahead of the rounding
+    // of 16 keys: scale of the keys, log2 of the values' scale, its reciprocal times 2^unit (negative: sums ahead of the rounding), unit
+    __shared__ float4 page_consts[Sh::kConsts][GROUPS];
     __shared__ int found[2], sums[Sh::kThreads / 32 + 1];
     const CacheSeqs &c = p.c;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, page_mask = (1 << c.page_sh) - 1;
@@ -172,7 +176,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             const int limit = pos0 + token, low = window_from(limit, p.window);
             const int least_limit = __reduce_min_sync(0xffffffffu, limit), most_low = __reduce_max_sync(0xffffffffu, low);
             const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16), out = at + Sh::kOut + r * D;
-            float M = -INFINITY, l = 0.f;
+            float M = -INFINITY, l = 0.f, unit = 0.f;
             for (int j = 0; j < tiles; ++j) {
                 const int k0 = (tile0 + j) * KT;
                 const bool plain = k0 + KT - 1 <= least_limit && k0 >= most_low;
@@ -201,8 +205,11 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                         }
                         const float next = mx > M + kPromptSlack || M == -INFINITY ? fmaxf(mx, M) : M;
                         const float g = next == M ? 1.f : exp2_fast(M - next);
+                        const float now = consts[0].w, larger = j > 0 ? now - unit : 0.f;      // (l is in units of 2^-(M + unit))
+                        unit = now;
+                        l *= exp2_fast(fminf((next == M ? 0.f : M - next) + larger, 126.f));
+                        l = l > 0x1p126f ? 0x1p126f : l;
                         M = next;
-                        l *= g;
                         if (j > 0) {                             // (behind the product of the tile before)
                             ok = warp_all(mbar_wait(smem_u32(&o_full[r]), (j - 1) & 1));
                             if (!ok) break;
@@ -220,7 +227,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                         }
                     }
                     const float Mu = M == -INFINITY ? 0.f : M;
-                    float mx = -INFINITY;
+                    float mx = -INFINITY, now = 0.f;
                     sum = 0.f;
                     uint32_t z[2][32];
                     tcgen05_ld_32x32b_x32(score, z[0]);
@@ -230,6 +237,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                         float4 c0, c1;
                         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(c0.x), "=f"(c0.y), "=f"(c0.z), "=f"(c0.w) : "r"(smem_u32(consts + 2 * i)) : "memory");
                         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(c1.x), "=f"(c1.y), "=f"(c1.z), "=f"(c1.w) : "r"(smem_u32(consts + 2 * i + 1)) : "memory");
+                        now = c1.w;
                         const float f0 = c0.x * rf, f1 = c1.x * rf, b0 = c0.y - Mu, b1 = c1.y - Mu;
                         if (i == 0) tcgen05_wait_ld();
                         tcgen05_loaded(z[i]);
@@ -260,7 +268,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                         asm volatile("" : "+f"(sum), "+f"(mx));          // (added up here: put off, the values would stay in registers)
                     }
                     // (once: what the maximum was taken of is rounded apart from this by less than a unit)
-                    if (raise || !__any_sync(0xffffffffu, mx > kPromptSlack || (M == -INFINITY && mx != -INFINITY))) break;
+                    if (raise || !__any_sync(0xffffffffu, mx > kPromptSlack || (M == -INFINITY && mx != -INFINITY) || now != unit)) break;
                 }
                 if (!ok) break;
                 l += sum;
@@ -274,7 +282,8 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
             if (ok) {
                 ok = warp_all(mbar_wait(smem_u32(&all_bar[r]), 0));
                 tcgen05_fence_after();
-                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const int e = (int)unit >> 1;
+                const float f1 = __uint_as_float((uint32_t)(127 + e) << 23), f2 = l == 0.f ? 0.f : __uint_as_float((uint32_t)(127 + (int)unit - e) << 23) / l;      // 2^unit / l
                 T *dst = static_cast<T *>(p.y) + (size_t)(q.row + token) * p.ldy + head_at;
 #pragma unroll 1
                 for (int i = 0; ok && i < D; i += 16) {
@@ -285,7 +294,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                     if (real) {
                         uint32_t h[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) h[e] = f4_from_float2<T>(__uint_as_float(z[2 * e]) * inv, __uint_as_float(z[2 * e + 1]) * inv);
+                        for (int e = 0; e < 8; ++e) h[e] = f4_from_float2<T>(__uint_as_float(z[2 * e]) * f1 * f2, __uint_as_float(z[2 * e + 1]) * f1 * f2);
                         *reinterpret_cast<uint4 *>(dst + i) = make_uint4(h[0], h[1], h[2], h[3]);
                         *reinterpret_cast<uint4 *>(dst + i + 8) = make_uint4(h[4], h[5], h[6], h[7]);
                     }
@@ -301,7 +310,10 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
         const float *scales = reinterpret_cast<const float *>(c.cache + c.scales_off) + head * 2;
         // Lane i looks up the page of group i of a tile, a tile before its codes and scales are asked for.
         int id = -1, next_id = -1;
-        float key_scale = 0.f, value_scale = 0.f, seen = 0.f, top = 0.f;      // seen: the largest scale of values of the last tile that has any; top: of all
+        float key_scale = 0.f, value_scale = 0.f, top = 0.f;      // top: the largest scale of values so far
+        int unit = -150;                                         // (below any scale)
+        float2 to_unit = make_float2(0x1p75f, 0x1p75f);          // 2^-unit
+        float small = 0.f;
         auto look = [&](int j) {
             const int token = (tile0 + j) * KT + 16 * (lane & (GROUPS - 1));
             return j < tiles && lane < GROUPS && token < hi ? cache_page(c, seq, token >> c.page_sh) : -1;
@@ -331,15 +343,22 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
         uint32_t ph = 1;                                         // (the first turn of the rings does not wait)
         for (int j = 0; j < tiles; ++j) {
             if (j >= NS && !warp_all(mbar_wait(smem_u32(&k_empty[s]), ph))) { ok = false; break; }
-            // Pages of zero values have no say in how large the others count, so they pass for what is around them.
             float most = lane < GROUPS && id >= 0 && value_scale == value_scale ? value_scale : 0.f;
             most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
-            if (most > 0.f) seen = most;
-            top = fmaxf(top, most);
+            if (most > top) {
+                top = most;
+                const int e = (int)floorf(__log2f(top));
+                if (e >= unit + kPromptMargin) {
+                    unit = e;
+                    to_unit = make_float2(__uint_as_float((uint32_t)(127 - (e >> 1)) << 23), __uint_as_float((uint32_t)(127 - (e - (e >> 1))) << 23));
+                }
+                small = top * to_unit.x * to_unit.y * kPromptSmall;
+            }
             if (w == 0 && lane < GROUPS) {
-                const bool none = value_scale != value_scale;     // values that are none: in the scores, whose masked ones do not count
-                const float u = value_scale == 0.f || none ? (seen > 0.f ? seen : 1.f) : value_scale, v = u < 0x1p-120f ? 0x1p-120f : u;
-                page_consts[j & (Sh::kConsts - 1)][lane] = id < 0 ? make_float4(0.f, -INFINITY, 0.f, 0.f) : make_float4(none ? value_scale : key_scale, __log2f(v), (v >= top * kPromptSmall ? 1.f : -1.f) / v, 0.f);
+                const bool none = value_scale != value_scale;    // values that are none: in the scores, whose masked ones do not count
+                const float v = fmaxf(none ? 0.f : value_scale * to_unit.x * to_unit.y, kPromptLeast), sign = value_scale > 0.f && v >= small ? 1.f : -1.f;
+                page_consts[j & (Sh::kConsts - 1)][lane] =
+                    make_float4(id < 0 ? 0.f : none ? value_scale : key_scale, id < 0 ? -INFINITY : (float)unit + __log2f(v), id < 0 ? 0.f : sign / v, (float)unit);
             }
             uint8_t *kt = smem + Sh::kQ + s * Sh::kKv, *vt = smem + Sh::kQ + (NS + s) * Sh::kKv;
 #pragma unroll

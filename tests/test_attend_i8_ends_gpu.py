@@ -92,3 +92,57 @@ def test_prompts_that_look_at_pages_of_small_values(small, ty):
     for size in (0.1, 0.4):
         x = np.abs(rng.standard_normal((202, 64))) * size
         attend(q, [n], [200], 1, ty, rng, q16=x, scale=0.5)
+
+
+def check_small(q, lens, new, heads, ty, rng, window=0):
+    """Like `attend`, with bf16's least number in place of fp16's: outputs are small."""
+    tt, code = TYPES[ty]
+    st = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T, row = int(st[-1]), heads * q.width
+    xd, xv = rows_on_device(rng.standard_normal((T, row)), row, tt)
+    y = H.alloc_matrix(T, row, tt)
+    B.tman_attend_i8(xd, row, y, row, code, heads, q.cache, *q.geometry(), q.table_d, q.table.shape[1], up(np.array(lens, dtype=np.int32)), up(st), len(lens), T, 0.125,
+                     window, q.ws)
+    assert B.tman_read_status(q.ws) == 0
+    ref, Bs, S, N, P = io.attend(xv.reshape(T, heads, -1), q.oracle, q.table, lens, st, 0.125, window)
+    n = N[:, None, None]
+    # (as for other values, but that log2 of a scale of 2^-140 is off by 2^-22 of 140, 2^-15 of the scale)
+    tol = io.HALF_STEP[ty] * np.abs(ref) + (2.0 ** -134 if ty == "bf16" else 2.0 ** -25)
+    tol = tol + Bs * (2.0 ** -11 + 2.0 ** -14 + 2 * (q.width + 16) * 2.0 ** -23 * S[..., None] + (n / 16 + 64) * 2.0 ** -23) + n * 127 * 2.0 ** -25 * P[..., None]
+    within(f64(y), ref.reshape(T, -1), tol.reshape(T, -1))
+
+
+@pytest.mark.parametrize("exponent", [-60, -104, -113, -118, -124, -128, 60, 110])
+@pytest.mark.parametrize("lens,new", [([300], [300]), ([500, 20], [90, 20]), ([300, 40], [3, 1]), ([5000], [2])])
+def test_values_of_any_size_of_bf16(lens, new, exponent):
+    rng = np.random.default_rng(exponent + 200)
+    q = Sequences(io, lens, 16, 1, 64, rng)
+    q.append(lens, lens, "bf16", rng, v=rng.standard_normal((sum(lens), 64)) * 2.0 ** exponent)
+    check_small(q, lens, new, 2, "bf16", rng)
+    check_small(q, lens, new, 2, "bf16", rng, window=70)
+
+
+@pytest.mark.parametrize("ty,size", [("bf16", 2.0 ** -20), ("bf16", 2.0 ** -90), ("bf16", 2.0 ** 50), ("f16", 2.0 ** -11), ("f16", 1.0)])
+@pytest.mark.parametrize("new", [2, 400])
+def test_pages_of_zeros_in_front_of_all_others(new, ty, size):
+    """Zeros count like their neighbours when there are none in front of them."""
+    rng = np.random.default_rng(17)
+    n = 700
+    q = Sequences(io, [n], 16, 1, 64, rng)
+    v = rng.standard_normal((n, 64)) * size
+    v[:320] = 0
+    v[400:450] = 0
+    q.append([n], [n], ty, rng, v=v)
+    check_small(q, [n], [new], 1, ty, rng)
+
+
+@pytest.mark.parametrize("new", [2, 400])
+@pytest.mark.parametrize("step", [2.0, -2.0])
+def test_value_scales_that_grow_or_shrink_along_the_sequence(new, step):
+    """By 2^2 a page over 2^80: probabilities times scales are what counts, and the sums of probabilities are those of all tokens."""
+    rng = np.random.default_rng(19)
+    n = 640
+    q = Sequences(io, [n], 16, 1, 64, rng)
+    v = rng.standard_normal((n, 64)) * 2.0 ** (step * (np.arange(n) // 16 - 20))[:, None]
+    q.append([n], [n], "bf16", rng, v=v)
+    check_small(q, [n], [new], 1, "bf16", rng)
