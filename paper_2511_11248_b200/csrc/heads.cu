@@ -147,7 +147,7 @@ template <typename T> tman_status launch(HeadParams p, cudaStream_t s)
     p.chunk_mul = p.chunk == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)p.chunk + 1u;
     if ((heads + p.chunk - 1) / p.chunk > 65535) return TMAN_ERR_SHAPE;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((p.T + p.tokens - 1) / p.tokens), (unsigned)((heads + p.chunk - 1) / p.chunk));
+    cfg.gridDim = dim3((unsigned)((p.T - 1) / p.tokens + 1), (unsigned)((heads + p.chunk - 1) / p.chunk));
     cfg.blockDim = dim3(kHeadThreads);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
