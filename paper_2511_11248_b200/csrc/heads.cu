@@ -103,12 +103,26 @@ __global__ void __launch_bounds__(kHeadThreads) norm_rotate_kernel(const __grid_
         }
         const bool query = head < p.q_heads;
         if (query ? p.q_weight != nullptr : p.k_weight != nullptr) {
-            float sum = 0.f;
+            float eps = p.eps;
+            const auto squares = [&] {
+                float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(z[e], z[e], sum);
+                for (int e = 0; e < 8; ++e) sum = fmaf(z[e], z[e], sum);
 #pragma unroll
-            for (int d = LANES / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(mask, sum, d);
-            const float r = rsqrtf(sum * p.inv_width + p.eps);
+                for (int d = LANES / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(mask, sum, d);
+                return fmaf(sum, p.inv_width, eps);
+            };
+            float mean = squares();
+            if constexpr (!std::is_same<T, __half>::value) {
+                if (mean > 0x1p120f || mean < 0x1p-100f) {       // beyond 32 bits: of bf16 values that are very large or small
+                    const float k = mean > 1.f ? 0x1p-80f : 0x1p80f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] *= k;
+                    eps = eps * k * k;
+                    mean = squares();
+                }
+            }
+            const float r = rsqrtf(mean);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 z[2 * e] *= r * (query ? wq[e].x : wk[e].x);
