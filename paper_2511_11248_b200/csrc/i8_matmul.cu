@@ -68,7 +68,7 @@ tman_status launch_i8_quantize(const void *x, int ldx, int dtype, int M, int K, 
 }
 
 // Rows of 16 bits whose codes every CTA of the product works out itself; others are quantized by a launch of their own.
-static bool i8_fused(int M, int K) { return (long long)M * K <= (M == 1 ? 16384 : 8192); }
+static bool i8_fused(int M, int K) { return (long long)M * K <= (M == 1 ? kI8FusedValues : kI8FusedValues / 2); }
 
 size_t i8_workspace_bytes(int op, int M, int K)
 {

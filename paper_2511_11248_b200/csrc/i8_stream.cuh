@@ -20,6 +20,9 @@ namespace {
 
 constexpr int kI8Warps = 16, kI8Threads = 32 * kI8Warps, kI8Channels = 128, kI8Unit = 2048, kI8Slots = 6;
 constexpr int kI8StreamSmem = 216 * 1024;
+constexpr int kI8FusedValues = 16384, kI8FusedSlots = 4;
+static_assert(kI8Warps * kI8FusedSlots * kI8Unit + kI8FusedValues + 8 * 127 + 8 * 8 * kI8Channels <= kI8StreamSmem &&
+              kI8Warps * kI8Slots * kI8Unit + 8 * 8 * kI8Channels <= kI8StreamSmem, "ring, codes and sums fit");
 constexpr int kI8FusedBytes = 64 * 1024; // codes in shared memory at most
 
 struct I8StreamParams {
@@ -200,7 +203,7 @@ __global__ void __launch_bounds__(kI8Threads, 1) i8_stream_kernel(const __grid_c
     }
 }
 
-// Rows of codes, or 16-bit rows whose codes fit kI8FusedBytes (then the ring is shorter).
+// Rows of codes, or 16-bit rows of kI8FusedValues values at most, whose codes are in shared memory (then the ring is shorter).
 template <typename T, bool CODES, int TILES>
 tman_status launch_i8_stream_as(I8StreamParams p, int sms, cudaStream_t s);
 
@@ -215,7 +218,7 @@ tman_status launch_i8_stream(const I8StreamParams &p, cudaStream_t s)
 template <typename T, bool CODES, int TILES>
 tman_status launch_i8_stream_as(I8StreamParams p, int sms, cudaStream_t s)
 {
-    constexpr int SLOTS = CODES ? kI8Slots : 4;
+    constexpr int SLOTS = CODES ? kI8Slots : kI8FusedSlots;
     auto kern = i8_stream_kernel<T, CODES, SLOTS, TILES>;
     static std::atomic<bool> raised[kMaxDevices];
     int dev = 0;
