@@ -67,8 +67,11 @@ tman_status launch_i8_quantize(const void *x, int ldx, int dtype, int M, int K, 
     return dtype == kF4TypeHalf ? quantize<__half>(x, ldx, M, K, a, row_scale, s) : quantize<__nv_bfloat16>(x, ldx, M, K, a, row_scale, s);
 }
 
-// Rows of 16 bits whose codes every CTA of the product works out itself; others are quantized by a launch of their own.
-static bool i8_fused(int M, int K) { return (long long)M * K <= (M == 1 ? kI8FusedValues : kI8FusedValues / 2); }
+// Rows of 16 bits whose codes every CTA of the product works out itself; others are quantized by a launch of their own.  A launch costs some 1.3 us, and every
+// CTA's own work grows with the rows.  In a graph, us, here / with a launch: 1 x 4096 x 4096 6.4 / 7.8, 1 x 14336 x 4096 14.0 / 15.1, 1 x 16384 x 4096 17.9 / 16.6,
+// 1 x 18944 x 3584 16.8 / 17.6, 2 x 2048 x 4096 5.5 / 5.7, 2 x 4096 x 4096 7.0 / 8.0, 2 x 8192 x 4096 10.6 / 11.0, 4 x 2048 x 4096 6.3 / 5.6, 4 x 4096 x 4096
+// 8.2 / 7.8, 8 x 1024 x 4096 7.7 / 4.8.
+static bool i8_fused(int M, int K) { return M <= 2 && M * K <= kI8FusedValues; }
 
 size_t i8_workspace_bytes(int op, int M, int K)
 {
