@@ -324,7 +324,9 @@ tman_status tman_mpgemm_f4(const void *packed, size_t packed_bytes, const void *
  * infinity or a NaN gets codes 0 and the scale NaN, so that its products are NaN.  a: int8 [M][K]. */
 tman_status tman_quantize_tokens_i8(const void *x, int ldx, int dtype, int M, int K, int8_t *a, float *row_scale, tman_stream_t stream);
 
-/* Bytes of scratch, op as for tman_workspace_bytes: 0 = tman_mpgemv_i8, 1 = tman_mpgemm_i8. */
+/* Bytes of scratch, op as for tman_workspace_bytes: 0 = tman_mpgemv_i8, 1 = tman_mpgemm_i8.  One workspace, of the largest size, will do for all calls of 8-bit
+ * integers and of the 8-bit cache that follow one another on a stream.  It must not be one of tman_mpgemv, tman_mpgemv_grouped, tman_mpgemv_ternary or tman_mpgemm
+ * too, whose sums expect what tman_workspace_init wrote: these calls leave codes and sums in it. */
 tman_status tman_workspace_bytes_i8(int op, int M, int K, int N, size_t *out_bytes /*host*/);
 
 /* Decode, M in [1, 8]: quantizes the rows of x in the call; the same result, bit for bit, as tman_quantize_tokens_i8 and tman_mpgemm_i8. */

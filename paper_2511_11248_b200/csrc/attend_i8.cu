@@ -584,7 +584,7 @@ tman_status launch_attend_i8(const CacheSeqs &c, const void *q, int ldq, void *y
     // steps are counted in 32 bits
     const long long steps = ((long long)c.ldt << c.page_sh) / 16 + kItemCost, tiles = ((prompts ? kPromptRows : rows) + kAttendRows - 1) / kAttendRows;
     if (tiles * steps > INT32_MAX || tiles * steps * c.heads > INT32_MAX || tiles * steps * c.heads * c.S > INT32_MAX) return TMAN_ERR_UNSUPPORTED;
-    const AttendParams p = {c, q, y, reinterpret_cast<float *>(w8 + kWsStatusBytes + kAttendCtas * 4), reinterpret_cast<uint32_t *>(w8 + kWsStatusBytes),
+    const AttendParams p = {c, q, y, reinterpret_cast<float *>(w8 + kI8ScratchOff), reinterpret_cast<uint32_t *>(w8 + kWsStatusBytes),
                             ldq, ldy, group, window, prompts ? kPromptRows : INT_MAX, group == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)group + 1u, scale};
     return dtype == kF4TypeHalf ? launch_width<__half>(p, s) : launch_width<__nv_bfloat16>(p, s);
 }

@@ -26,10 +26,9 @@ struct CacheSeqs {
 inline size_t cache_scales_off(int pages, int page, int heads, int width) { return up256((size_t)pages * heads * 2 * page * width); }
 inline size_t cache_bytes(int pages, int page, int heads, int width) { return cache_scales_off(pages, page, heads, width) + (size_t)pages * heads * 8; }
 
-constexpr int kAttendCtas = 320;         // at most
 constexpr int kAttendRows = 16;          // rows of a tile
 inline size_t attend_slot_bytes(int width) { return (size_t)kAttendRows * (width + 4) * 4; }
-inline size_t attend_workspace_bytes(int width) { return kWsStatusBytes + kAttendCtas * 4 + 2 * kAttendCtas * attend_slot_bytes(width); }
+inline size_t attend_workspace_bytes(int width) { return kI8ScratchOff + 2 * kAttendCtas * attend_slot_bytes(width); }
 
 tman_status launch_append_i8(const CacheSeqs &c, const void *k, int ldk, const void *v, int ldv, int dtype, cudaStream_t s);
 tman_status launch_read_cache_i8(const CacheSeqs &c, void *k, int ldk, void *v, int ldv, int dtype, cudaStream_t s);

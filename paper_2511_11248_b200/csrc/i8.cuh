@@ -8,6 +8,11 @@
 namespace tman {
 
 constexpr int kI8MaxK = 131056;          // products of two bytes, 2^14 at most, in 32-bit sums
+// Workspace: status word (kWsStatusBytes), the counters of attention, which are at rest between calls, and behind them what a call leaves lying: codes of a decode
+// product, parts of attention.  So that the calls of 8-bit integers can have one workspace in turn.
+constexpr int kAttendCtas = 320;         // of attention, at most
+constexpr size_t kI8ScratchOff = kWsStatusBytes + kAttendCtas * sizeof(uint32_t);
+static_assert(kI8ScratchOff % 256 == 0, "codes are read in 16-byte pieces");
 
 // entry points implemented per file
 tman_status launch_i8_quantize(const void *x, int ldx, int dtype, int M, int K, int8_t *a, float *row_scale, cudaStream_t s);

@@ -75,7 +75,7 @@ static bool i8_fused(int M, int K) { return M <= 2 && M * K <= kI8FusedValues; }
 
 size_t i8_workspace_bytes(int op, int M, int K)
 {
-    return kWsStatusBytes + (op == 0 && !i8_fused(M, K) ? up256((size_t)M * K) + up256(M * sizeof(float)) : 0);
+    return op == 0 && !i8_fused(M, K) ? kI8ScratchOff + up256((size_t)M * K) + up256(M * sizeof(float)) : kWsStatusBytes;
 }
 
 tman_status launch_i8_gemv(const int8_t *w, int ldw, const float *w_scale, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N,
@@ -84,8 +84,8 @@ tman_status launch_i8_gemv(const int8_t *w, int ldw, const float *w_scale, const
     uint8_t *w8 = static_cast<uint8_t *>(ws);
     const I8StreamParams p = {w, x, w_scale, nullptr, y, ldw, ldx, ldy, M, K, N, 0, 0};
     if (i8_fused(M, K)) return dtype == kF4TypeHalf ? launch_i8_stream<__half, false>(p, s) : launch_i8_stream<__nv_bfloat16, false>(p, s);
-    int8_t *a = reinterpret_cast<int8_t *>(w8 + kWsStatusBytes);
-    float *a_scale = reinterpret_cast<float *>(w8 + kWsStatusBytes + up256((size_t)M * K));
+    int8_t *a = reinterpret_cast<int8_t *>(w8 + kI8ScratchOff);
+    float *a_scale = reinterpret_cast<float *>(w8 + kI8ScratchOff + up256((size_t)M * K));
     const tman_status st = launch_i8_quantize(x, ldx, dtype, M, K, a, a_scale, s);
     if (st != TMAN_OK) return st;
     return launch_i8_gemm(w, ldw, w_scale, a, a_scale, y, ldy, dtype, M, K, N, ws, s);

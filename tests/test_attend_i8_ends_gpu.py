@@ -146,3 +146,22 @@ def test_value_scales_that_grow_or_shrink_along_the_sequence(new, step):
     v = rng.standard_normal((n, 64)) * 2.0 ** (step * (np.arange(n) // 16 - 20))[:, None]
     q.append([n], [n], "bf16", rng, v=v)
     check_small(q, [n], [new], 1, "bf16", rng)
+
+
+@pytest.mark.parametrize("M", [1, 5, 8])
+def test_products_and_attention_over_long_contexts_have_one_workspace_in_turn(M):
+    """A decode product leaves codes in the workspace, attention parts of heads that several CTAs share: neither is in the other's way."""
+    rng = np.random.default_rng(M)
+    lens, K, N = [5000] * M, 18944, 512
+    q = Sequences(io, lens, 16, 2, 64, rng)
+    q.append(lens, lens, "f16", rng)
+    size = max(B.tman_workspace_bytes_attend(64), B.tman_workspace_bytes_i8(B.OP_GEMV, M, K, N))
+    q.ws = workspace(size)
+    x, w, s = up(rng.standard_normal((M, K))).half(), up(rng.integers(-127, 128, (N, K)).astype(np.int8)), torch.ones(N, device="cuda")
+    first = None
+    for _ in range(3):
+        y = H.alloc_matrix(M, N, torch.float16)
+        B.tman_mpgemv_i8(w, K, s * 1e-4, x, K, y, N, B.DTYPE_F16, M, K, N, q.ws)
+        first = y if first is None else first
+        attend(q, lens, [1] * M, 8, "f16", rng)
+        assert torch.equal(y.view(torch.int16), first.view(torch.int16))
