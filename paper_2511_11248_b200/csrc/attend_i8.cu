@@ -17,7 +17,16 @@
 namespace tman {
 namespace {
 
-constexpr int kPromptRows = 64;          // rows of a sequence from which the kernel for prompts takes it
+// Rows of a sequence from which the kernel for prompts takes it.  Here every 16 rows read the keys again, and all of that is spread over all CTAs; there up to 256 rows
+// read them once, but one CTA walks over all of a key head's.  32 heads on 8 of 128, us in a graph, here / there:
+//   rows      8 x 512     8 x 4096    8 x 32768   1 x 512     1 x 4096    1 x 32768 tokens
+//   32        12 / 17     42 / 94     207 / 682   11 / 17     16 / 74     39 / 665
+//   64        20 / 17     71 / 94     392 / 682   11 / 17     22 / 74     65 / 666
+//   128       37 / 18     128 / 95    761 / 684   14 / 18     29 / 75     113 / 666
+//   256       74 / 24     245 / 107   1539 / 749  17 / 24     46 / 91     205 / 734
+//   512       162 / 25    497 / 104   3440 / 732  34 / 24     83 / 92     394 / 719
+// The line is right for several sequences of some hundred tokens; where there are fewer (sequences x key heads) than multiprocessors it comes too soon.
+constexpr int kPromptRows = 64;
 constexpr int kItemCost = 48;            // steps that beginning and ending a head are worth
 constexpr int kShortSteps = 96;          // heads of so few steps are not cut
 constexpr uint32_t kNoneYet = 0x7FA5A5A5u;      // what tman_workspace_init writes: a counter at rest
