@@ -315,7 +315,7 @@ tman_status tman_mpgemm_f4(const void *packed, size_t packed_bytes, const void *
  * (No counterpart in the paper, whose integer path has one scale for all weights.)  y[m][n] = a_scale[m] w_scale[n] sum_k a[m][k] w[n][k].
  *   - w: int8 [N][K], one row per output channel, rows ldw bytes apart (ldw >= K, a multiple of 16; 16-byte aligned), w_scale fp32 [N]; as a
  *     checkpoint holds them, or as tman_quantize_tokens_i8 makes them of 16-bit weights.
- *   - K a multiple of 16, at most 131056; any N.  dtype, ldx, ldy, x and y as for 4-bit floating point.  Codes are 16-byte aligned.
+ *   - K a multiple of 16, at most 131056; M and N at most 2^30.  dtype, ldx, ldy, x and y as for 4-bit floating point.  Codes are 16-byte aligned.
  *   - Sums are exact 32-bit integers; the product with the two scales is right to 2^-22 before y's rounding, whatever the scales' sizes.
  *   - Everything is read behind the kernels ahead on the stream: no rule about what they write. */
 
@@ -333,7 +333,7 @@ tman_status tman_workspace_bytes_i8(int op, int M, int K, int N, size_t *out_byt
 tman_status tman_mpgemv_i8(const int8_t *w, int ldw, const float *w_scale, const void *x, int ldx, void *y, int ldy, int dtype, int M, int K, int N,
                            void *workspace, size_t ws_bytes, tman_stream_t stream);
 
-/* Any M >= 1, activations quantized (a: int8 [M][K], a_scale fp32 [M]). */
+/* Any number of rows, activations quantized (a: int8 [M][K], a_scale fp32 [M]). */
 tman_status tman_mpgemm_i8(const int8_t *w, int ldw, const float *w_scale, const int8_t *a, const float *a_scale, void *y, int ldy, int dtype, int M,
                            int K, int N, void *workspace, size_t ws_bytes, tman_stream_t stream);
 
@@ -353,7 +353,7 @@ tman_status tman_norm_rotate(const void *x, int ldx, void *y, int ldy, int dtype
  * (No counterpart in the paper.)  The cache has `pages` pages; a page holds `page` consecutive tokens of one sequence (16, 32, 64 or 128), for
  * `kv_heads` heads of `width` values (64, 128, 192 or 256).  Keys of a page and head have one scale, values another; what is held is code x scale,
  * codes in [-127, 127] (layout: csrc/cache_i8.cuh).  The buffer needs no preparation; its size counts what pages may be named.
- * Sequences, S of them: lens[s] tokens, the newest included; table[s * ld_table + i] (int32) is the page of tokens i * page ..; a call's rows of sequence s,
+ * Sequences, S of them (at most 2^30): lens[s] tokens, the newest included; table[s * ld_table + i] (int32) is the page of tokens i * page ..; a call's rows of sequence s,
  * starts[s] .. starts[s + 1] - 1 (int32 [S + 1], T rows in all), are its last tokens; starts NULL: one row each (T = S).  All are device
  * memory.  Rows behind the last sequence's are left alone.
  * What only the device can see is reported in the status word as TMAN_ERR_INDEX, and skipped: sequences whose rows lie outside of [0, T) or

@@ -381,7 +381,7 @@ tman_status tman_mpgemm_f4(const void *packed, size_t packed_bytes, const void *
 static tman_status check_i8_weights(const int8_t *w, int ldw, const float *w_scale, int K, int N)
 {
     if (!w || !w_scale) return TMAN_ERR_NULL;
-    if (K < 16 || K % 16 != 0 || K > kI8MaxK || N < 1 || ldw < K || ldw % 16 != 0) return TMAN_ERR_SHAPE;
+    if (K < 16 || K % 16 != 0 || K > kI8MaxK || N < 1 || N > kI8MaxRows || ldw < K || ldw % 16 != 0) return TMAN_ERR_SHAPE;
     return aligned_to(w, 16) && aligned_to(w_scale, 4) ? TMAN_OK : TMAN_ERR_SHAPE;
 }
 static tman_status check_i8_tokens(const int8_t *a, const float *a_scale, int M, int K)
@@ -402,7 +402,7 @@ tman_status tman_workspace_bytes_i8(int op, int M, int K, int N, size_t *out_byt
 {
     if (!out_bytes) return TMAN_ERR_NULL;
     if (op < 0 || op > 1) return TMAN_ERR_UNSUPPORTED;
-    if (M < 1 || (op == 0 && M > 8) || K < 16 || K % 16 != 0 || K > kI8MaxK || N < 1) return TMAN_ERR_SHAPE;
+    if (M < 1 || (op == 0 && M > 8) || M > kI8MaxRows || K < 16 || K % 16 != 0 || K > kI8MaxK || N < 1 || N > kI8MaxRows) return TMAN_ERR_SHAPE;
     *out_bytes = i8_workspace_bytes(op, M, K);
     return TMAN_OK;
 }
@@ -423,6 +423,7 @@ tman_status tman_mpgemm_i8(const int8_t *w, int ldw, const float *w_scale, const
 {
     TMAN_F4_CHECK(check_i8_weights(w, ldw, w_scale, K, N));
     TMAN_F4_CHECK(check_i8_tokens(a, a_scale, M, K));
+    if (M > kI8MaxRows) return TMAN_ERR_SHAPE;
     TMAN_F4_CHECK(check_f4_output(y, ldy, dtype, N));
     TMAN_F4_CHECK(check_f4_workspace(workspace, ws_bytes, i8_workspace_bytes(1, M, K)));
     return launch_i8_gemm(w, ldw, w_scale, a, a_scale, y, ldy, dtype, M, K, N, workspace, reinterpret_cast<cudaStream_t>(stream));
@@ -457,7 +458,7 @@ static tman_status check_cache(const void *cache, size_t bytes, int pages, int p
     TMAN_F4_CHECK(check_cache_format(pages, page, kv_heads, width));
     if (bytes < cache_bytes(pages, page, kv_heads, width)) return TMAN_ERR_BUFFER_TOO_SMALL;
     if (!aligned_to(cache, 256) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_to(starts, 4)) return TMAN_ERR_SHAPE;
-    return ld_table < 1 || S < 1 || T < 1 || (!starts && T != S) ? TMAN_ERR_SHAPE : TMAN_OK;
+    return ld_table < 1 || S < 1 || S > kI8MaxRows || T < 1 || (!starts && T != S) ? TMAN_ERR_SHAPE : TMAN_OK;
 }
 static tman_status check_cache_rows(const void *x, int ld, int dtype, long long row, int T)
 {

@@ -8,6 +8,7 @@
 namespace tman {
 
 constexpr int kI8MaxK = 131056;          // products of two bytes, 2^14 at most, in 32-bit sums
+constexpr int kI8MaxRows = 1 << 30;      // rows and channels of products, sequences: their indexes go on for a tile or a CTA's share behind the last
 // Workspace: status word (kWsStatusBytes), the counters of attention, which are at rest between calls, and behind them what a call leaves lying: codes of a decode
 // product, parts of attention.  So that the calls of 8-bit integers can have one workspace in turn.
 constexpr int kAttendCtas = 320;         // of attention, at most
