@@ -10,8 +10,8 @@
 // Scores are products of 16-bit queries and codes, 32-bit sums, times the key page's scale.  Probabilities meet the values as fp16 numbers
 // p x (scale of the value page), relative to the largest of those so far: each off by 2^-12 of itself, or 2^-25 of that largest one.  Sums and maxima are
 // held in 32 bits.  A bf16 query row is brought into fp16 by a power of two, exact down to 2^-38 of its largest value.
-// Measured: 32 sequences of 9830 to 32768 tokens, 28 heads on 4 of 128, 144 us (floor 108; the stream itself at 6.1 TB/s, 8 us its start and end); one of
-// 500 tokens 9.2, the chain from lengths to pages to keys to sums.
+// Measured: 32 sequences of 9830 to 32768 tokens, 28 heads on 4 of 128, 145 us in a graph (floor 108): 4.9 TB/s over the call, some 8 us of it start and end; one of
+// 500 tokens 9.1, the chain from lengths to pages to keys to sums.
 #include "attend_prompt.cuh"
 
 namespace tman {

@@ -9,11 +9,13 @@
 // multiplied with, and the row's sum is that of p' / vs, of p' as fp16 holds it: what the rounding takes from a probability it takes from the sum too, so that one
 // that counts for nearly all is not off (with sums ahead of the rounding it was, by up to 2^-12, since M need not be the maximum).  Pages whose values are small
 // beside others' may count for much in the sum and be far down in fp16's range: theirs are added up ahead of the rounding.  1 / vs is relative to a power of two
-// that follows the largest vs, so that values of any size have their sum in range; the maximum does not see pages of zeros, whose vs is taken as very small.  They go back to tensor memory over the scores, as the A operand of the second product.  M
+// that follows the largest vs, so that values of any size have their sum in range; the maximum does not see pages of zeros, whose vs is taken as very small.
+// Probabilities go back to tensor memory over the scores, as the A operand of the second product.  M
 // is the maximum so far and raised, and the output so far scaled, only when a score is above it by more than 10: p' is at most 2^10, rows seldom
 // raise it after their first keys, and one pass over the scores is enough; one that finds such a score is made again behind the raise.
 // 2 x 2048 new tokens over 4096, 32 heads of 128 (floor 87): scores twice from tensor memory and a wait for both products in turn 274 us; with one pass, keys
-// 128 at a time, 197 (two threads a row instead of one made no difference); this 190, a tile of 64 keys in 2250 clocks.
+// 128 at a time, 197 (two threads a row instead of one made no difference); keys 64 at a time 190, a tile in 2250 clocks;
+// with sums of the rounded probabilities, this, 197.
 #pragma once
 
 #include "attend.cuh"
