@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             float s0 = 0.f, s1 = 0.f;
-                            const float unit = half == 0 ? c0.z : c1.z;
+                            const float inverse = half == 0 ? c0.z : c1.z;
                             const auto add16 = [&](auto as_rounded) {
 #pragma unroll
                                 for (int e = 16 * half; e < 16 * half + 16; e += 2) {
@@ -264,8 +264,8 @@ __global__ void __launch_bounds__(PromptShape<D>::kThreads, 1) attend_prompt_ker
                                     else { s0 += u; s1 += v; }
                                 }
                             };
-                            if (unit >= 0.f) add16(std::true_type()); else add16(std::false_type());
-                            sum = fmaf(s0 + s1, fabsf(unit), sum);
+                            if (inverse >= 0.f) add16(std::true_type()); else add16(std::false_type());
+                            sum = fmaf(s0 + s1, fabsf(inverse), sum);
                         }
                         asm volatile("" : "+f"(sum), "+f"(mx));          // (added up here: put off, the values would stay in registers)
                     }
